@@ -22,6 +22,9 @@
  *   dkv_page_select   zero-copy alternative to the pack: the retained runs
  *                     of a paged cache, listed in place
  *   dkv_paged_decode_attn  decode over a paged cache through those entries
+ *   dkv_page_extend   page tables, slots and entries of growing requests, built
+ *                     from their lengths (dkv_page_release: pages back)
+ *   dkv_paged_append  new tokens -> their slots in the pages
  *   dkv_topk_pattern  the exact-budget export of a pattern from retention
  *                     probabilities (K_rho largest entries)
  *
@@ -555,6 +558,119 @@ dkv_status dkv_paged_append_decode_attn(dkv_dtype dtype, int32_t batch, int32_t 
                                         int32_t max_entries, int32_t context_len,
                                         float sm_scale, int64_t rows_hint, float *out,
                                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Filling a paged cache
+ * ---------------------
+ * A server that admits and grows requests on the GPU needs no host copy of
+ * its tables: dkv_page_extend gives every request the pages for its new
+ * tokens and says where each token's rows go, dkv_paged_append writes them,
+ * dkv_paged_query_attn lets the new tokens attend to what their request
+ * holds, and dkv_page_release takes pages back (the ones a selection marks
+ * unused, or all of a finished request).
+ *
+ * Units and segments are those of the other calls: unit n is one (layer,
+ * sequence), segment s = n * Hkv + g, and every segment has pages of its own
+ * (its KV head's rows of positions [p * page_rows, (p + 1) * page_rows)).
+ * Tokens are token-major: row tok_off[n] + t of the batch's arrays is new
+ * token t of unit n, as a model's activations lie.
+ *
+ * Free pages stand on a stack: free_pages[0 .. *n_free) (device), the top at
+ * the end; *n_free is taken within [0, free_cap].  An output that has an
+ * input's meaning (new_len and unit_len, n_free_out and n_free, table_out and
+ * page_table) may be the same buffer, which updates it in place; otherwise
+ * outputs and inputs must not overlap.
+ */
+
+/* Workspace bytes of dkv_page_extend (host, no GPU call). */
+size_t dkv_page_extend_workspace_bytes(int32_t num_units);
+
+/*
+ * dkv_page_extend -- page tables, slots and entries from lengths.
+ *
+ * unit_new    int32 [N]: tokens to add to each unit.
+ * unit_len    int32 [N]: positions that each unit holds (0 for a new request);
+ *             its segments' pages for them are in page_table.
+ * new_len     out, int32 [N]: unit_len + unit_new, or unit_len for a unit that
+ *             is not served.
+ * n_free_out  out, int32 [1]: the stack's height afterwards.
+ * page_table  int32 [N * Hkv][pages_per_seg], in and out: the new pages' words
+ *             are written, all others stay.  A unit needs
+ *             Hkv * (ceil((len + new) / page_rows) - ceil(len / page_rows))
+ *             pages; page i of the call, segment by segment and page by page,
+ *             is the i-th from the top of the stack.
+ * tok_off     out, int32 [N + 1]: exclusive sums of the new tokens (a negative
+ *             unit_new counts as 0), at most max_tokens.
+ * first_pos   out, int32 [N]: position of the unit's first new token (its
+ *             unit_len), or -1 when it is not served.
+ * slots       out, int64 [max_tokens][Hkv]: pool row (page * page_rows + slot)
+ *             of every new token and head; -1 for tokens of units that are not
+ *             served, for tokens whose page is negative, and for all rows at
+ *             or past tok_off[N] (a padded batch writes nothing there).
+ * entries     optional (NULL with max_entries = 0), int32
+ *             [N * Hkv][max_entries][4], 16-byte aligned, in and out: entry p
+ *             of a segment is (page, p, 0, slots filled) for its page p, the
+ *             format of dkv_page_select for an unpruned cache; the entries of
+ *             the pages that got tokens are written, below max_entries.
+ * n_entries   optional, int32 [N * Hkv], in and out: set to the pages of every
+ *             served unit that got tokens (even above max_entries).
+ * pages_needed optional out, int64 [1]: pages needed by all units that could
+ *             be served with enough free pages.
+ * A unit is not served when its length or new tokens are negative, its new
+ * length passes pages_per_seg * page_rows (or 2^31 - 1), its rows do not lie
+ * wholly below max_tokens, or the pages it needs, counted behind those of all
+ * the units before it, pass the free ones.  Nothing of it changes; a unit that
+ * needs no page is not held up by the ones before it.
+ * DKV_ERR_UNSUPPORTED when N * Hkv > 65535 or max_tokens * Hkv > 2^32 - 256.
+ * The call enqueues one kernel over the units and one over the tokens.
+ */
+dkv_status dkv_page_extend(int32_t num_units, int32_t num_kv_heads, int32_t page_rows,
+                           const int32_t *unit_new, const int32_t *unit_len, int32_t *new_len,
+                           const int32_t *free_pages, int32_t free_cap, const int32_t *n_free,
+                           int32_t *n_free_out, int32_t *page_table, int32_t pages_per_seg,
+                           int32_t *tok_off, int32_t *first_pos, int64_t *slots,
+                           int32_t max_tokens, int32_t *entries, int32_t *n_entries,
+                           int32_t max_entries, int64_t *pages_needed, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/* Workspace bytes of dkv_page_release (host, no GPU call). */
+size_t dkv_page_release_workspace_bytes(int32_t num_segments, int32_t pages_per_seg);
+
+/*
+ * dkv_page_release -- pages back to the stack.
+ *
+ * page_table  int32 [nseg][pages_per_seg]; negative words name no page.
+ * keep        optional uint8 [nseg][pages_per_seg]: a page goes when its byte
+ *             is 0 (e.g. page_used of dkv_page_select); NULL: every page goes.
+ * table_out   out, int32 [nseg][pages_per_seg]: -1 for the pages that went, the
+ *             word of page_table otherwise.
+ * free_pages  the pages that go are pushed on the stack in table order, below
+ *             free_cap; a page that finds no room stays in the table.
+ * n_free_out  out, int32 [1]: the stack's height afterwards.
+ * A page that two words name is pushed twice: give every page one owner.
+ * DKV_ERR_UNSUPPORTED when nseg * pages_per_seg > 2^31 - 1.
+ */
+dkv_status dkv_page_release(int32_t num_segments, int32_t pages_per_seg, const int32_t *page_table,
+                            const uint8_t *keep, int32_t *table_out, int32_t *free_pages,
+                            int32_t free_cap, const int32_t *n_free, int32_t *n_free_out,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dkv_paged_append -- rows of new tokens into their slots (Sec. 3.4: appended
+ * tokens are retained in full).
+ *
+ * k_new, v_new  [num_tokens][Hkv][d], tokens token_stride elements apart
+ *               (>= Hkv * d, a multiple of 16 bytes; the K and V parts of a
+ *               fused projection's rows can be passed where they are).
+ * slots         int64 [num_tokens][Hkv] as dkv_page_extend writes them; a
+ *               token and head with a slot outside [0, num_pages * page_rows)
+ *               is skipped.  Two rows with the same slot leave either of them.
+ * k_pages, v_pages  the pools, [num_pages][page_rows][d].
+ */
+dkv_status dkv_paged_append(dkv_dtype dtype, int32_t num_tokens, int32_t num_kv_heads,
+                            int32_t head_dim, const void *k_new, const void *v_new,
+                            int64_t token_stride, const int64_t *slots, void *k_pages,
+                            void *v_pages, int64_t num_pages, int32_t page_rows, void *stream);
 
 /* Static description of a status code. */
 const char *dkv_status_string(dkv_status status);

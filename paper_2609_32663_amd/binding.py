@@ -25,6 +25,8 @@ __all__ = [
     "dkv_page_select_workspace_bytes", "dkv_page_entries_bound", "dkv_page_select",
     "dkv_paged_decode_attn", "dkv_paged_append_decode_attn", "dkv_budget_entries",
     "dkv_topk_workspace_bytes", "dkv_topk_pattern", "dkv_map_pattern_ragged",
+    "dkv_page_extend_workspace_bytes", "dkv_page_extend", "dkv_page_release_workspace_bytes", "dkv_page_release",
+    "dkv_paged_append",
 ]
 
 (DKV_OK, DKV_ERR_INVALID_ARG, DKV_ERR_UNSUPPORTED, DKV_ERR_MISALIGNED, DKV_ERR_CAPACITY,
@@ -122,6 +124,12 @@ def library_at(path):
         "dkv_topk_workspace_bytes": (SZ, [I32, I32, I32]),
         "dkv_map_pattern_ragged": (I32, [P, VP, VP, VP, VP, VP, VP]),
         "dkv_topk_pattern": (I32, [I32, I32, I32, VP, I64, VP, VP, SZ, VP]),
+        "dkv_page_extend_workspace_bytes": (SZ, [I32]),
+        "dkv_page_extend": (I32, [I32, I32, I32, VP, VP, VP, VP, I32, VP, VP, VP, I32, VP, VP, VP, I32, VP, VP, I32,
+                                  VP, VP, SZ, VP]),
+        "dkv_page_release_workspace_bytes": (SZ, [I32, I32]),
+        "dkv_page_release": (I32, [I32, I32, VP, VP, VP, VP, I32, VP, VP, VP, SZ, VP]),
+        "dkv_paged_append": (I32, [I32, I32, I32, I32, VP, VP, I64, VP, VP, VP, I64, I32, VP]),
         "dkv_compact_bins_workspace_bytes": (SZ, [P]),
         "dkv_compact_bins": (I32, [P, I32, VP, VP, VP, I32, VP, VP, I64, VP, VP, VP, VP, VP, SZ, VP]),
         "dkv_compact_bins_ragged": (I32, [P, VP, I32, VP, VP, VP, I32, VP, VP, I64, VP, VP, VP, VP, VP, SZ, VP]),
@@ -159,6 +167,29 @@ def _dev(t, name, optional=False):
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
+
+
+def _rows(t, name, heads, dim, dtype):
+    """Data pointer and token stride (elements) of [tokens][heads][dim] rows whose tokens may be further apart
+    than heads * dim: a part of a fused projection's output."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"{name} must be {dtype} [tokens][{heads}][{dim}]")
+    one, st = t.shape[0] <= 1, t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != dim) or (not one and st[0] < heads * dim):
+        raise ValueError(f"{name} must hold each token's heads as consecutive rows, tokens not overlapping")
+    return t.data_ptr(), heads * dim if one else st[0]
+
+
+def _typed(t, name, dtype, shape=None, optional=False):
+    """_dev of a tensor of this element type (and shape)."""
+    if t is None and optional:
+        return None
+    p = _dev(t, name)
+    if t.dtype != dtype or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be {dtype}" + ("" if shape is None else f" of shape {list(shape)}"))
+    return p
 
 
 try:  # the current stream's handle without a Stream object around it
@@ -418,3 +449,64 @@ def dkv_map_pattern_ragged(layout, unit_len, pattern, kv_mask, kv_len, q_mask=No
     _check("dkv_map_pattern_ragged", library().dkv_map_pattern_ragged(
         ctypes.byref(layout), _dev(unit_len, "unit_len"), _dev(pattern, "pattern"), _dev(kv_mask, "kv_mask"),
         _dev(kv_len, "kv_len"), _dev(q_mask, "q_mask", optional=True), _stream(stream)))
+
+
+def dkv_page_extend_workspace_bytes(num_units):
+    return library().dkv_page_extend_workspace_bytes(int(num_units))
+
+
+def dkv_page_extend(unit_new, unit_len, free_pages, n_free, page_table, page_rows, num_kv_heads, tok_off, first_pos,
+                    slots, workspace, new_len=None, n_free_out=None, entries=None, n_entries=None, pages_needed=None,
+                    stream=None):
+    """unit_new, unit_len: int32 [N]; free_pages: int32 stack, n_free: int32 [1] its height; page_table: int32
+    [N*Hkv][pages_per_seg]; tok_off: int32 [N+1], first_pos: int32 [N], slots: int64 [max_tokens][Hkv] (out);
+    new_len, n_free_out: unit_len and n_free in place when not given; entries: optional int32
+    [N*Hkv][max_entries][4], n_entries: optional int32 [N*Hkv]; pages_needed: optional int64 [1]."""
+    N, Hkv, i32 = unit_len.shape[0], int(num_kv_heads), torch.int32
+    nseg, pps = page_table.shape
+    if nseg != N * Hkv or slots.dim() != 2 or slots.shape[1] != Hkv:
+        raise ValueError("page_table must have N * Hkv rows and slots Hkv columns")
+    max_entries = 0 if entries is None else entries.shape[1]
+    _check("dkv_page_extend", library().dkv_page_extend(
+        N, Hkv, int(page_rows), _typed(unit_new, "unit_new", i32, (N,)), _typed(unit_len, "unit_len", i32, (N,)),
+        _typed(unit_len if new_len is None else new_len, "new_len", i32, (N,)),
+        _typed(free_pages, "free_pages", i32), free_pages.numel(), _typed(n_free, "n_free", i32, (1,)),
+        _typed(n_free if n_free_out is None else n_free_out, "n_free_out", i32, (1,)),
+        _typed(page_table, "page_table", i32), pps, _typed(tok_off, "tok_off", i32, (N + 1,)),
+        _typed(first_pos, "first_pos", i32, (N,)), _typed(slots, "slots", torch.int64), slots.shape[0],
+        _typed(entries, "entries", i32, (nseg, max_entries, 4), True), _typed(n_entries, "n_entries", i32, (nseg,), True),
+        max_entries, _typed(pages_needed, "pages_needed", torch.int64, (1,), True), _dev(workspace, "workspace"),
+        workspace.nbytes, _stream(stream)))
+
+
+def dkv_page_release_workspace_bytes(num_segments, pages_per_seg):
+    return library().dkv_page_release_workspace_bytes(int(num_segments), int(pages_per_seg))
+
+
+def dkv_page_release(page_table, free_pages, n_free, workspace, keep=None, table_out=None, n_free_out=None, stream=None):
+    """page_table: int32 [nseg][pages_per_seg]; free_pages: int32 stack, n_free: int32 [1] its height; keep: optional
+    uint8 of page_table's shape (None: every page goes); table_out, n_free_out: in place when not given."""
+    shape, i32 = tuple(page_table.shape), torch.int32
+    if len(shape) != 2:
+        raise ValueError("page_table must be [nseg][pages_per_seg]")
+    _check("dkv_page_release", library().dkv_page_release(
+        shape[0], shape[1], _typed(page_table, "page_table", i32), _typed(keep, "keep", torch.uint8, shape, True),
+        _typed(page_table if table_out is None else table_out, "table_out", i32, shape),
+        _typed(free_pages, "free_pages", i32), free_pages.numel(), _typed(n_free, "n_free", i32, (1,)),
+        _typed(n_free if n_free_out is None else n_free_out, "n_free_out", i32, (1,)), _dev(workspace, "workspace"),
+        workspace.nbytes, _stream(stream)))
+
+
+def dkv_paged_append(k_new, v_new, slots, k_pages, v_pages, stream=None):
+    """k_new, v_new: [tokens][Hkv][d], tokens evenly spaced (views of a fused projection included); slots: int64
+    [tokens][Hkv]; k_pages, v_pages: [num_pages][page_rows][d]."""
+    num_pages, page_rows, dim = k_pages.shape
+    tokens, Hkv = slots.shape
+    k_ptr, stride = _rows(k_new, "k_new", Hkv, dim, k_pages.dtype)
+    v_ptr, v_stride = _rows(v_new, "v_new", Hkv, dim, k_pages.dtype)
+    if k_new.shape[0] != tokens or v_new.shape[0] != tokens or v_stride != stride:
+        raise ValueError("k_new and v_new must have a row per row of slots, evenly spaced alike")
+    _check("dkv_paged_append", library().dkv_paged_append(
+        dtype_code(k_pages.dtype), tokens, Hkv, dim, k_ptr, v_ptr, stride, _typed(slots, "slots", torch.int64),
+        _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", k_pages.dtype, (num_pages, page_rows, dim)), num_pages,
+        page_rows, _stream(stream)))

@@ -110,6 +110,57 @@ struct PageSelectParams {
 size_t page_select_workspace_bytes(int64_t nseg, int64_t T);
 hipError_t launch_page_select(PageSelectParams p, hipStream_t stream);
 
+// ------------------------------------------------- filling a paged cache on the GPU
+// The plan (one workgroup) leaves in the workspace what the fill reads: the
+// stack height before the call, then per unit the first of its pages in the
+// order the call hands them out (-1: not served).
+struct PageExtendParams {
+  const int32_t* unit_new;   // [N] tokens to add
+  const int32_t* unit_len;   // [N] positions held
+  int32_t* new_len;          // [N] (may be unit_len)
+  const int32_t* free_pages; // [free_cap] stack
+  const int32_t* n_free;     // [1]
+  int32_t* n_free_out;       // [1] (may be n_free)
+  int32_t* table;            // [N * Hkv][pages_per_seg]
+  int32_t* tok_off;          // [N + 1]
+  int32_t* first_pos;        // [N]
+  int64_t* slots;            // [max_tokens][Hkv]
+  int32_t* entries;          // [N * Hkv][max_entries][4] or null
+  int32_t* n_entries;        // [N * Hkv] or null
+  int64_t* pages_needed;     // [1] or null
+  int32_t* top;              // [1] (workspace)
+  int32_t* base;             // [N] (workspace)
+  int32_t num_units, Hkv, page_shift, pages_per_seg, max_tokens, free_cap, max_entries;
+};
+size_t page_extend_workspace_bytes(int64_t num_units);
+hipError_t launch_page_extend(const PageExtendParams& p, hipStream_t stream);
+
+struct PageReleaseParams {
+  const int32_t* table;  // [words]
+  const uint8_t* keep;   // [words] or null (nothing is kept)
+  int32_t* table_out;    // [words] (may be table)
+  int32_t* free_pages;   // [free_cap] stack
+  const int32_t* n_free; // [1]
+  int32_t* n_free_out;   // [1] (may be n_free)
+  int32_t* top;          // [1] stack height before the call (workspace)
+  int32_t* counts;       // [chunks] pages released per chunk (workspace)
+  int32_t words, free_cap;
+};
+size_t page_release_workspace_bytes(int64_t words);
+hipError_t launch_page_release(const PageReleaseParams& p, hipStream_t stream);
+
+struct PagedAppendParams {
+  const void* k_new;     // token-major rows: [tokens][Hkv] rows of row_bytes, tokens token_bytes apart
+  const void* v_new;
+  const int64_t* slots;  // [tokens][Hkv]
+  void* k_pages;
+  void* v_pages;
+  int64_t pool_rows;     // num_pages * page_rows
+  int64_t token_bytes;
+  int32_t tokens, Hkv, row_bytes;
+};
+hipError_t launch_paged_append(const PagedAppendParams& p, hipStream_t stream);
+
 // -------------------------------------------------------- exact-budget export
 struct TopkParams {
   const float* probs;  // [n] retention probabilities

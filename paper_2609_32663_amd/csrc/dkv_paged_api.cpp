@@ -143,6 +143,126 @@ dkv_status dkv_page_select(int32_t num_segments, int32_t context_len, int32_t ap
   return hip_status(dkv::launch_page_select(p, (hipStream_t)stream));
 }
 
+size_t dkv_page_extend_workspace_bytes(int32_t num_units) {
+  return num_units < 0 ? 0 : dkv::page_extend_workspace_bytes(num_units);
+}
+
+dkv_status dkv_page_extend(int32_t num_units, int32_t num_kv_heads, int32_t page_rows, const int32_t* unit_new,
+                           const int32_t* unit_len, int32_t* new_len, const int32_t* free_pages, int32_t free_cap,
+                           const int32_t* n_free, int32_t* n_free_out, int32_t* page_table, int32_t pages_per_seg,
+                           int32_t* tok_off, int32_t* first_pos, int64_t* slots, int32_t max_tokens, int32_t* entries,
+                           int32_t* n_entries, int32_t max_entries, int64_t* pages_needed, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  if (num_units < 0 || num_kv_heads <= 0 || pages_per_seg < 0 || max_tokens < 0 || free_cap < 0 || max_entries < 0)
+    return DKV_ERR_INVALID_ARG;
+  if (!page_rows_ok(page_rows)) return DKV_ERR_UNSUPPORTED;
+  if ((int64_t)num_units * num_kv_heads > 65535) return DKV_ERR_UNSUPPORTED;
+  // one work-item per token and KV head
+  if ((int64_t)max_tokens * num_kv_heads > 0xFFFFFFFFLL - 255) return DKV_ERR_UNSUPPORTED;
+  if (n_free == nullptr || n_free_out == nullptr || tok_off == nullptr) return DKV_ERR_INVALID_ARG;
+  if (num_units > 0 && (unit_new == nullptr || unit_len == nullptr || new_len == nullptr || first_pos == nullptr))
+    return DKV_ERR_INVALID_ARG;
+  if (num_units > 0 && pages_per_seg > 0 && page_table == nullptr) return DKV_ERR_INVALID_ARG;
+  if (free_cap > 0 && free_pages == nullptr) return DKV_ERR_INVALID_ARG;
+  if (max_tokens > 0 && slots == nullptr) return DKV_ERR_INVALID_ARG;
+  if (max_entries > 0 && entries == nullptr) return DKV_ERR_INVALID_ARG;
+  if (!aligned16(entries) || (reinterpret_cast<uintptr_t>(slots) & 7u) != 0) return DKV_ERR_MISALIGNED;
+  if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 3u) != 0 ||
+      workspace_bytes < dkv_page_extend_workspace_bytes(num_units))
+    return DKV_ERR_WORKSPACE;
+  dkv::PageExtendParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.unit_new = unit_new;
+  p.unit_len = unit_len;
+  p.new_len = new_len;
+  p.free_pages = free_pages;
+  p.n_free = n_free;
+  p.n_free_out = n_free_out;
+  p.table = page_table;
+  p.tok_off = tok_off;
+  p.first_pos = first_pos;
+  p.slots = slots;
+  p.entries = entries;
+  p.n_entries = n_entries;
+  p.pages_needed = pages_needed;
+  p.top = static_cast<int32_t*>(workspace);
+  p.base = p.top + 1;
+  p.num_units = num_units;
+  p.Hkv = num_kv_heads;
+  p.page_shift = __builtin_ctz((unsigned)page_rows);
+  p.pages_per_seg = pages_per_seg;
+  p.max_tokens = max_tokens;
+  p.free_cap = free_cap;
+  p.max_entries = max_entries;
+  return hip_status(dkv::launch_page_extend(p, (hipStream_t)stream));
+}
+
+size_t dkv_page_release_workspace_bytes(int32_t num_segments, int32_t pages_per_seg) {
+  if (num_segments < 0 || pages_per_seg < 0) return 0;
+  return dkv::page_release_workspace_bytes((int64_t)num_segments * pages_per_seg);
+}
+
+dkv_status dkv_page_release(int32_t num_segments, int32_t pages_per_seg, const int32_t* page_table,
+                            const uint8_t* keep, int32_t* table_out, int32_t* free_pages, int32_t free_cap,
+                            const int32_t* n_free, int32_t* n_free_out, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  if (num_segments < 0 || pages_per_seg < 0 || free_cap < 0) return DKV_ERR_INVALID_ARG;
+  const int64_t words = (int64_t)num_segments * pages_per_seg;
+  if (words > INT32_MAX) return DKV_ERR_UNSUPPORTED;
+  if (n_free == nullptr || n_free_out == nullptr) return DKV_ERR_INVALID_ARG;
+  if (words > 0 && (page_table == nullptr || table_out == nullptr)) return DKV_ERR_INVALID_ARG;
+  if (free_cap > 0 && free_pages == nullptr) return DKV_ERR_INVALID_ARG;
+  if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 3u) != 0 ||
+      workspace_bytes < dkv_page_release_workspace_bytes(num_segments, pages_per_seg))
+    return DKV_ERR_WORKSPACE;
+  dkv::PageReleaseParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.table = page_table;
+  p.keep = keep;
+  p.table_out = table_out;
+  p.free_pages = free_pages;
+  p.n_free = n_free;
+  p.n_free_out = n_free_out;
+  p.top = static_cast<int32_t*>(workspace);
+  p.counts = p.top + 1;
+  p.words = (int32_t)words;
+  p.free_cap = free_cap;
+  return hip_status(dkv::launch_page_release(p, (hipStream_t)stream));
+}
+
+dkv_status dkv_paged_append(dkv_dtype dtype, int32_t num_tokens, int32_t num_kv_heads, int32_t head_dim,
+                            const void* k_new, const void* v_new, int64_t token_stride, const int64_t* slots,
+                            void* k_pages, void* v_pages, int64_t num_pages, int32_t page_rows, void* stream) {
+  if (dtype != DKV_BF16 && dtype != DKV_F32) return DKV_ERR_INVALID_ARG;
+  if (num_tokens < 0 || num_kv_heads <= 0 || num_pages < 0) return DKV_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return DKV_ERR_UNSUPPORTED;
+  if (!page_rows_ok(page_rows)) return DKV_ERR_UNSUPPORTED;
+  if (num_pages > INT32_MAX) return DKV_ERR_UNSUPPORTED;
+  const int32_t elem = dtype == DKV_BF16 ? 2 : 4;
+  if (token_stride < (int64_t)num_kv_heads * head_dim || token_stride > INT32_MAX) return DKV_ERR_INVALID_ARG;
+  // one work-item per 16 bytes of a token's K rows
+  if ((int64_t)num_tokens * num_kv_heads > (0xFFFFFFFFLL - 255) / (head_dim * elem / 16)) return DKV_ERR_UNSUPPORTED;
+  if (num_tokens == 0 || num_pages == 0) return DKV_OK;
+  if (k_new == nullptr || v_new == nullptr || slots == nullptr || k_pages == nullptr || v_pages == nullptr)
+    return DKV_ERR_INVALID_ARG;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages) ||
+      token_stride * elem % 16 != 0 || (reinterpret_cast<uintptr_t>(slots) & 7u) != 0)
+    return DKV_ERR_MISALIGNED;
+  dkv::PagedAppendParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.k_new = k_new;
+  p.v_new = v_new;
+  p.slots = slots;
+  p.k_pages = k_pages;
+  p.v_pages = v_pages;
+  p.pool_rows = num_pages * page_rows;
+  p.token_bytes = token_stride * elem;
+  p.tokens = num_tokens;
+  p.Hkv = num_kv_heads;
+  p.row_bytes = head_dim * elem;
+  return hip_status(dkv::launch_paged_append(p, (hipStream_t)stream));
+}
+
 dkv_status dkv_paged_decode_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
                                  int32_t head_dim, const void* q, const void* k_pages, const void* v_pages,
                                  int64_t num_pages, int32_t page_rows, const int32_t* entries,

@@ -1,0 +1,268 @@
+// Filling a paged cache on the GPU: page tables and slots from request lengths
+// (extend), rows of K and V into their slots (append), pages back to the stack
+// of free ones (release).
+//
+// Extend.  Unit n holds len positions and gets `new` more; its Hkv segments
+// need per = ceil((len + new) / R) - ceil(len / R) pages each.  With exclusive
+// sums over the units of new tokens (row of the unit's first token) and of
+// Hkv * per (its first page in the order of the call), everything else is
+// elementwise: page i of the call is stack[top - 1 - i], token at position pos
+// of segment s has page pos / R, which is one of the call's pages when it
+// starts at or past ceil(len / R) * R and stands in the table otherwise, and
+// slot page * R + pos % R.  So the plan is two scans over the units by one
+// workgroup, and the fill takes one (token, head) per thread: no thread reads
+// what another one writes.  The call has next to no arithmetic; single tokens
+// are bound by the two launches' dependent round trips, prompts by writing
+// the slots.
+//
+// Release.  The pages to go, in table order, are pushed on the stack: a count
+// per chunk of table words, then every chunk sums the counts before it and
+// places its own.
+
+#include "dkv_device.hpp"
+#include "dkv_launch.hpp"
+
+namespace dkv {
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kFillThreads = 256;
+
+// ------------------------------------------------------------------- extend
+
+struct ExtendUnit {
+  int32_t len, add;
+  int64_t rows;  // rows of the token-major arrays that the unit takes
+};
+
+__device__ __forceinline__ ExtendUnit extend_unit(const PageExtendParams& p, int n) {
+  ExtendUnit u;
+  u.len = p.unit_len[n];
+  u.add = p.unit_new[n];
+  u.rows = u.add > 0 ? u.add : 0;
+  return u;
+}
+
+__device__ __forceinline__ int64_t pages_of(int64_t rows, int shift) { return (rows + (1 << shift) - 1) >> shift; }
+
+// Pages that each segment of the unit needs, or -1 when the unit cannot be
+// served however many pages are free: an invalid length, a table that is too
+// short, rows past max_tokens.
+__device__ __forceinline__ int64_t extend_need(const PageExtendParams& p, const ExtendUnit& u, int64_t end) {
+  const int64_t grown = (int64_t)u.len + u.add;
+  if (u.len < 0 || u.add < 0 || grown > INT32_MAX || grown > ((int64_t)p.pages_per_seg << p.page_shift) ||
+      end > p.max_tokens)
+    return -1;
+  return pages_of(grown, p.page_shift) - pages_of(u.len, p.page_shift);
+}
+
+// Thread t plans units [t * per, t * per + per): sums of its units' rows and
+// pages, a scan of each over the workgroup, and its units again.
+__global__ __launch_bounds__(kPlanThreads) void page_extend_plan_kernel(PageExtendParams p) {
+  __shared__ int64_t red[kPlanThreads / kWave + 1];
+  const int tid = threadIdx.x;
+  const int N = p.num_units;
+  const int per = (N + kPlanThreads - 1) / kPlanThreads;
+  const int lo = min(N, tid * per), hi = min(N, lo + per);
+  const int32_t height = *p.n_free;
+  const int64_t top = height < 0 ? 0 : (height > p.free_cap ? p.free_cap : height);
+  int64_t rows = 0;
+  for (int n = lo; n < hi; ++n) rows += extend_unit(p, n).rows;
+  int64_t all_rows;
+  const int64_t row0 = block_exclusive_scan<kPlanThreads>(rows, red, &all_rows);
+  int64_t row = row0, pages = 0;
+  for (int n = lo; n < hi; ++n) {
+    const ExtendUnit u = extend_unit(p, n);
+    const int64_t need = extend_need(p, u, row += u.rows);
+    if (need > 0) pages += need * p.Hkv;
+  }
+  int64_t all_pages;
+  int64_t base = block_exclusive_scan<kPlanThreads>(pages, red, &all_pages);
+  int64_t given = 0;
+  row = row0;
+  for (int n = lo; n < hi; ++n) {
+    const ExtendUnit u = extend_unit(p, n);
+    const int64_t first = row;
+    row += u.rows;
+    const int64_t need = extend_need(p, u, row);
+    const int64_t all = need > 0 ? need * p.Hkv : 0;
+    const bool served = need == 0 || (need > 0 && base + all <= top);
+    p.tok_off[n] = (int32_t)(first < p.max_tokens ? first : p.max_tokens);
+    p.first_pos[n] = served ? u.len : -1;
+    p.base[n] = served ? (int32_t)(base < top ? base : top) : -1;
+    p.new_len[n] = served ? u.len + u.add : u.len;
+    if (served) given += all;
+    base += all;
+  }
+  int64_t all_given;
+  block_exclusive_scan<kPlanThreads>(given, red, &all_given);
+  if (tid == 0) {
+    p.tok_off[N] = (int32_t)(all_rows < p.max_tokens ? all_rows : p.max_tokens);
+    p.top[0] = (int32_t)top;
+    p.n_free_out[0] = (int32_t)(top - all_given);
+    if (p.pages_needed != nullptr) p.pages_needed[0] = all_pages;
+  }
+}
+
+// Number of offsets off[1 .. n] that are <= row, i.e. the unit of a row below
+// off[n] (units without rows are stepped over).
+__device__ __forceinline__ int unit_of(const int32_t* off, int n, int32_t row) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (off[mid + 1] <= row) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(kFillThreads) void page_extend_fill_kernel(PageExtendParams p) {
+  const int64_t i = (int64_t)blockIdx.x * kFillThreads + threadIdx.x;
+  if (i >= (int64_t)p.max_tokens * p.Hkv) return;
+  const int32_t row = (int32_t)(i / p.Hkv);
+  const int g = (int)(i - (int64_t)row * p.Hkv);
+  int64_t slot = -1;
+  if (row < p.tok_off[p.num_units]) {
+    const int n = unit_of(p.tok_off, p.num_units, row);
+    const int32_t len = p.first_pos[n];
+    if (len >= 0) {
+      const int sh = p.page_shift;
+      const int32_t first_row = p.tok_off[n];
+      const int32_t grown = len + (p.tok_off[n + 1] - first_row);
+      const int32_t pos = len + (row - first_row);
+      const int32_t lpage = pos >> sh, in_page = pos & ((1 << sh) - 1);
+      const int32_t old = (int32_t)pages_of(len, sh);
+      const int64_t s = (int64_t)n * p.Hkv + g;
+      int32_t page;
+      if (lpage >= old) {
+        const int32_t per = (int32_t)pages_of(grown, sh) - old;
+        page = p.free_pages[p.top[0] - 1 - (p.base[n] + g * per + (lpage - old))];
+        if (in_page == 0) p.table[s * p.pages_per_seg + lpage] = page;
+      } else {
+        page = p.table[s * p.pages_per_seg + lpage];
+      }
+      if (page >= 0) slot = ((int64_t)page << sh) + in_page;
+      if (in_page == 0 || row == first_row) {
+        if (p.entries != nullptr && lpage < p.max_entries) {
+          const int64_t end = (int64_t)grown - ((int64_t)lpage << sh);
+          int32_t* e = p.entries + 4 * (s * p.max_entries + lpage);
+          *reinterpret_cast<int4*>(e) = int4{page, lpage, 0, (int32_t)(end < (1 << sh) ? end : (1 << sh))};
+        }
+        if (p.n_entries != nullptr && row == first_row) p.n_entries[s] = (int32_t)pages_of(grown, sh);
+      }
+    }
+  }
+  p.slots[i] = slot;
+}
+
+// ------------------------------------------------------------------ release
+
+constexpr int kReleaseThreads = 256;
+constexpr int kReleaseWords = 1024;    // table words of a chunk at least
+constexpr int kReleaseChunks = 4096;   // chunks at most
+
+int64_t release_chunk(int64_t words) {
+  const int64_t c = (words + kReleaseChunks - 1) / kReleaseChunks;
+  return c <= kReleaseWords ? kReleaseWords : (c + kReleaseThreads - 1) / kReleaseThreads * kReleaseThreads;
+}
+
+__device__ __forceinline__ bool released(const PageReleaseParams& p, int64_t i) {
+  return p.table[i] >= 0 && (p.keep == nullptr || p.keep[i] == 0);
+}
+
+__global__ __launch_bounds__(kReleaseThreads) void page_release_count_kernel(PageReleaseParams p, int64_t chunk) {
+  __shared__ int64_t red[kReleaseThreads / kWave + 1];
+  const int64_t lo = blockIdx.x * chunk, hi = lo + chunk < p.words ? lo + chunk : p.words;
+  int64_t n = 0;
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kReleaseThreads) n += released(p, i) ? 1 : 0;
+  int64_t all;
+  block_exclusive_scan<kReleaseThreads>(n, red, &all);
+  if (threadIdx.x == 0) {
+    p.counts[blockIdx.x] = (int32_t)all;
+    if (blockIdx.x == 0) {
+      const int32_t height = *p.n_free;
+      p.top[0] = height < 0 ? 0 : (height > p.free_cap ? p.free_cap : height);
+    }
+  }
+}
+
+__global__ __launch_bounds__(kReleaseThreads) void page_release_push_kernel(PageReleaseParams p, int64_t chunk) {
+  __shared__ int64_t red[kReleaseThreads / kWave + 1];
+  const int tid = threadIdx.x;
+  int64_t before = 0, at;
+  for (int c = tid; c < (int)blockIdx.x; c += kReleaseThreads) before += p.counts[c];
+  block_exclusive_scan<kReleaseThreads>(before, red, &at);
+  at += p.top[0];
+  const int64_t lo = blockIdx.x * chunk, hi = lo + chunk < p.words ? lo + chunk : p.words;
+  for (int64_t i0 = lo; i0 < hi; i0 += kReleaseThreads) {
+    const int64_t i = i0 + tid;
+    const bool go = i < hi && released(p, i);
+    int64_t sum;
+    const int64_t to = at + block_exclusive_scan<kReleaseThreads>(go ? 1 : 0, red, &sum);
+    if (i < hi) {
+      const int32_t page = p.table[i];
+      const bool push = go && to < p.free_cap;  // a page that the stack has no room for stays
+      if (push) p.free_pages[to] = page;
+      p.table_out[i] = push ? -1 : page;
+    }
+    at += sum;
+  }
+  if (blockIdx.x == gridDim.x - 1 && tid == 0) p.n_free_out[0] = (int32_t)(at < p.free_cap ? at : p.free_cap);
+}
+
+// ------------------------------------------------------------------- append
+
+// One 16-byte granule of K and of V per thread: a row is row_bytes / 16
+// threads, rows of one token side by side.  Bound by moving the rows.
+__global__ __launch_bounds__(kFillThreads) void paged_append_kernel(PagedAppendParams p) {
+  const int per_row = p.row_bytes / 16;
+  const int64_t i = (int64_t)blockIdx.x * kFillThreads + threadIdx.x;
+  const int64_t r = i / per_row;  // token * Hkv + head
+  if (r >= (int64_t)p.tokens * p.Hkv) return;
+  const int64_t slot = p.slots[r];
+  if (slot < 0 || slot >= p.pool_rows) return;
+  const int c = (int)(i - r * per_row) * 16;
+  const int64_t tok = r / p.Hkv;
+  const int64_t from = tok * p.token_bytes + (r - tok * p.Hkv) * p.row_bytes + c;
+  const int64_t to = slot * p.row_bytes + c;
+  const u32x4 k = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.k_new) + from);
+  const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.v_new) + from);
+  *reinterpret_cast<u32x4*>(static_cast<char*>(p.k_pages) + to) = k;
+  *reinterpret_cast<u32x4*>(static_cast<char*>(p.v_pages) + to) = v;
+}
+
+}  // namespace
+
+size_t page_extend_workspace_bytes(int64_t num_units) { return (size_t)(num_units + 1) * sizeof(int32_t); }
+
+hipError_t launch_page_extend(const PageExtendParams& p, hipStream_t stream) {
+  hipLaunchKernelGGL(page_extend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p);
+  const int64_t n = (int64_t)p.max_tokens * p.Hkv;
+  if (n > 0)
+    hipLaunchKernelGGL(page_extend_fill_kernel, dim3((unsigned)((n + kFillThreads - 1) / kFillThreads)),
+                       dim3(kFillThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+size_t page_release_workspace_bytes(int64_t words) {
+  const int64_t chunks = (words + kReleaseWords - 1) / kReleaseWords;
+  return (size_t)(2 + (chunks < kReleaseChunks ? chunks : kReleaseChunks)) * sizeof(int32_t);
+}
+
+hipError_t launch_page_release(const PageReleaseParams& p, hipStream_t stream) {
+  const int64_t chunk = release_chunk(p.words);
+  const unsigned chunks = p.words > 0 ? (unsigned)((p.words + chunk - 1) / chunk) : 1u;
+  hipLaunchKernelGGL(page_release_count_kernel, dim3(chunks), dim3(kReleaseThreads), 0, stream, p, chunk);
+  hipLaunchKernelGGL(page_release_push_kernel, dim3(chunks), dim3(kReleaseThreads), 0, stream, p, chunk);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_append(const PagedAppendParams& p, hipStream_t stream) {
+  const int64_t n = (int64_t)p.tokens * p.Hkv * (p.row_bytes / 16);
+  hipLaunchKernelGGL(paged_append_kernel, dim3((unsigned)((n + kFillThreads - 1) / kFillThreads)), dim3(kFillThreads),
+                     0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace dkv
