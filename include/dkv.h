@@ -25,6 +25,8 @@
  *   dkv_page_extend   page tables, slots and entries of growing requests, built
  *                     from their lengths (dkv_page_release: pages back)
  *   dkv_paged_append  new tokens -> their slots in the pages
+ *   dkv_paged_query_attn  a chunk of new tokens of every sequence over a paged
+ *                     cache, causally
  *   dkv_topk_pattern  the exact-budget export of a pattern from retention
  *                     probabilities (K_rho largest entries)
  *
@@ -671,6 +673,60 @@ dkv_status dkv_paged_append(dkv_dtype dtype, int32_t num_tokens, int32_t num_kv_
                             int32_t head_dim, const void *k_new, const void *v_new,
                             int64_t token_stride, const int64_t *slots, void *k_pages,
                             void *v_pages, int64_t num_pages, int32_t page_rows, void *stream);
+
+/* Workspace bytes for dkv_paged_query_attn with the same shapes and rows_hint
+ * (host, no GPU call); 0 when the call needs none (workspace may be NULL). */
+size_t dkv_paged_query_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                       int32_t head_dim, int32_t num_tokens, int32_t max_q,
+                                       int64_t rows_hint);
+
+/*
+ * dkv_paged_query_attn -- attention of a chunk of new tokens of every sequence
+ * over a paged cache (dkv_query_attn's counterpart for pages; chunks of
+ * different lengths, single tokens included, in one call).
+ *
+ * q         [num_tokens][Hq][d] bf16, token-major, tokens q_stride elements
+ *           apart (>= Hq * d, a multiple of 8: the Q part of a fused
+ *           projection's rows can be passed where it is).
+ * tok_off   int32 [B + 1]: sequence b's chunk is rows [tok_off[b],
+ *           tok_off[b + 1]); taken within [0, num_tokens], and of a chunk
+ *           longer than max_q only the first max_q tokens are attended.
+ * first_pos int32 [B]: position of the chunk's first token; a negative one
+ *           marks a sequence that attends nothing (its outputs are zeros).
+ * entries, n_entries, max_entries  the pages of the B * Hkv segments, from
+ *           dkv_page_extend (an unpruned cache) or dkv_page_select (the
+ *           retained runs and the append region), in position order.
+ *           Token i of the chunk, head h (g = h / G) attends to the slots of
+ *           segment (b, g)'s entries whose position (logical page * page_rows
+ *           + slot) is at most first_pos[b] + i: what the sequence holds, and
+ *           the chunk causally up to itself.  The chunk's K/V must already be
+ *           written (dkv_paged_append).  An entry that names a page outside
+ *           [0, num_pages) or slots outside [0, page_rows) attends nothing;
+ *           slots past the chunk's last position are never read.
+ * out       [num_tokens][Hq][d] fp32, softmax(sm_scale * K q) V over those
+ *           slots; zeros for a token that sees none.  Rows of no sequence
+ *           (padding) are left as they were.
+ *           q, the attended K and V and sm_scale must be finite; slots that no
+ *           token of the chunk attends may hold anything.
+ * max_q     (host) tokens of the longest chunk.
+ * rows_hint (host) expected total rows of the call, sum over segments of
+ *           entries * page_rows (0 = unknown); it sizes the split of the keys
+ *           and must equal the value given to dkv_paged_query_workspace_bytes.
+ * workspace dkv_paged_query_workspace_bytes(...) bytes, no initial contents
+ *           required, or NULL when that is 0.
+ * Only DKV_BF16 is supported (DKV_ERR_UNSUPPORTED otherwise); head_dim 64 or
+ * 128; DKV_ERR_UNSUPPORTED also when max_entries * page_rows > 2^30 or a
+ * dispatch would exceed 2^32 work-items.
+ */
+dkv_status dkv_paged_query_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_heads,
+                                int32_t num_kv_heads, int32_t head_dim, int32_t num_tokens,
+                                int32_t max_q, const void *q, int64_t q_stride,
+                                const int32_t *tok_off, const int32_t *first_pos,
+                                const void *k_pages, const void *v_pages, int64_t num_pages,
+                                int32_t page_rows, const int32_t *entries,
+                                const int32_t *n_entries, int32_t max_entries, float sm_scale,
+                                int64_t rows_hint, float *out, void *workspace,
+                                size_t workspace_bytes, void *stream);
 
 /* Static description of a status code. */
 const char *dkv_status_string(dkv_status status);

@@ -26,7 +26,7 @@ __all__ = [
     "dkv_paged_decode_attn", "dkv_paged_append_decode_attn", "dkv_budget_entries",
     "dkv_topk_workspace_bytes", "dkv_topk_pattern", "dkv_map_pattern_ragged",
     "dkv_page_extend_workspace_bytes", "dkv_page_extend", "dkv_page_release_workspace_bytes", "dkv_page_release",
-    "dkv_paged_append",
+    "dkv_paged_append", "dkv_paged_query_workspace_bytes", "dkv_paged_query_attn",
 ]
 
 (DKV_OK, DKV_ERR_INVALID_ARG, DKV_ERR_UNSUPPORTED, DKV_ERR_MISALIGNED, DKV_ERR_CAPACITY,
@@ -129,6 +129,9 @@ def library_at(path):
                                   VP, VP, SZ, VP]),
         "dkv_page_release_workspace_bytes": (SZ, [I32, I32]),
         "dkv_page_release": (I32, [I32, I32, VP, VP, VP, VP, I32, VP, VP, VP, SZ, VP]),
+        "dkv_paged_query_workspace_bytes": (SZ, [I32, I32, I32, I32, I32, I32, I64]),
+        "dkv_paged_query_attn": (I32, [I32, I32, I32, I32, I32, I32, I32, VP, I64, VP, VP, VP, VP, I64, I32, VP, VP, I32,
+                                       F32, I64, VP, VP, SZ, VP]),
         "dkv_paged_append": (I32, [I32, I32, I32, I32, VP, VP, I64, VP, VP, VP, I64, I32, VP]),
         "dkv_compact_bins_workspace_bytes": (SZ, [P]),
         "dkv_compact_bins": (I32, [P, I32, VP, VP, VP, I32, VP, VP, I64, VP, VP, VP, VP, VP, SZ, VP]),
@@ -510,3 +513,29 @@ def dkv_paged_append(k_new, v_new, slots, k_pages, v_pages, stream=None):
         dtype_code(k_pages.dtype), tokens, Hkv, dim, k_ptr, v_ptr, stride, _typed(slots, "slots", torch.int64),
         _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", k_pages.dtype, (num_pages, page_rows, dim)), num_pages,
         page_rows, _stream(stream)))
+
+
+def dkv_paged_query_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q, rows_hint=0):
+    return library().dkv_paged_query_workspace_bytes(int(batch), int(num_q_heads), int(num_kv_heads), int(head_dim),
+                                                     int(num_tokens), int(max_q), int(rows_hint))
+
+
+def dkv_paged_query_attn(q, tok_off, first_pos, k_pages, v_pages, entries, n_entries, sm_scale, out, workspace,
+                         num_kv_heads, max_q, rows_hint=0, stream=None):
+    """q: [tokens][Hq][d] bf16, tokens evenly spaced (a view of a fused projection included); tok_off: int32 [B+1];
+    first_pos: int32 [B]; k_pages, v_pages: [num_pages][page_rows][d]; entries: int32 [B*Hkv][max_entries][4];
+    n_entries: int32 [B*Hkv]; out: fp32 [tokens][Hq][d]; max_q: the longest chunk; workspace: device tensor of
+    dkv_paged_query_workspace_bytes(...) bytes, or None when that is 0."""
+    tokens, Hq, dim = q.shape
+    B, Hkv, i32 = first_pos.shape[0], int(num_kv_heads), torch.int32
+    num_pages, page_rows, _ = k_pages.shape
+    q_ptr, stride = _rows(q, "q", Hq, dim, k_pages.dtype)
+    ws_ptr, ws_bytes = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.nbytes)
+    _check("dkv_paged_query_attn", library().dkv_paged_query_attn(
+        dtype_code(k_pages.dtype), B, Hq, Hkv, dim, tokens, int(max_q), q_ptr, stride,
+        _typed(tok_off, "tok_off", i32, (B + 1,)), _typed(first_pos, "first_pos", i32),
+        _typed(k_pages, "k_pages", k_pages.dtype, (num_pages, page_rows, dim)),
+        _typed(v_pages, "v_pages", k_pages.dtype, (num_pages, page_rows, dim)), num_pages, page_rows,
+        _typed(entries, "entries", i32, (B * Hkv, entries.shape[1], 4)), _typed(n_entries, "n_entries", i32, (B * Hkv,)),
+        entries.shape[1], float(sm_scale), int(rows_hint), _typed(out, "out", torch.float32, (tokens, Hq, dim)), ws_ptr,
+        ws_bytes, _stream(stream)))

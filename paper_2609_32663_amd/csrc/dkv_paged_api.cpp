@@ -8,6 +8,7 @@
 #include <cstring>
 
 #include "dkv_launch.hpp"
+#include "dkv_query.hpp"
 
 namespace {
 
@@ -82,6 +83,20 @@ dkv_status paged_decode(dkv_dtype dtype, int32_t batch, int32_t hq, int32_t hkv,
   // pointer; with max_entries = 0 no entry is ever read
   if (p.entries == nullptr) p.entries = n_entries;
   return hip_status(dkv::launch_decode(p, dtype, d, rows_hint, (hipStream_t)stream));
+}
+
+// Shape checks shared by paged query-block attention and its workspace query.
+dkv_status check_paged_query(int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_t num_tokens, int32_t max_q) {
+  if (batch < 0 || hq <= 0 || hkv <= 0 || hq % hkv != 0 || num_tokens < 0 || max_q < 0) return DKV_ERR_INVALID_ARG;
+  if (hq / hkv > DKV_MAX_GROUP || (d != 64 && d != 128)) return DKV_ERR_UNSUPPORTED;
+  if ((int64_t)batch * hkv > DKV_MAX_SEGMENTS) return DKV_ERR_UNSUPPORTED;
+  // query rows per segment must fit 31 bits, workgroups of 512 threads 32 bits of work-items
+  const int64_t longest = max_q < num_tokens ? max_q : num_tokens;
+  const int64_t rows = longest * (hq / hkv);
+  if (rows > INT32_MAX / 2) return DKV_ERR_UNSUPPORTED;
+  if ((rows + dkv::kQueryRowsPerWG - 1) / dkv::kQueryRowsPerWG * batch * hkv > 0xFFFFFFFFLL / 512)
+    return DKV_ERR_UNSUPPORTED;
+  return DKV_OK;
 }
 
 }  // namespace
@@ -261,6 +276,65 @@ dkv_status dkv_paged_append(dkv_dtype dtype, int32_t num_tokens, int32_t num_kv_
   p.Hkv = num_kv_heads;
   p.row_bytes = head_dim * elem;
   return hip_status(dkv::launch_paged_append(p, (hipStream_t)stream));
+}
+
+size_t dkv_paged_query_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                       int32_t num_tokens, int32_t max_q, int64_t rows_hint) {
+  (void)rows_hint;
+  if (check_paged_query(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q) != DKV_OK) return 0;
+  return 0;
+}
+
+dkv_status dkv_paged_query_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                int32_t head_dim, int32_t num_tokens, int32_t max_q, const void* q, int64_t q_stride,
+                                const int32_t* tok_off, const int32_t* first_pos, const void* k_pages,
+                                const void* v_pages, int64_t num_pages, int32_t page_rows, const int32_t* entries,
+                                const int32_t* n_entries, int32_t max_entries, float sm_scale, int64_t rows_hint,
+                                float* out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (dtype != DKV_BF16 && dtype != DKV_F32) return DKV_ERR_INVALID_ARG;
+  const dkv_status st = check_paged_query(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q);
+  if (st != DKV_OK) return st;
+  if (dtype != DKV_BF16) return DKV_ERR_UNSUPPORTED;
+  if (!dkv::scale_in_range(sm_scale) || num_pages < 0 || max_entries < 0) return DKV_ERR_INVALID_ARG;
+  if (!page_rows_ok(page_rows)) return DKV_ERR_UNSUPPORTED;
+  // the row space of a segment is walked with 32-bit rows
+  if (num_pages > INT32_MAX || (int64_t)max_entries * page_rows > (int64_t)1 << 30) return DKV_ERR_UNSUPPORTED;
+  if (q_stride < (int64_t)num_q_heads * head_dim || q_stride > INT32_MAX) return DKV_ERR_INVALID_ARG;
+  if (batch == 0 || num_tokens == 0 || max_q == 0) return DKV_OK;
+  if (q == nullptr || tok_off == nullptr || first_pos == nullptr || n_entries == nullptr || out == nullptr ||
+      (num_pages > 0 && (k_pages == nullptr || v_pages == nullptr)) || (max_entries > 0 && entries == nullptr))
+    return DKV_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(entries) ||
+      q_stride % 8 != 0)
+    return DKV_ERR_MISALIGNED;
+  const size_t need = dkv_paged_query_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q,
+                                                      rows_hint);
+  if (need > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need)) return DKV_ERR_WORKSPACE;
+
+  dkv::QueryParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.q = q;
+  p.k = k_pages;
+  p.v = v_pages;
+  p.nseg = batch * num_kv_heads;
+  p.Hkv = num_kv_heads;
+  p.Hq = num_q_heads;
+  p.G = num_q_heads / num_kv_heads;
+  p.max_q = max_q < num_tokens ? max_q : num_tokens;
+  p.rows = p.max_q * p.G;
+  p.qtiles = (p.rows + dkv::kQueryRowsPerWG - 1) / dkv::kQueryRowsPerWG;
+  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  p.out = out;
+  p.tok_off = tok_off;
+  p.first_pos = first_pos;
+  p.entries = entries;
+  p.n_entries = n_entries;
+  p.num_pages = num_pages;
+  p.q_stride = q_stride * 2;
+  p.max_entries = max_entries;
+  p.page_shift = __builtin_ctz((unsigned)page_rows);
+  p.num_tokens = num_tokens;
+  return hip_status(dkv::launch_paged_query_attn(p, head_dim, (hipStream_t)stream));
 }
 
 dkv_status dkv_paged_decode_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,

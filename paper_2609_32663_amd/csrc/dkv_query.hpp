@@ -41,6 +41,19 @@ struct QueryParams {
   int32_t P, rec_rows;
   int32_t stream_once;     // load K and V past the caches
   int32_t* seg_meta;
+  // Paged calls only.  q is [num_tokens][Hq][d] with tokens q_stride bytes
+  // apart, out [num_tokens][Hq][d]; sequence b's block is tokens [tok_off[b],
+  // tok_off[b + 1]), its first one at position first_pos[b].  k and v are page
+  // pools; a segment's row space is the page_rows slots of each of its
+  // entries, in entry order (rows of entry e: [e << page_shift, ...)), and a
+  // slot counts when it lies in the entry's [lo, hi) and at or below the query
+  // token's position.
+  const int32_t* tok_off;    // [B + 1]
+  const int32_t* first_pos;  // [B]
+  const int32_t* entries;    // [nseg][max_entries][4]: page, logical page, lo, hi
+  const int32_t* n_entries;  // [nseg]
+  int64_t num_pages, q_stride;
+  int32_t max_entries, page_shift, num_tokens, max_q;
 };
 
 // How a call is split, from the shapes and the caller's hint of the total
@@ -97,5 +110,6 @@ inline bool query_takes_short(int32_t nseg, int32_t rows, int32_t head_dim, int6
 constexpr int64_t kShortCachedBytes = 96 << 20;
 hipError_t launch_query_short(const QueryParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, hipStream_t stream);
+hipError_t launch_paged_query_attn(const QueryParams& p, int head_dim, hipStream_t stream);
 
 }  // namespace dkv

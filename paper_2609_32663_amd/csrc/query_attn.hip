@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kPlanThreads) void query_plan_kernel(QueryParams p)
   }
 }
 
-template <int D>
+template <int D, bool PAGED>
 __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
   using C = QCfg<D>;
   // two tile buffers per matrix (separate arrays: the compiler then tells the
@@ -141,7 +141,22 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
   int item, s, qt;
   bool single;             // the segment has one range: write the output
   int64_t t_lo, t_hi;      // key tiles [t_lo, t_hi) of the range
-  if (p.plan == nullptr) {
+  int rows;                // query rows of the segment
+  PagedBlock blk{0, 0, 0};
+  int32_t nent = 0;        // entries that the workgroup's rows see
+  if constexpr (PAGED) {
+    item = blockIdx.x;
+    s = item / p.qtiles;
+    qt = item - s * p.qtiles;
+    single = true;
+    blk = paged_block(p, s / p.Hkv);
+    rows = blk.n * p.G;
+    if (qt * kQRows >= rows) return;
+    if (blk.pos0 >= 0) nent = paged_entries(p, s, paged_pos(blk, (min(rows, (qt + 1) * kQRows) - 1) / p.G));
+    nent = __builtin_amdgcn_readfirstlane(nent);
+    t_lo = 0;
+    t_hi = (((int64_t)nent << p.page_shift) + kQKeys - 1) / kQKeys;
+  } else if (p.plan == nullptr) {
     item = blockIdx.x;
     s = item / p.qtiles;
     qt = item - s * p.qtiles;
@@ -176,19 +191,25 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
   }
   const int bseq = s / p.Hkv;
   const int g = s - bseq * p.Hkv;
-  if (p.seg_len[s] < 0) {
-    // a segment dkv_compact could not pack (one range, so this workgroup
-    // owns its query tile's output): no rows to attend, zeros
-    for (int i = tid; i < kQRows * D; i += kQThreads) {
-      const int rq = qt * kQRows + i / D;
-      if (rq >= p.rows) break;
-      const int tq = rq / p.G;
-      p.out[(((int64_t)bseq * p.n_q + tq) * p.Hq + (int64_t)g * p.G + (rq - tq * p.G)) * D + i % D] = 0.f;
+  int64_t base_len = 0, row0 = 0;
+  if constexpr (!PAGED) {
+    rows = p.rows;
+    if (p.seg_len[s] < 0) {
+      // a segment dkv_compact could not pack (one range, so this workgroup
+      // owns its query tile's output): no rows to attend, zeros
+      for (int i = tid; i < kQRows * D; i += kQThreads) {
+        const int rq = qt * kQRows + i / D;
+        if (rq >= p.rows) break;
+        const int tq = rq / p.G;
+        p.out[(((int64_t)bseq * p.n_q + tq) * p.Hq + (int64_t)g * p.G + (rq - tq * p.G)) * D + i % D] = 0.f;
+      }
+      return;
     }
-    return;
+    base_len = q_uniform64((int64_t)p.seg_len[s] + p.n_tail);  // rows every query row sees
+    row0 = q_uniform64(p.seg_off[s]);
   }
-  const int64_t base_len = q_uniform64((int64_t)p.seg_len[s] + p.n_tail);  // rows every query row sees
-  const int64_t row0 = q_uniform64(p.seg_off[s]);
+  // where the block starts in the token-major arrays
+  const int64_t tok_row0 = PAGED ? (int64_t)blk.tok0 : (int64_t)bseq * p.n_q;
 
   // this lane's query rows (one per row group) in the score layout, and the keys they see
   int r[kRG], tok[kRG];
@@ -197,20 +218,23 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
 #pragma unroll
   for (int q = 0; q < kRG; ++q) {
     r[q] = qt * kQRows + wave * 16 * kRG + 16 * q + n16;
-    row_ok[q] = r[q] < p.rows;
+    row_ok[q] = r[q] < rows;
     tok[q] = row_ok[q] ? r[q] / p.G : 0;
     limit[q] = base_len + tok[q] + 1;
   }
   // this workgroup's keys: the range, up to what its last row sees
   // (all workgroup-uniform; readfirstlane keeps them in scalar registers)
-  const int r_last = min(p.rows - 1, qt * kQRows + kQRows - 1);
-  const int64_t lim_max = base_len + r_last / p.G + 1;
+  const int r_last = min(rows - 1, qt * kQRows + kQRows - 1);
+  const int64_t lim_max = PAGED ? (int64_t)nent << p.page_shift : base_len + r_last / p.G + 1;
   const int64_t k_lo = q_uniform64(t_lo * kQKeys);
   const int64_t k_end = t_hi * kQKeys < lim_max ? t_hi * kQKeys : lim_max;
   const int64_t k_hi = q_uniform64(k_end > k_lo ? k_end : k_lo);
-  int32_t cut[kRG];  // keys [k_lo, k_lo + cut) count for the row (cut <= the range length)
+  // packed: keys [k_lo, k_lo + cut) count for the row (cut <= the range length);
+  // paged: keys at positions below cut
+  int32_t cut[kRG];
 #pragma unroll
-  for (int q = 0; q < kRG; ++q) cut[q] = (int32_t)((limit[q] < k_hi ? limit[q] : k_hi) - k_lo);
+  for (int q = 0; q < kRG; ++q)
+    cut[q] = PAGED ? paged_pos(blk, tok[q]) + 1 : (int32_t)((limit[q] < k_hi ? limit[q] : k_hi) - k_lo);
   // every row of the workgroup sees all keys below this one
   const int64_t all_see = q_uniform64(base_len + 1 < k_hi ? base_len + 1 : k_hi);
 
@@ -224,9 +248,11 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
 #pragma unroll
   for (int q = 0; q < kRG; ++q) {
     const int hh = r[q] - tok[q] * p.G;
-    const char* qrow = reinterpret_cast<const char*>(p.q) +
-                       (((int64_t)bseq * p.n_q + tok[q]) * p.Hq + (int64_t)g * p.G + (row_ok[q] ? hh : 0)) *
-                           C::kRowBytes;
+    const char* qrow = reinterpret_cast<const char*>(p.q);
+    if constexpr (PAGED)
+      qrow += (tok_row0 + tok[q]) * p.q_stride + ((int64_t)g * p.G + (row_ok[q] ? hh : 0)) * C::kRowBytes;
+    else
+      qrow += ((tok_row0 + tok[q]) * p.Hq + (int64_t)g * p.G + (row_ok[q] ? hh : 0)) * C::kRowBytes;
 #pragma unroll
     for (int u = 0; u < C::kChunks; ++u) {
       const u32x4 z = {0u, 0u, 0u, 0u};
@@ -278,6 +304,39 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
   // tests/test_gpu_query_room.py holds with NaN behind every segment; the
   // displacement in the vector offset cost 4 registers and 1% of a 256-token
   // call at 128K.)
+  // Paged: the two 32-row runs of a tile lie in pages of their own, each with
+  // a descriptor over its slots [lo, hi): slots outside them (and runs past
+  // the range) read zeros.  A wave instruction stays within one run.  `run`
+  // holds the runs of tiles t (parity t % 2) for the masks; K of a tile is
+  // issued before V of it and before anything of the next, so `at` names the
+  // pool rows of the tile issued last.
+  PagedRun run[2][2] = {};
+  PagedEntries held{0, 0, 0, 0};
+  const int32_t pos_stop = PAGED && blk.pos0 >= 0 ? paged_pos(blk, blk.n - 1) + 1 : 0;
+  if constexpr (PAGED) {
+    held.load(p, s, nent, (int32_t)(k_lo >> p.page_shift));
+    if (D == 64) {  // one instruction per wave: waves 4-7 fill the second run
+      koff -= (uint32_t)((wave_u >> 2) * kRun * C::kRowBytes);
+      voff -= (uint32_t)((wave_u >> 2) * kRun * C::kRowBytes);
+    }
+  }
+  auto find_runs = [&](PagedRun (&u)[2], int64_t kt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) u[h] = paged_run(p, held, s, nent, (int32_t)kt + kRun * h, (int32_t)k_hi, pos_stop);
+  };
+  auto issue_runs = [&](const void* pool, uint32_t off, const PagedRun (&u)[2], uint16_t* buf)
+                        __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < C::kDma; ++i) {
+      const int mi = i * (kQThreads / kWave) + wave_u;
+      const bool second = D == 64 ? wave_u >= 4 : i == 1;
+      const PagedRun& x = second ? u[1] : u[0];
+      const __amdgpu_buffer_rsrc_t rs = q_rsrc(static_cast<const char*>(pool) + (x.row + x.lo) * C::kRowBytes,
+                                               (uint32_t)(x.hi - x.lo) * C::kRowBytes);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(buf + 512 * mi), 16,
+                                               off - (uint32_t)(x.lo * C::kRowBytes), 0, 0, 0);
+    }
+  };
   auto issue = [&](const char* base, uint32_t off, int64_t kt, uint16_t* buf) __attribute__((always_inline)) {
     const int64_t left = k_hi - kt;
     const uint32_t nk = (uint32_t)(left <= 0 ? 0 : (left < kQKeys ? left : kQKeys));
@@ -331,12 +390,30 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
   // spread by 1 to 2 us on either side; taking the bf16 remainders by dot products
   // as well, 16 instructions fewer per half, gave nothing: the kernel runs at the
   // power limit).
-  auto softmax = [&](auto masked, float (&sc)[kRG][2][4], int64_t kh) __attribute__((always_inline)) {
+  const int32_t pos_all = PAGED ? paged_pos(blk, min(qt * kQRows + 16 * kRG * wave_u, rows - 1) / p.G) + 1 : 0;
+  auto softmax = [&](auto masked, float (&sc)[kRG][2][4], int64_t kh, const PagedRun& u) __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+      // slots outside the entry, or past the position of one of the wave's rows
+      if (u.lo > 0 || u.hi < kRun || u.pos + kRun > pos_all) {
+        asm volatile("");  // keeps this a branch: the selects would run for every half
+#pragma unroll
+        for (int q = 0; q < kRG; ++q) {
+          const int32_t lim = cut[q] - u.pos < u.hi ? cut[q] - u.pos : u.hi;
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int key = 16 * jj + 4 * kg + v;
+              if (key >= lim || key < u.lo) sc[q][jj][v] = -INFINITY;
+            }
+        }
+      }
+    }
 #pragma unroll
     for (int q = 0; q < kRG; ++q) {
       // keys past a row's causal limit or past the range: only in the
       // halves that reach min over rows of that limit
-      if (decltype(masked)::value && kh + 32 > all_see) {
+      if (!PAGED && decltype(masked)::value && kh + 32 > all_see) {
         const int32_t lim = cut[q] - (int32_t)(kh - k_lo);  // keys [0, lim) of this half count
 #pragma unroll
         for (int jj = 0; jj < 2; ++jj)
@@ -460,16 +537,24 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
   uint16_t* const kbuf[2] = {k0, k1};
   uint16_t* const vbuf[2] = {v0, v1};
   const bool lead = __builtin_amdgcn_readfirstlane(wave < 4 ? 1 : 0) != 0;
-  issue(kbase, koff, k_lo, kbuf[0]);
-  issue(vbase, voff, k_lo, vbuf[0]);
-  issue(kbase, koff, k_lo + kQKeys, kbuf[1]);
+  if constexpr (PAGED) {
+    find_runs(run[0], k_lo);
+    issue_runs(p.k, koff, run[0], kbuf[0]);
+    issue_runs(p.v, voff, run[0], vbuf[0]);
+    find_runs(run[1], k_lo + kQKeys);
+    issue_runs(p.k, koff, run[1], kbuf[1]);
+  } else {
+    issue(kbase, koff, k_lo, kbuf[0]);
+    issue(vbase, voff, k_lo, vbuf[0]);
+    issue(kbase, koff, k_lo + kQKeys, kbuf[1]);
+  }
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
   __syncthreads();
   float sc[kRG][2][4];
   u32x4 ph[kRG], pl[kRG];
   constexpr int kWaitOne = 0x0F70 | C::kDma;  // vmcnt(kDma): the younger of two tiles may still be in flight
-  auto vphase = [&](auto masked, int64_t kh) __attribute__((always_inline)) {
-    softmax(masked, sc, kh);
+  auto vphase = [&](auto masked, int64_t kh, const PagedRun& u) __attribute__((always_inline)) {
+    softmax(masked, sc, kh, u);
     split(sc, ph, pl);
   };
   // P V first: the probabilities are dead before the new scores are formed
@@ -485,7 +570,7 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
   // pairs of tiles whose halves (up to 32 keys past the pair) all lie below
   // every row's limit need no masking
   const int64_t clear = all_see - k_lo - 5 * 32;
-  int64_t nclear = clear >= 0 ? clear / (2 * kQKeys) + 1 : 0;
+  int64_t nclear = !PAGED && clear >= 0 ? clear / (2 * kQKeys) + 1 : 0;
   nclear = q_uniform64(nclear < nround ? nclear : nround);
   int64_t kt = k_lo;
   // Tile t (K in kbuf[i], V in vbuf[i]) takes phases 4t + 1 .. 4t + 4.  K of
@@ -500,29 +585,36 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       // 4t + 1: lead: vector phase of half 2t; follow: P V of half 2t - 1, scores of 2t
-      if (L) vphase(masked, kt);
+      if (L) vphase(masked, kt, run[i][0]);
       else mphase(kbuf[i], 0, vbuf[1 - i], 1, i == 1 || kt != k_lo);
       __builtin_amdgcn_s_waitcnt(kWaitOne);  // V of tile t
       meet();
       // 4t + 2: lead: P V of 2t, scores of 2t + 1; follow: vector phase of 2t
-      issue(vbase, voff, kt + kQKeys, vbuf[1 - i]);
+      if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
+      else issue(vbase, voff, kt + kQKeys, vbuf[1 - i]);
       if (L) mphase(kbuf[i], 1, vbuf[i], 0, true);
-      else vphase(masked, kt);
+      else vphase(masked, kt, run[i][0]);
       meet();
       // 4t + 3: lead: vector phase of 2t + 1; follow: P V of 2t, scores of 2t + 1
-      if (L) vphase(masked, kt + 32);
+      const PagedRun second = run[i][1];
+      if (L) vphase(masked, kt + 32, second);
       else mphase(kbuf[i], 1, vbuf[i], 0, true);
       __builtin_amdgcn_s_waitcnt(kWaitOne);  // K of tile t + 1
       meet();
       // 4t + 4: lead: P V of 2t + 1, scores of 2t + 2; follow: vector phase of 2t + 1
-      issue(kbase, koff, kt + 2 * kQKeys, kbuf[i]);
+      if constexpr (PAGED) {
+        find_runs(run[i], kt + 2 * kQKeys);
+        issue_runs(p.k, koff, run[i], kbuf[i]);
+      } else {
+        issue(kbase, koff, kt + 2 * kQKeys, kbuf[i]);
+      }
       if (L) mphase(kbuf[1 - i], 0, vbuf[i], 1, true);
-      else vphase(masked, kt + 32);
+      else vphase(masked, kt + 32, second);
       meet();
       kt += kQKeys;
     }
   };
-  auto run = [&](auto leadc) __attribute__((always_inline)) {
+  auto walk = [&](auto leadc) __attribute__((always_inline)) {
     constexpr bool L = decltype(leadc)::value;
     if (L) mphase(kbuf[0], 0, vbuf[0], 0, false);  // scores of half 0
     meet();
@@ -532,8 +624,8 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
     // zeros and all their keys are masked, so the lead's last scores are unused)
     if (!L && nround > 0) pv(vbuf[1], 1, ph, pl);
   };
-  if (lead) run(std::true_type{});
-  else run(std::false_type{});
+  if (lead) walk(std::true_type{});
+  else walk(std::false_type{});
   // no direct load may still be writing LDS when the workgroup ends
   __builtin_amdgcn_s_waitcnt(0x0F70);
 
@@ -548,10 +640,10 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
       const int rq = qt * kQRows + rr;
       const float lq = __shfl(l[q], 4 * kg + v, 64);
       const float mq = __shfl(m[q], 4 * kg + v, 64);
-      if (rq < p.rows) {
+      if (rq < rows) {
         if (single) {
           const int tq = rq / p.G;
-          float* orow = p.out + (((int64_t)bseq * p.n_q + tq) * p.Hq + (int64_t)g * p.G + (rq - tq * p.G)) * D;
+          float* orow = p.out + ((tok_row0 + tq) * p.Hq + (int64_t)g * p.G + (rq - tq * p.G)) * D;
           const float inv = lq > 0.f ? 1.f / lq : 0.f;
 #pragma unroll
           for (int b = 0; b < C::kBlocks; ++b) orow[16 * b + n16] = o[q][b][v] * inv;
@@ -641,7 +733,7 @@ __global__ __launch_bounds__(kMergeThreads) void query_merge_kernel(QueryParams 
 template <int D>
 hipError_t launch_d(const QueryParams& p, int64_t grid, hipStream_t stream) {
   if (p.plan != nullptr) hipLaunchKernelGGL(query_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p);
-  hipLaunchKernelGGL((query_attn_kernel<D>), dim3((unsigned)grid), dim3(kQThreads), 0, stream, p);
+  hipLaunchKernelGGL((query_attn_kernel<D, false>), dim3((unsigned)grid), dim3(kQThreads), 0, stream, p);
   if (p.plan != nullptr) {
     const int64_t parts = (int64_t)kQRows * (D / 4) / kMergeThreads;
     hipLaunchKernelGGL((query_merge_kernel<D>), dim3((unsigned)((int64_t)p.nseg * p.qtiles * parts)),
@@ -681,6 +773,13 @@ QueryPlanShape query_plan_shape(int32_t nseg, int32_t rows, int32_t head_dim, in
 
 hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, hipStream_t stream) {
   return head_dim == 64 ? launch_d<64>(p, grid, stream) : launch_d<128>(p, grid, stream);
+}
+
+hipError_t launch_paged_query_attn(const QueryParams& p, int head_dim, hipStream_t stream) {
+  const dim3 grid((unsigned)((int64_t)p.nseg * p.qtiles)), block(kQThreads);
+  if (head_dim == 64) hipLaunchKernelGGL((query_attn_kernel<64, true>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((query_attn_kernel<128, true>), grid, block, 0, stream, p);
+  return hipGetLastError();
 }
 
 }  // namespace dkv

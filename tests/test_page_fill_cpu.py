@@ -137,3 +137,30 @@ def test_binding_refuses_what_the_kernels_would_misread():
     x = torch.zeros(4, 6, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         d.dkv_paged_append(x[:, :2], x[:, 2:4], torch.zeros(4, 2, dtype=torch.int64), torch.zeros(3, 32, 64), x)
+
+
+def test_paged_query_validation():
+    lib = d.library()
+    ws = d.dkv_paged_query_workspace_bytes(1, 32, 8, 128, 40, 40, 0)
+
+    def call(dtype=d.DKV_BF16, B=1, Hq=32, Hkv=8, dim=128, n=40, most=40, q=A, stride=4096, off=A, pos=A, k=A, v=A, pages=9,
+             R=128, ent=A, ne=A, max_e=5, scale=1.0, hint=0, out=A, w=A, w_bytes=max(ws, 1 << 40)):
+        return lib.dkv_paged_query_attn(dtype, B, Hq, Hkv, dim, n, most, q, stride, off, pos, k, v, pages, R, ent, ne,
+                                        max_e, scale, hint, out, w, w_bytes, NUL)
+
+    for bad in (dict(dtype=7), dict(B=-1), dict(Hq=0), dict(Hkv=0), dict(Hq=33), dict(n=-1), dict(most=-1), dict(pages=-1),
+                dict(max_e=-1), dict(scale=float("nan")), dict(scale=3e38), dict(stride=4095), dict(stride=1 << 31),
+                dict(q=NUL), dict(off=NUL), dict(pos=NUL), dict(k=NUL), dict(v=NUL), dict(ent=NUL), dict(ne=NUL),
+                dict(out=NUL)):
+        assert call(**bad) == d.DKV_ERR_INVALID_ARG, bad
+    for bad in (dict(dtype=d.DKV_F32), dict(dim=96), dict(Hq=136), dict(B=257), dict(R=96), dict(pages=1 << 31),
+                dict(max_e=(1 << 23) + 1), dict(n=1 << 30, most=1 << 30), dict(n=1 << 28, most=1 << 28)):
+        assert call(**bad) == d.DKV_ERR_UNSUPPORTED, bad
+    for bad in (dict(q=MIS), dict(k=MIS), dict(v=MIS), dict(out=MIS), dict(ent=MIS), dict(stride=4100)):
+        assert call(**bad) == d.DKV_ERR_MISALIGNED, bad
+    for nothing in (dict(B=0), dict(n=0), dict(most=0)):
+        assert call(q=NUL, off=NUL, pos=NUL, k=NUL, v=NUL, ent=NUL, ne=NUL, out=NUL, w=NUL, w_bytes=0, **nothing) == d.DKV_OK
+    assert d.dkv_paged_query_workspace_bytes(1, 32, 8, 96, 40, 40, 0) == 0
+    if ws:
+        for bad in (dict(w=NUL), dict(w=MIS), dict(w_bytes=ws - 1)):
+            assert call(**bad) == d.DKV_ERR_WORKSPACE, bad
