@@ -280,9 +280,12 @@ dkv_status dkv_paged_append(dkv_dtype dtype, int32_t num_tokens, int32_t num_kv_
 
 size_t dkv_paged_query_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                        int32_t num_tokens, int32_t max_q, int64_t rows_hint) {
-  (void)rows_hint;
   if (check_paged_query(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q) != DKV_OK) return 0;
-  return 0;
+  if (batch == 0 || num_tokens == 0 || max_q == 0) return 0;
+  const dkv::PagedPlanShape sh =
+      dkv::paged_plan_shape(batch, num_kv_heads, num_q_heads / num_kv_heads, head_dim, num_tokens,
+                            max_q < num_tokens ? max_q : num_tokens, rows_hint);
+  return sh.plan_bytes + sh.rec_bytes;
 }
 
 dkv_status dkv_paged_query_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
@@ -307,8 +310,10 @@ dkv_status dkv_paged_query_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_he
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(entries) ||
       q_stride % 8 != 0)
     return DKV_ERR_MISALIGNED;
-  const size_t need = dkv_paged_query_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q,
-                                                      rows_hint);
+  const dkv::PagedPlanShape sh =
+      dkv::paged_plan_shape(batch, num_kv_heads, num_q_heads / num_kv_heads, head_dim, num_tokens,
+                            max_q < num_tokens ? max_q : num_tokens, rows_hint);
+  const size_t need = sh.plan_bytes + sh.rec_bytes;
   if (need > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need)) return DKV_ERR_WORKSPACE;
 
   dkv::QueryParams p;
@@ -334,6 +339,12 @@ dkv_status dkv_paged_query_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_he
   p.max_entries = max_entries;
   p.page_shift = __builtin_ctz((unsigned)page_rows);
   p.num_tokens = num_tokens;
+  if (sh.slices > 0) {
+    p.P = sh.slices;
+    p.max_items = (int32_t)sh.units;
+    p.plan = static_cast<int32_t*>(workspace);
+    p.rec = reinterpret_cast<float*>(static_cast<char*>(workspace) + sh.plan_bytes);
+  }
   return hip_status(dkv::launch_paged_query_attn(p, head_dim, (hipStream_t)stream));
 }
 

@@ -110,6 +110,17 @@ inline bool query_takes_short(int32_t nseg, int32_t rows, int32_t head_dim, int6
 constexpr int64_t kShortCachedBytes = 96 << 20;
 hipError_t launch_query_short(const QueryParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, hipStream_t stream);
+
+// How a paged call is split: the most units ((segment, query tile) pairs) it
+// can have, and the slices its keys are cut into (0: no split).
+constexpr int kPagedSlices = 256;  // one workgroup per compute unit
+struct PagedPlanShape {
+  int64_t units;
+  int32_t slices;
+  size_t plan_bytes, rec_bytes;
+};
+PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t head_dim, int32_t num_tokens,
+                                int32_t max_q, int64_t rows_hint);
 hipError_t launch_paged_query_attn(const QueryParams& p, int head_dim, hipStream_t stream);
 
 }  // namespace dkv

@@ -56,6 +56,7 @@
 #include <type_traits>
 
 #include "dkv_device.hpp"
+#include "../../include/dkv.h"
 #include "dkv_query_device.hpp"
 
 namespace dkv {
@@ -123,8 +124,19 @@ __global__ __launch_bounds__(kPlanThreads) void query_plan_kernel(QueryParams p)
   }
 }
 
+// One item of a workgroup: query tile qt of segment s over key tiles [t_lo,
+// t_hi), which writes the output (`single`) or a record.
+struct QueryItem {
+  int s, qt;
+  int64_t t_lo, t_hi;
+  bool single;
+  float* rec;
+  PagedBlock blk;  // paged: the sequence's block, and the entries that the tile's rows see
+  int32_t nent;
+};
+
 template <int D, bool PAGED>
-__global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
+__device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem& item) {
   using C = QCfg<D>;
   // two tile buffers per matrix (separate arrays: the compiler then tells the
   // direct loads into one apart from the reads of the other)
@@ -137,63 +149,15 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
   const int n16 = lane & 15;
   const int kg = lane >> 4;
 
-  // ---- this workgroup's item: segment, query tile, key tiles ---------------
-  int item, s, qt;
-  bool single;             // the segment has one range: write the output
-  int64_t t_lo, t_hi;      // key tiles [t_lo, t_hi) of the range
-  int rows;                // query rows of the segment
-  PagedBlock blk{0, 0, 0};
-  int32_t nent = 0;        // entries that the workgroup's rows see
-  if constexpr (PAGED) {
-    item = blockIdx.x;
-    s = item / p.qtiles;
-    qt = item - s * p.qtiles;
-    single = true;
-    blk = paged_block(p, s / p.Hkv);
-    rows = blk.n * p.G;
-    if (qt * kQRows >= rows) return;
-    if (blk.pos0 >= 0) nent = paged_entries(p, s, paged_pos(blk, (min(rows, (qt + 1) * kQRows) - 1) / p.G));
-    nent = __builtin_amdgcn_readfirstlane(nent);
-    t_lo = 0;
-    t_hi = (((int64_t)nent << p.page_shift) + kQKeys - 1) / kQKeys;
-  } else if (p.plan == nullptr) {
-    item = blockIdx.x;
-    s = item / p.qtiles;
-    qt = item - s * p.qtiles;
-    single = true;
-    t_lo = 0;
-    t_hi = seg_tiles(p, s);
-  } else {
-    // the grid is a multiple of 8 and at least the items, so every item
-    // i = x * per + y (x < 8, y < per) has its workgroup 8y + x
-    const int total = p.plan[0];
-    const int per = (total + 7) / 8;  // items per L2 domain
-    const int b = blockIdx.x;
-    if (b / 8 >= per) return;
-    item = (b % 8) * per + b / 8;
-    if (item >= total) return;
-    // the segment: the last s with first item <= item
-    int lo = 0, hi = p.nseg;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (p.plan[kQueryPlanHead + mid] <= item) lo = mid;
-      else hi = mid;
-    }
-    s = lo;
-    const int first = p.plan[kQueryPlanHead + s];
-    const int nr = (p.plan[kQueryPlanHead + s + 1] - first) / p.qtiles;
-    const int r = (item - first) / p.qtiles;
-    qt = item - first - r * p.qtiles;
-    single = nr == 1;
-    const int64_t tiles = seg_tiles(p, s);
-    t_lo = (int64_t)r * tiles / nr;
-    t_hi = (int64_t)(r + 1) * tiles / nr;
-  }
+  const int s = item.s, qt = item.qt;
+  const int64_t t_lo = item.t_lo, t_hi = item.t_hi;
+  const PagedBlock blk = item.blk;
+  const int32_t nent = item.nent;
+  const int rows = PAGED ? blk.n * p.G : p.rows;  // query rows of the segment
   const int bseq = s / p.Hkv;
   const int g = s - bseq * p.Hkv;
   int64_t base_len = 0, row0 = 0;
   if constexpr (!PAGED) {
-    rows = p.rows;
     if (p.seg_len[s] < 0) {
       // a segment dkv_compact could not pack (one range, so this workgroup
       // owns its query tile's output): no rows to attend, zeros
@@ -630,7 +594,7 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
   __builtin_amdgcn_s_waitcnt(0x0F70);
 
   // ---- row totals; write the output or this range's record ------------------
-  float* rec = p.rec + (int64_t)item * kQRows * C::kRec;
+  float* rec = item.rec;
 #pragma unroll
   for (int q = 0; q < kRG; ++q) {
     l[q] = lane_xor_sum<16>(l[q]);
@@ -641,7 +605,7 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
       const float lq = __shfl(l[q], 4 * kg + v, 64);
       const float mq = __shfl(m[q], 4 * kg + v, 64);
       if (rq < rows) {
-        if (single) {
+        if (item.single) {
           const int tq = rq / p.G;
           float* orow = p.out + ((tok_row0 + tq) * p.Hq + (int64_t)g * p.G + (rq - tq * p.G)) * D;
           const float inv = lq > 0.f ? 1.f / lq : 0.f;
@@ -658,6 +622,196 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
         }
       }
     }
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
+  // ---- this workgroup's item: segment, query tile, key tiles ---------------
+  int item, s, qt;
+  bool single;             // the segment has one range: write the output
+  int64_t t_lo, t_hi;      // key tiles [t_lo, t_hi) of the range
+  if (p.plan == nullptr) {
+    item = blockIdx.x;
+    s = item / p.qtiles;
+    qt = item - s * p.qtiles;
+    single = true;
+    t_lo = 0;
+    t_hi = seg_tiles(p, s);
+  } else {
+    // the grid is a multiple of 8 and at least the items, so every item
+    // i = x * per + y (x < 8, y < per) has its workgroup 8y + x
+    const int total = p.plan[0];
+    const int per = (total + 7) / 8;  // items per L2 domain
+    const int b = blockIdx.x;
+    if (b / 8 >= per) return;
+    item = (b % 8) * per + b / 8;
+    if (item >= total) return;
+    // the segment: the last s with first item <= item
+    int lo = 0, hi = p.nseg;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (p.plan[kQueryPlanHead + mid] <= item) lo = mid;
+      else hi = mid;
+    }
+    s = lo;
+    const int first = p.plan[kQueryPlanHead + s];
+    const int nr = (p.plan[kQueryPlanHead + s + 1] - first) / p.qtiles;
+    const int r = (item - first) / p.qtiles;
+    qt = item - first - r * p.qtiles;
+    single = nr == 1;
+    const int64_t tiles = seg_tiles(p, s);
+    t_lo = (int64_t)r * tiles / nr;
+    t_hi = (int64_t)(r + 1) * tiles / nr;
+  }
+  query_item<D, false>(p, QueryItem{s, qt, t_lo, t_hi, single, p.rec + (int64_t)item * kQRows * QCfg<D>::kRec,
+                                    PagedBlock{0, 0, 0}, 0});
+}
+
+// ---------------------------------------------------------------------------
+// Paged calls.  A unit is one query tile of one segment (of a sequence's own
+// number of them); its length is its key tiles (up to what its last row sees)
+// plus kUnitTiles for its fixed cost.  The lengths of all units, laid end to
+// end, are cut into P equal slices, one per workgroup: however unequal the
+// chunks and the contexts, every workgroup has the same work and all run at
+// once.  A unit that lies in one slice is written directly.  A slice holds at
+// most two parts of others, the rest of the unit it starts in (record slot 2w)
+// and the head of the unit it ends in (2w + 1; a unit that starts with the
+// slice is in slot 2w), and a combine kernel folds a unit's records in slice
+// order.  Consecutive slices, which share keys, go to the same L2 domain.
+// ---------------------------------------------------------------------------
+constexpr int kUnitTiles = 2;
+
+struct PagedUnit {
+  int32_t s, qt, nent, pad;
+};
+
+// Words of the plan: the slice count, the units' total length, each slice's
+// first unit, each unit's start and what it is.
+struct PagedPlan {
+  int32_t* slices;      // [2]: P, spare
+  int64_t* total;
+  int32_t* first;       // [kPagedSlices + 1] unit that holds the slice's start
+  int64_t* start;       // [units + 1]
+  PagedUnit* unit;      // [units]
+};
+
+__host__ __device__ __forceinline__ PagedPlan paged_plan_of(int32_t* words, int64_t units) {
+  PagedPlan x;
+  x.slices = words;
+  x.total = reinterpret_cast<int64_t*>(words + 2);
+  x.first = words + 4;
+  x.unit = reinterpret_cast<PagedUnit*>(words + 4 + kPagedSlices + 4);
+  x.start = reinterpret_cast<int64_t*>(x.unit + units);
+  return x;
+}
+
+__device__ __forceinline__ int64_t unit_tiles(const QueryParams& p, int32_t nent) {
+  return (((int64_t)nent << p.page_shift) + kQKeys - 1) / kQKeys;
+}
+
+// Entries that query tile qt of a block sees.
+__device__ __forceinline__ int32_t unit_entries(const QueryParams& p, const PagedBlock& k, int s, int qt) {
+  if (k.pos0 < 0) return 0;
+  const int64_t last = (int64_t)(qt + 1) * kQRows < (int64_t)k.n * p.G ? (int64_t)(qt + 1) * kQRows : (int64_t)k.n * p.G;
+  return paged_entries(p, s, paged_pos(k, (int32_t)((last - 1) / p.G)));
+}
+
+__global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p) {
+  __shared__ int64_t red[kPlanThreads / kWave + 1];
+  __shared__ int32_t pre[DKV_MAX_SEGMENTS + 1];  // query tiles of the sequences before
+  const int tid = threadIdx.x;
+  const int B = p.nseg / p.Hkv;
+  const PagedPlan plan = paged_plan_of(p.plan, p.max_items);
+  int64_t base = 0;
+  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    int64_t tiles = 0, sum;
+    if (b < B) tiles = ((int64_t)paged_block(p, b).n * p.G + kQRows - 1) / kQRows;
+    const int64_t ex = block_exclusive_scan<kPlanThreads>(tiles, red, &sum);
+    if (b < B) pre[b] = (int32_t)(base + ex);
+    base += sum;
+  }
+  if (tid == 0) pre[B] = (int32_t)base;
+  __syncthreads();
+  // offsets that overlap could name more units than the workspace holds
+  const int64_t units = base * p.Hkv < p.max_items ? base * p.Hkv : p.max_items;
+  int64_t len = 0;
+  for (int64_t u0 = 0; u0 < units; u0 += kPlanThreads) {
+    const int64_t u = u0 + tid;
+    int64_t mine = 0, sum;
+    if (u < units) {
+      int lo = 0, hi = B;  // the last sequence whose units start at or before u, and which has any
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((int64_t)pre[mid] * p.Hkv <= u) lo = mid;
+        else hi = mid;
+      }
+      const int tiles = pre[lo + 1] - pre[lo];
+      const int in = (int)(u - (int64_t)pre[lo] * p.Hkv);
+      const int g = in / tiles, qt = in - g * tiles;
+      const int s = lo * p.Hkv + g;
+      const int32_t nent = unit_entries(p, paged_block(p, lo), s, qt);
+      plan.unit[u] = PagedUnit{s, qt, nent, 0};
+      mine = unit_tiles(p, nent) + kUnitTiles;
+    }
+    const int64_t ex = block_exclusive_scan<kPlanThreads>(mine, red, &sum);
+    if (u < units) plan.start[u] = len + ex;
+    len += sum;
+  }
+  if (tid == 0) {
+    plan.start[units] = len;
+    plan.slices[0] = (int32_t)(len < p.P ? len : p.P);
+    plan.slices[1] = (int32_t)units;
+    plan.total[0] = len;
+  }
+  __syncthreads();
+  const int64_t P = len < p.P ? len : p.P;
+  if (tid < P) {
+    const int64_t x = (int64_t)tid * len / P;
+    int64_t lo = 0, hi = units;
+    while (hi - lo > 1) {
+      const int64_t mid = (lo + hi) >> 1;
+      if (plan.start[mid] <= x) lo = mid;
+      else hi = mid;
+    }
+    plan.first[tid] = (int32_t)lo;
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
+  if (p.plan == nullptr) {  // too few keys to split: one workgroup per (segment, query tile)
+    const int s = blockIdx.x / p.qtiles;
+    const int qt = blockIdx.x - s * p.qtiles;
+    const PagedBlock blk = paged_block(p, s / p.Hkv);
+    if ((int64_t)qt * kQRows >= (int64_t)blk.n * p.G) return;
+    const int32_t nent = __builtin_amdgcn_readfirstlane(unit_entries(p, blk, s, qt));
+    query_item<D, true>(p, QueryItem{s, qt, 0, unit_tiles(p, nent), true, nullptr, blk, nent});
+    return;
+  }
+  const PagedPlan plan = paged_plan_of(p.plan, p.max_items);
+  const int P = plan.slices[0], units = plan.slices[1];
+  const int64_t total = plan.total[0];
+  const int w = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;  // the grid is a multiple of 8
+  if (w >= P) return;
+  const int64_t lo = q_uniform64((int64_t)w * total / P), hi = q_uniform64((int64_t)(w + 1) * total / P);
+  int64_t end;
+  for (int u = plan.first[w]; u < units; ++u) {
+    const int64_t from = q_uniform64(plan.start[u]) + kUnitTiles;  // the unit's first key tile
+    end = q_uniform64(plan.start[u + 1]);
+    if (from - kUnitTiles >= hi) break;
+    const bool empty = from == end;  // no keys: zeros, by the slice that holds its start
+    const int64_t a = lo > from ? lo : from, b = hi < end ? hi : end;
+    if (empty ? from - kUnitTiles < lo : a >= b) continue;
+    const PagedUnit x = plan.unit[u];
+    const int s = __builtin_amdgcn_readfirstlane(x.s);
+    const int qt = __builtin_amdgcn_readfirstlane(x.qt);
+    const int32_t nent = __builtin_amdgcn_readfirstlane(x.nent);
+    float* rec = p.rec + (int64_t)(2 * w + (from > lo ? 1 : 0)) * kQRows * QCfg<D>::kRec;
+    query_item<D, true>(p, QueryItem{s, qt, a - from, b - from, empty || (a == from && b == end), rec,
+                                     paged_block(p, s / p.Hkv), nent});
+    __syncthreads();  // the tile buffers are free for the next unit
   }
 }
 
@@ -730,10 +884,87 @@ __global__ __launch_bounds__(kMergeThreads) void query_merge_kernel(QueryParams 
   *reinterpret_cast<f32x4*>(orow + 4 * c4) = A * inv;
 }
 
+// Combine kernel of paged calls: a unit that several slices share is folded by
+// the workgroups of the first of them.
+template <int D>
+__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(QueryParams p) {
+  using C = QCfg<D>;
+  constexpr int kParts = kQRows * (D / 4) / kMergeThreads;
+  const int w = blockIdx.x / kParts;
+  const PagedPlan plan = paged_plan_of(p.plan, p.max_items);
+  const int64_t P = plan.slices[0], total = plan.total[0];
+  if (w + 1 >= P) return;
+  const int64_t lo = (int64_t)w * total / P, hi = (int64_t)(w + 1) * total / P;
+  const int u = plan.first[w + 1];  // holds hi
+  const int64_t from = plan.start[u] + kUnitTiles, end = plan.start[u + 1];
+  if (from < lo || from >= hi || end <= hi) return;  // starts in another slice, or ends with this one
+  const int nr = (int)owner_of(end - 1, total, P) - w + 1;
+  const PagedUnit x = plan.unit[u];
+  const PagedBlock blk = paged_block(p, x.s / p.Hkv);
+  const int it = (blockIdx.x - w * kParts) * kMergeThreads + threadIdx.x;
+  const int rr = it / (D / 4);
+  const int c4 = it - rr * (D / 4);
+  const int rq = x.qt * kQRows + rr;
+  if (rq >= blk.n * p.G) return;
+  float M = -INFINITY, L = 0.f;
+  f32x4 A = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = 0; k0 < nr; k0 += kMergeBatch) {
+    float mk[kMergeBatch], lk[kMergeBatch];
+    f32x4 ak[kMergeBatch];
+#pragma unroll
+    for (int k = 0; k < kMergeBatch; ++k) {
+      mk[k] = -INFINITY;
+      lk[k] = 0.f;
+      ak[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (k0 + k < nr) {
+        const int slot = 2 * (w + k0 + k) + (k0 + k == 0 && from > lo ? 1 : 0);
+        const float* r = p.rec + (int64_t)slot * kQRows * C::kRec + (int64_t)rr * C::kRec;
+        mk[k] = r[0];
+        lk[k] = r[1];
+        ak[k] = *reinterpret_cast<const f32x4*>(r + 2 + 4 * c4);
+      }
+    }
+    float Mn = M;
+#pragma unroll
+    for (int k = 0; k < kMergeBatch; ++k) Mn = fmaxf(Mn, mk[k]);
+    const float Mu = Mn == -INFINITY ? 0.f : Mn;
+    const float fo = fast_exp2(M - Mu);
+    L *= fo;
+    A *= fo;
+#pragma unroll
+    for (int k = 0; k < kMergeBatch; ++k) {
+      const float f = fast_exp2(mk[k] - Mu);
+      L += f * lk[k];
+      A += f * ak[k];
+    }
+    M = Mn;
+  }
+  const float inv = L > 0.f ? 1.f / L : 0.f;
+  const int tq = rq / p.G;
+  const int g = x.s % p.Hkv;
+  float* orow = p.out + (((int64_t)blk.tok0 + tq) * p.Hq + (int64_t)g * p.G + (rq - tq * p.G)) * D;
+  *reinterpret_cast<f32x4*>(orow + 4 * c4) = A * inv;
+}
+
+template <int D>
+hipError_t launch_paged_d(const QueryParams& p, hipStream_t stream) {
+  if (p.plan == nullptr) {
+    hipLaunchKernelGGL((paged_query_kernel<D>), dim3((unsigned)((int64_t)p.nseg * p.qtiles)), dim3(kQThreads), 0, stream,
+                       p);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p);
+  hipLaunchKernelGGL((paged_query_kernel<D>), dim3((unsigned)p.P), dim3(kQThreads), 0, stream, p);
+  if (p.P > 1)
+    hipLaunchKernelGGL((paged_merge_kernel<D>), dim3((unsigned)((p.P - 1) * (kQRows * (D / 4) / kMergeThreads))),
+                       dim3(kMergeThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
 template <int D>
 hipError_t launch_d(const QueryParams& p, int64_t grid, hipStream_t stream) {
   if (p.plan != nullptr) hipLaunchKernelGGL(query_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p);
-  hipLaunchKernelGGL((query_attn_kernel<D, false>), dim3((unsigned)grid), dim3(kQThreads), 0, stream, p);
+  hipLaunchKernelGGL((query_attn_kernel<D>), dim3((unsigned)grid), dim3(kQThreads), 0, stream, p);
   if (p.plan != nullptr) {
     const int64_t parts = (int64_t)kQRows * (D / 4) / kMergeThreads;
     hipLaunchKernelGGL((query_merge_kernel<D>), dim3((unsigned)((int64_t)p.nseg * p.qtiles * parts)),
@@ -775,11 +1006,30 @@ hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, h
   return head_dim == 64 ? launch_d<64>(p, grid, stream) : launch_d<128>(p, grid, stream);
 }
 
+PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t head_dim, int32_t num_tokens,
+                                int32_t max_q, int64_t rows_hint) {
+  PagedPlanShape sh;
+  const int64_t nseg = (int64_t)batch * hkv;
+  const int64_t qtiles = ((int64_t)max_q * G + kQRows - 1) / kQRows;
+  // query tiles of all sequences: each has at most one that is not full
+  const int64_t full = (int64_t)num_tokens * G / kQRows + batch;
+  sh.units = hkv * (full < batch * qtiles ? full : batch * qtiles);
+  const int64_t hint = rows_hint < ((int64_t)1 << 40) ? rows_hint : ((int64_t)1 << 40);
+  const int64_t seg = hint > 0 ? (hint + nseg * kQKeys - 1) / (nseg * kQKeys) : kQueryUnknownTiles;  // tiles, on average
+  sh.slices = 0;
+  sh.plan_bytes = sh.rec_bytes = 0;
+  // segments of fewer than two ranges' worth of keys on average: no split
+  if (seg < 2 * kQueryMinTiles) return sh;
+  const int64_t P = sh.units * seg / kQueryMinTiles;
+  sh.slices = (int32_t)((P < kPagedSlices ? P + 7 : kPagedSlices) / 8 * 8);
+  sh.plan_bytes = ((size_t)(4 + kPagedSlices + 4) * sizeof(int32_t) + (size_t)sh.units * sizeof(PagedUnit) +
+                   (size_t)(sh.units + 1) * sizeof(int64_t) + 255) / 256 * 256;
+  sh.rec_bytes = (size_t)(2 * sh.slices) * kQRows * (head_dim + 2) * sizeof(float);
+  return sh;
+}
+
 hipError_t launch_paged_query_attn(const QueryParams& p, int head_dim, hipStream_t stream) {
-  const dim3 grid((unsigned)((int64_t)p.nseg * p.qtiles)), block(kQThreads);
-  if (head_dim == 64) hipLaunchKernelGGL((query_attn_kernel<64, true>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((query_attn_kernel<128, true>), grid, block, 0, stream, p);
-  return hipGetLastError();
+  return head_dim == 64 ? launch_paged_d<64>(p, stream) : launch_paged_d<128>(p, stream);
 }
 
 }  // namespace dkv
