@@ -339,6 +339,14 @@ dkv_status dkv_paged_query_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_he
   p.max_entries = max_entries;
   p.page_shift = __builtin_ctz((unsigned)page_rows);
   p.num_tokens = num_tokens;
+  if (sh.shorts) {
+    p.stream_once = rows_hint <= 0 || rows_hint > dkv::kShortCachedBytes / (4 * head_dim);
+    p.P = sh.slices;
+    p.rec_rows = sh.rec_rows;
+    p.seg_meta = static_cast<int32_t*>(workspace);
+    p.rec = reinterpret_cast<float*>(static_cast<char*>(workspace) + sh.plan_bytes);
+    return hip_status(dkv::launch_paged_query_short(p, head_dim, (hipStream_t)stream));
+  }
   if (sh.slices > 0) {
     p.P = sh.slices;
     p.max_items = (int32_t)sh.units;

@@ -115,12 +115,15 @@ hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, h
 // can have, and the slices its keys are cut into (0: no split).
 constexpr int kPagedSlices = 256;  // one workgroup per compute unit
 struct PagedPlanShape {
+  bool shorts;  // the kernels for short blocks take the call
   int64_t units;
   int32_t slices;
-  size_t plan_bytes, rec_bytes;
+  size_t plan_bytes, rec_bytes;  // short blocks: segment metadata, records of rec_rows rows
+  int32_t rec_rows;
 };
 PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t head_dim, int32_t num_tokens,
                                 int32_t max_q, int64_t rows_hint);
 hipError_t launch_paged_query_attn(const QueryParams& p, int head_dim, hipStream_t stream);
+hipError_t launch_paged_query_short(const QueryParams& p, int head_dim, hipStream_t stream);
 
 }  // namespace dkv

@@ -40,6 +40,18 @@ __device__ __forceinline__ void bf16_split(float x0, float x1, uint32_t& a, uint
   b = __builtin_bit_cast(uint32_t, l);
 }
 
+// The same in three bf16 pairs: a + b + c carries all 24 bits of x.
+__device__ __forceinline__ void bf16_split3(float x0, float x1, uint32_t& a, uint32_t& b, uint32_t& c) {
+  const f32x2 x = {x0, x1};
+  const bf16x2 h = __builtin_convertvector(x, bf16x2);
+  const f32x2 r = x - __builtin_convertvector(h, f32x2);
+  const bf16x2 l = __builtin_convertvector(r, bf16x2);
+  const bf16x2 t = __builtin_convertvector(r - __builtin_convertvector(l, f32x2), bf16x2);
+  a = __builtin_bit_cast(uint32_t, h);
+  b = __builtin_bit_cast(uint32_t, l);
+  c = __builtin_bit_cast(uint32_t, t);
+}
+
 // Maximum over the lanes that share (lane % 16).
 __device__ __forceinline__ float row4_max(float x) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);

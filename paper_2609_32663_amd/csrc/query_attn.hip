@@ -1018,8 +1018,19 @@ PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t h
   const int64_t seg = hint > 0 ? (hint + nseg * kQKeys - 1) / (nseg * kQKeys) : kQueryUnknownTiles;  // tiles, on average
   sh.slices = 0;
   sh.plan_bytes = sh.rec_bytes = 0;
+  const int64_t rows = (int64_t)max_q * G;
+  sh.rec_rows = (int32_t)((rows + 3) / 4 * 4);
+  sh.shorts = rows <= kShortRows / 4;
   // segments of fewer than two ranges' worth of keys on average: no split
   if (seg < 2 * kQueryMinTiles) return sh;
+  if (sh.shorts) {
+    // at least 128 keys per workgroup, up to 256 workgroups
+    const int64_t P = hint > 0 && hint < kPagedSlices * 128 ? (hint + 127) / 128 : kPagedSlices;
+    sh.slices = (int32_t)P;
+    sh.plan_bytes = ((size_t)nseg * 2 * sizeof(int32_t) + 255) / 256 * 256;
+    sh.rec_bytes = (size_t)(P + nseg) * sh.rec_rows * (head_dim + 2) * sizeof(float);
+    return sh;
+  }
   const int64_t P = sh.units * seg / kQueryMinTiles;
   sh.slices = (int32_t)((P < kPagedSlices ? P + 7 : kPagedSlices) / 8 * 8);
   sh.plan_bytes = ((size_t)(4 + kPagedSlices + 4) * sizeof(int32_t) + (size_t)sh.units * sizeof(PagedUnit) +

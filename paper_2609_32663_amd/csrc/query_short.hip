@@ -62,7 +62,16 @@ struct SCfg {
   static constexpr int kDma = kSKeys * kRowChunks / 64;  // direct loads per tile and matrix
 };
 
-__device__ __forceinline__ int64_t short_rows(const QueryParams& p, int s) {
+// Length of segment s in the split's units: rows, or runs of 32 rows of the
+// row space of a paged cache (the slots outside an entry's range included).
+template <bool PAGED>
+__device__ __forceinline__ int64_t short_units(const QueryParams& p, int s) {
+  if constexpr (PAGED) {
+    const PagedBlock k = paged_block(p, s / p.Hkv);
+    const int32_t n = p.n_entries[s];
+    if (k.n == 0 || k.pos0 < 0 || n < 0) return 0;
+    return (int64_t)(n > p.max_entries ? p.max_entries : n) << (p.page_shift - 5);
+  }
   const int32_t len = p.seg_len[s];
   return len < 0 ? 0 : (int64_t)len + p.n_tail + p.n_q;
 }
@@ -76,19 +85,24 @@ constexpr int short_stages() {
   return KW == 1 || (RW > 1 && NT) ? 3 : 2;
 }
 
-template <int D, int RW, int KW, bool NT>
+template <int D, int RW, int KW, bool NT, bool PAGED>
 __global__ __launch_bounds__(512)
 void query_short_kernel(QueryParams p) {
   using C = SCfg<D>;
   constexpr int RG = kSRG;
   constexpr int kThreads = RW * KW * kWave;
-  constexpr int64_t kSegCost = 196608 / (2 * C::kRowBytes);  // as the decode step's
-  extern __shared__ __align__(16) int64_t pre[];             // [nseg + 1] unit prefix, [nseg] offsets (split calls)
+  constexpr int64_t kUnit = PAGED ? kRun : 1;                        // rows per unit of the split
+  constexpr int64_t kSegCost = 196608 / (2 * C::kRowBytes) / kUnit;  // as the decode step's
+  // [nseg + 1] unit prefix, packed: [nseg] offsets (split calls)
+  extern __shared__ __align__(16) int64_t pre[];
   // S tiles per key wave and matrix (separate arrays: the compiler then tells
   // the direct loads into one apart from the reads of the others), and what
   // the key waves hand each other at the fold
   constexpr int S = short_stages<RW, KW, NT>();
   constexpr int kTile = KW * kSKeys * D;
+  // Packed: two parts, 16 to 17 bits.  Paged: three, the probabilities' 24
+  // bits; the third product hides behind the loads of these kernels.
+  constexpr int kParts = PAGED ? 3 : 2;
   static_assert(S == 2 || S == 3, "the ring's arrays");
   __shared__ __align__(1024) uint16_t k0[kTile], k1[kTile], k2[S > 2 ? kTile : 8];
   __shared__ __align__(1024) uint16_t v0[kTile], v1[kTile], v2[S > 2 ? kTile : 8];
@@ -116,9 +130,9 @@ void query_short_kernel(QueryParams p) {
     const int s_lo = tid * per, s_hi = min(nseg, s_lo + per);
     int64_t sum = 0;
     for (int i = s_lo; i < s_hi; ++i) {
-      const int64_t rows = short_rows(p, i);
+      const int64_t rows = short_units<PAGED>(p, i);
       const int64_t u = rows > 0 ? rows + kSegCost : 0;
-      pre[nseg + 1 + i] = p.seg_off[i];
+      if (!PAGED) pre[nseg + 1 + i] = p.seg_off[i];
       pre[i] = u;
       sum += u;
     }
@@ -136,11 +150,20 @@ void query_short_kernel(QueryParams p) {
   }
   // segments with no rows (not packed) produce zeros
   for (int z = w; z < nseg; z += gridDim.x) {
-    if (p.seg_len[z] >= 0) continue;
     const int b = z / p.Hkv, g = z - (z / p.Hkv) * p.Hkv;
-    for (int i = tid; i < p.rows * D; i += kThreads) {
+    int rows = p.rows;
+    int64_t tok_row0 = (int64_t)b * p.n_q;
+    if constexpr (PAGED) {
+      if (short_units<PAGED>(p, z) > 0) continue;
+      const PagedBlock k = paged_block(p, b);
+      rows = k.n * p.G;
+      tok_row0 = k.tok0;
+    } else {
+      if (p.seg_len[z] >= 0) continue;
+    }
+    for (int i = tid; i < rows * D; i += kThreads) {
       const int r = i / D, tok = r / p.G;
-      p.out[(((int64_t)b * p.n_q + tok) * p.Hq + (int64_t)g * p.G + (r - tok * p.G)) * D + i % D] = 0.f;
+      p.out[((tok_row0 + tok) * p.Hq + (int64_t)g * p.G + (r - tok * p.G)) * D + i % D] = 0.f;
     }
     if (split && tid == 0) p.seg_meta[2 * z] = p.seg_meta[2 * z + 1] = 0;  // nothing to combine
   }
@@ -179,7 +202,7 @@ void query_short_kernel(QueryParams p) {
       a = (lo > seg_lo ? lo : seg_lo) - seg_lo;
       bnd = (hi < seg_hi ? hi : seg_hi) - seg_lo;
     } else {
-      bnd = q_uniform64(short_rows(p, s));
+      bnd = q_uniform64(short_units<PAGED>(p, s));
     }
     if (a >= bnd) {
       if (!split) break;
@@ -187,11 +210,29 @@ void query_short_kernel(QueryParams p) {
     }
     const int bseq = s / p.Hkv;
     const int g = s - bseq * p.Hkv;
-    const int64_t base_len = (split ? seg_hi - seg_lo : bnd) - p.n_q;  // rows every query row sees
-    const int64_t row0 = q_uniform64(split ? pre[nseg + 1 + s] : p.seg_off[s]) + a;
+    const int64_t base_len = (split ? seg_hi - seg_lo : bnd) - p.n_q;  // packed: rows every query row sees
+    const int64_t row0 = PAGED ? 0 : q_uniform64(split ? pre[nseg + 1 + s] : p.seg_off[s]) + a;
     const char* kbase = reinterpret_cast<const char*>(p.k) + row0 * C::kRowBytes;
     const char* vbase = reinterpret_cast<const char*>(p.v) + row0 * C::kRowBytes;
-    const int64_t nkeys = q_uniform64(bnd - a);
+    const int64_t nkeys = q_uniform64((bnd - a) * kUnit);
+    // paged: the sequence's block, the entries held, and where the piece ends
+    // in the segment's rows and positions
+    PagedBlock blk{0, 0, 0};
+    PagedEntries held{0, 0, 0, 0};
+    int32_t nent = 0, row_lo = 0, row_hi = 0, pos_stop = 0, pos_all = 0;
+    int rows = p.rows;
+    if constexpr (PAGED) {
+      nent = (int32_t)q_uniform64((split ? seg_hi - seg_lo : bnd) >> (p.page_shift - 5));
+      row_lo = (int32_t)q_uniform64(a * kUnit);
+      row_hi = (int32_t)q_uniform64(bnd * kUnit);
+      held.load(p, s, nent, row_lo >> p.page_shift);
+      blk = paged_block(p, bseq);
+      rows = blk.n * p.G;
+      pos_stop = paged_pos(blk, blk.n - 1) + 1;
+      pos_all = paged_pos(blk, min(16 * RG * rw, rows - 1) / p.G) + 1;  // the wave's first row's position, past it
+    }
+    PagedRun ring[S] = {};
+    const int64_t tok_row0 = PAGED ? (int64_t)blk.tok0 : (int64_t)bseq * p.n_q;
     // every row sees the piece's keys below this one
     const int64_t all_see = q_uniform64(base_len + 1 - a < nkeys ? base_len + 1 - a : nkeys);
 
@@ -200,10 +241,19 @@ void query_short_kernel(QueryParams p) {
     // touching memory; the row displacement is part of the vector offset,
     // which costs these kernels nothing (23 tokens of an 8B layer at 32K 27.7
     // us either way).
-    auto load = [&](uint16_t* kt, uint16_t* vt, int64_t t) __attribute__((always_inline)) {
+    // Paged: a tile is one run; its descriptor covers the run's slots [lo, hi),
+    // so the slots before them get wrapped offsets and read zeros too.
+    auto load = [&](uint16_t* kt, uint16_t* vt, int64_t t, PagedRun& run) __attribute__((always_inline)) {
       const int64_t left = nkeys - t * kSKeys;
-      const uint32_t nk = (uint32_t)(left <= 0 ? 0 : (left < kSKeys ? left : kSKeys));
-      const int64_t from = nk > 0 ? t * kSKeys * C::kRowBytes : 0;
+      uint32_t nk = (uint32_t)(left <= 0 ? 0 : (left < kSKeys ? left : kSKeys));
+      int64_t from = nk > 0 ? t * kSKeys * C::kRowBytes : 0;
+      uint32_t skip = 0;
+      if constexpr (PAGED) {
+        run = paged_run(p, held, s, nent, row_lo + (int32_t)t * kSKeys, row_hi, pos_stop);
+        nk = (uint32_t)(run.hi - run.lo);
+        from = (run.row + run.lo) * C::kRowBytes;
+        skip = (uint32_t)(run.lo * C::kRowBytes);
+      }
       const __amdgpu_buffer_rsrc_t ks = q_rsrc(kbase + from, nk * C::kRowBytes);
       const __amdgpu_buffer_rsrc_t vs = q_rsrc(vbase + from, nk * C::kRowBytes);
 #pragma unroll
@@ -212,7 +262,7 @@ void query_short_kernel(QueryParams p) {
         if (RW > C::kDma && rw >= C::kDma) break;
         const int at = 16 * (4 * i / C::kRowChunks) * C::kRowBytes + 16 * (4 * i % C::kRowChunks);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (__attribute__((address_space(3))) void*)(kt + 512 * i), 16,
-                                                 koff + at, 0, 0, NT ? kStreamOnce : 0);
+                                                 koff + at - skip, 0, 0, NT ? kStreamOnce : 0);
       }
 #pragma unroll
       for (int i0 = 0; i0 < C::kDma; i0 += RW) {
@@ -220,7 +270,7 @@ void query_short_kernel(QueryParams p) {
         if (RW > C::kDma && rw >= C::kDma) break;
         const int at = 8 * (4 * i / C::kPairs) * C::kRowBytes + 32 * (4 * i % C::kPairs);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (__attribute__((address_space(3))) void*)(vt + 512 * i), 16,
-                                                 voff + at, 0, 0, NT ? kStreamOnce : 0);
+                                                 voff + at - skip, 0, 0, NT ? kStreamOnce : 0);
       }
       __builtin_amdgcn_sched_barrier(0);
     };
@@ -228,22 +278,24 @@ void query_short_kernel(QueryParams p) {
     uint16_t* const kb[3] = {k0 + kw * kSKeys * D, k1 + kw * kSKeys * D, S > 2 ? k2 + kw * kSKeys * D : k2};
     uint16_t* const vb[3] = {v0 + kw * kSKeys * D, v1 + kw * kSKeys * D, S > 2 ? v2 + kw * kSKeys * D : v2};
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i) load(kb[i], vb[i], kw + i * KW);
+    for (int i = 0; i < S - 1; ++i) load(kb[i], vb[i], kw + i * KW, ring[i]);
 
     // B operand of QK: query row 16 (RG rw + q) + n16, dims 32u + 8kg .. +7;
-    // cut: the keys of the piece that the row sees
+    // cut: the keys of the piece that the row sees; paged: the positions below which it sees
     u32x4 qb[RG][C::kChunks];
     int64_t cut[RG];
 #pragma unroll
     for (int q = 0; q < RG; ++q) {
       const int r = 16 * (RG * rw + q) + n16;
-      const bool ok = r < p.rows;
+      const bool ok = r < rows;
       const int tok = ok ? r / p.G : 0;
       const int64_t see = base_len + tok + 1 - a;
-      cut[q] = see < nkeys ? see : nkeys;
-      const char* qrow = reinterpret_cast<const char*>(p.q) +
-                         (((int64_t)bseq * p.n_q + tok) * p.Hq + (int64_t)g * p.G + (ok ? r - tok * p.G : 0)) *
-                             C::kRowBytes;
+      cut[q] = PAGED ? paged_pos(blk, tok) + 1 : (see < nkeys ? see : nkeys);
+      const char* qrow = reinterpret_cast<const char*>(p.q);
+      if constexpr (PAGED)
+        qrow += (tok_row0 + tok) * p.q_stride + ((int64_t)g * p.G + (ok ? r - tok * p.G : 0)) * C::kRowBytes;
+      else
+        qrow += ((tok_row0 + tok) * p.Hq + (int64_t)g * p.G + (ok ? r - tok * p.G : 0)) * C::kRowBytes;
 #pragma unroll
       for (int u = 0; u < C::kChunks; ++u) {
         const u32x4 z = {0u, 0u, 0u, 0u};
@@ -262,7 +314,7 @@ void query_short_kernel(QueryParams p) {
     }
 
     float sc[RG][2][4];
-    u32x4 ph[RG], pl[RG];
+    u32x4 pp[kParts][RG];  // the probabilities' bf16 parts
     // S^T = K Q^T: lane (n16, kg) receives the scores of keys 16j + 4kg + v
     auto qk = [&](const uint16_t* kt) __attribute__((always_inline)) {
       f32x4 acc[RG][2];
@@ -286,9 +338,26 @@ void query_short_kernel(QueryParams p) {
           for (int v = 0; v < 4; ++v) sc[q][j][v] = acc[q][j][v];
     };
     // Scores of tile t to probabilities, as two bf16 parts.
-    auto softmax = [&](int64_t t) __attribute__((always_inline)) {
+    auto softmax = [&](int64_t t, const PagedRun& run) __attribute__((always_inline)) {
       const int64_t key0 = t * kSKeys;
-      if (key0 + kSKeys > all_see) {
+      if constexpr (PAGED) {
+        // slots outside the entry, or past the position of one of the wave's rows
+        if (run.lo > 0 || run.hi < kRun || run.pos + kRun > pos_all) {
+          asm volatile("");
+#pragma unroll
+          for (int q = 0; q < RG; ++q) {
+            const int32_t rel = (int32_t)cut[q] - run.pos;
+            const int32_t lim = rel < run.hi ? rel : run.hi;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) {
+                const int key = 16 * j + 4 * kg + v;
+                if (key >= lim || key < run.lo) sc[q][j][v] = -INFINITY;
+              }
+          }
+        }
+      } else if (key0 + kSKeys > all_see) {
         asm volatile("");  // keeps this a branch: the selects would run for every tile
 #pragma unroll
         for (int q = 0; q < RG; ++q) {
@@ -346,10 +415,12 @@ void query_short_kernel(QueryParams p) {
         asm volatile("" : "+v"(l[q]));  // the sum is formed here, not sunk into a later phase
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          uint32_t x, y;
-          bf16_split(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y);
-          ph[q][e] = x;
-          pl[q][e] = y;
+          uint32_t x, y, z = 0;
+          if constexpr (kParts == 3) bf16_split3(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y, z);
+          else bf16_split(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y);
+          pp[0][q][e] = x;
+          pp[1][q][e] = y;
+          if constexpr (kParts == 3) pp[2][q][e] = z;
         }
       }
     };
@@ -371,14 +442,14 @@ void query_short_kernel(QueryParams p) {
           vf[bb] = u32x4{w0.x, w0.y, w1.x, w1.y};
         }
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
+        for (int part = 0; part < kParts; ++part)
 #pragma unroll
           for (int bb = 0; bb < 2; ++bb)
 #pragma unroll
             for (int q = 0; q < RG; ++q) {
               const int b = b0 + bb;
               f32x4 c = {o[q][b][0], o[q][b][1], o[q][b][2], o[q][b][3]};
-              c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, part ? pl[q] : ph[q]),
+              c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pp[part][q]),
                                                           __builtin_bit_cast(bf16x8, vf[bb]), c, 0, 0, 0);
               o[q][b][0] = c[0];
               o[q][b][1] = c[1];
@@ -412,11 +483,11 @@ void query_short_kernel(QueryParams p) {
       for (int i = 0; i < S; ++i) {
         const int64_t r = r0 + i;
         if (r < nround) {
-          if (RW == 1) load(kb[(i + S - 1) % S], vb[(i + S - 1) % S], kw + (r + S - 1) * KW);
+          if (RW == 1) load(kb[(i + S - 1) % S], vb[(i + S - 1) % S], kw + (r + S - 1) * KW, ring[(i + S - 1) % S]);
           arrive(std::integral_constant<int, (RW == 1 ? S - 1 : S - 2) * 2 * C::kDma / RW>{});
-          if (RW > 1) load(kb[(i + S - 1) % S], vb[(i + S - 1) % S], kw + (r + S - 1) * KW);
+          if (RW > 1) load(kb[(i + S - 1) % S], vb[(i + S - 1) % S], kw + (r + S - 1) * KW, ring[(i + S - 1) % S]);
           qk(kb[i]);
-          softmax(kw + r * KW);
+          softmax(kw + r * KW, ring[i]);
           pv(vb[i]);
         }
       }
@@ -496,15 +567,15 @@ void query_short_kernel(QueryParams p) {
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const int r = r0 + v;
-          if (r < p.rows) {
+          if (r < rows) {
             const int tok = r / p.G;
-            float* orow = p.out + (((int64_t)bseq * p.n_q + tok) * p.Hq + (int64_t)g * p.G + (r - tok * p.G)) * D;
+            float* orow = p.out + ((tok_row0 + tok) * p.Hq + (int64_t)g * p.G + (r - tok * p.G)) * D;
             const float inv = L[v] > 0.f ? 1.f / L[v] : 0.f;
 #pragma unroll
             for (int b = 0; b < HB; ++b) orow[c0 + 16 * b] = A[b][v] * inv;
           }
         }
-      } else if (r0 < p.rows) {  // rec_rows covers whole groups of 4 rows
+      } else if (r0 < rows) {  // rec_rows covers whole groups of 4 rows
         if (kw == 0 && h0 == 0 && n16 == 0) {
           *reinterpret_cast<f32x4*>(rec + r0) = M;
           *reinterpret_cast<f32x4*>(rec + p.rec_rows + r0) = L;
@@ -524,7 +595,7 @@ void query_short_kernel(QueryParams p) {
 // Combine kernel: one workgroup per (segment, row), as the decode step's:
 // thread (ph, cq) folds pieces ph, ph + kPhases, ... of columns 4cq..4cq+3,
 // kBatch records per memory round trip, then the phases are folded in order.
-template <int D>
+template <int D, bool PAGED>
 __global__ __launch_bounds__(kSMergeThreads) void query_short_merge_kernel(QueryParams p) {
   constexpr int kQuads = D / 4;
   constexpr int kPhases = kSMergeThreads / kQuads;
@@ -535,6 +606,12 @@ __global__ __launch_bounds__(kSMergeThreads) void query_short_merge_kernel(Query
   const int r = blockIdx.x - s * p.rows;
   const int n = p.seg_meta[2 * s + 1];
   if (n <= 1) return;
+  int64_t tok_row0 = (int64_t)(s / p.Hkv) * p.n_q;
+  if constexpr (PAGED) {
+    const PagedBlock k = paged_block(p, s / p.Hkv);
+    if (r >= k.n * p.G) return;
+    tok_row0 = k.tok0;
+  }
   const int64_t stride = (int64_t)p.rec_rows * (D + 2);
   const float* first = p.rec + (int64_t)p.seg_meta[2 * s] * stride;
   const int tid = threadIdx.x;
@@ -590,37 +667,41 @@ __global__ __launch_bounds__(kSMergeThreads) void query_short_merge_kernel(Query
       Lt += f * xl[t];
       At += f * xa[t];
     }
-    const int bseq = s / p.Hkv, g = s - (s / p.Hkv) * p.Hkv;
+    const int g = s - (s / p.Hkv) * p.Hkv;
     const int tok = r / p.G;
-    float* o = p.out + (((int64_t)bseq * p.n_q + tok) * p.Hq + (int64_t)g * p.G + (r - tok * p.G)) * D + 4 * cq;
+    float* o = p.out + ((tok_row0 + tok) * p.Hq + (int64_t)g * p.G + (r - tok * p.G)) * D + 4 * cq;
     *reinterpret_cast<f32x4*>(o) = At * (Lt > 0.f ? 1.f / Lt : 0.f);
   }
 }
 
-template <int D, int RW, int KW>
+template <int D, int RW, int KW, bool PAGED>
 hipError_t launch_short_r(const QueryParams& p, hipStream_t stream) {
-  const size_t lds = p.P > 0 ? (2 * (size_t)p.nseg + 1) * sizeof(int64_t) : 0;
+  const size_t lds = p.P > 0 ? ((PAGED ? 1 : 2) * (size_t)p.nseg + 1) * sizeof(int64_t) : 0;
   const dim3 grid((unsigned)(p.P > 0 ? p.P : p.nseg)), block(RW * KW * kWave);
-  if (p.stream_once) hipLaunchKernelGGL((query_short_kernel<D, RW, KW, true>), grid, block, lds, stream, p);
-  else hipLaunchKernelGGL((query_short_kernel<D, RW, KW, false>), grid, block, lds, stream, p);
+  if (p.stream_once) hipLaunchKernelGGL((query_short_kernel<D, RW, KW, true, PAGED>), grid, block, lds, stream, p);
+  else hipLaunchKernelGGL((query_short_kernel<D, RW, KW, false, PAGED>), grid, block, lds, stream, p);
   if (p.P > 1)
-    hipLaunchKernelGGL((query_short_merge_kernel<D>), dim3((unsigned)(p.nseg * p.rows)), dim3(kSMergeThreads), 0,
+    hipLaunchKernelGGL((query_short_merge_kernel<D, PAGED>), dim3((unsigned)(p.nseg * p.rows)), dim3(kSMergeThreads), 0,
                        stream, p);
   return hipGetLastError();
 }
 
-template <int D>
+template <int D, bool PAGED>
 hipError_t launch_short_d(const QueryParams& p, hipStream_t stream) {
-  if (p.rows <= 32) return launch_short_r<D, 1, 4>(p, stream);
-  if (p.rows <= 64) return launch_short_r<D, 2, 2>(p, stream);
-  if (p.rows <= 128) return launch_short_r<D, 4, 2>(p, stream);
-  return launch_short_r<D, 8, 1>(p, stream);
+  if (p.rows <= 32) return launch_short_r<D, 1, 4, PAGED>(p, stream);
+  if (p.rows <= 64) return launch_short_r<D, 2, 2, PAGED>(p, stream);
+  if (p.rows <= 128) return launch_short_r<D, 4, 2, PAGED>(p, stream);
+  return launch_short_r<D, 8, 1, PAGED>(p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_query_short(const QueryParams& p, int head_dim, hipStream_t stream) {
-  return head_dim == 64 ? launch_short_d<64>(p, stream) : launch_short_d<128>(p, stream);
+  return head_dim == 64 ? launch_short_d<64, false>(p, stream) : launch_short_d<128, false>(p, stream);
+}
+
+hipError_t launch_paged_query_short(const QueryParams& p, int head_dim, hipStream_t stream) {
+  return head_dim == 64 ? launch_short_d<64, true>(p, stream) : launch_short_d<128, true>(p, stream);
 }
 
 }  // namespace dkv
