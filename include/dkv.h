@@ -623,8 +623,11 @@ size_t dkv_page_extend_workspace_bytes(int32_t num_units);
  * wholly below max_tokens, or the pages it needs, counted behind those of all
  * the units before it, pass the free ones.  Nothing of it changes; a unit that
  * needs no page is not held up by the ones before it.
- * DKV_ERR_UNSUPPORTED when N * Hkv > 65535 or max_tokens * Hkv > 2^32 - 256.
- * The call enqueues one kernel over the units and one over the tokens.
+ * DKV_ERR_UNSUPPORTED when N * Hkv > 65535, max_tokens > 2^31 - 128 or
+ * max_tokens * Hkv > 2^32 - 256.
+ * The call enqueues one kernel when max_tokens is at most 128, or at most 8,192
+ * and neither new_len nor n_free_out is updated in place; otherwise one over
+ * the units and one over the tokens.
  */
 dkv_status dkv_page_extend(int32_t num_units, int32_t num_kv_heads, int32_t page_rows,
                            const int32_t *unit_new, const int32_t *unit_len, int32_t *new_len,

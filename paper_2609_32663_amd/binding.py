@@ -177,22 +177,24 @@ def _rows(t, name, heads, dim, dtype):
     than heads * dim: a part of a fused projection's output."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.dtype != dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+    tokens, h, n = t.shape
+    if t.dtype is not dtype or h != heads or n != dim:
         raise ValueError(f"{name} must be {dtype} [tokens][{heads}][{dim}]")
-    one, st = t.shape[0] <= 1, t.stride()
-    if st[2] != 1 or (heads > 1 and st[1] != dim) or (not one and st[0] < heads * dim):
+    per_token, per_head, per_dim = t.stride()
+    if per_dim != 1 or (per_head != dim and heads > 1) or (per_token < heads * dim and tokens > 1):
         raise ValueError(f"{name} must hold each token's heads as consecutive rows, tokens not overlapping")
-    return t.data_ptr(), heads * dim if one else st[0]
+    return t.data_ptr(), per_token if tokens > 1 else heads * dim
 
 
 def _typed(t, name, dtype, shape=None, optional=False):
     """_dev of a tensor of this element type (and shape)."""
+    if (type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.is_contiguous()
+            and (shape is None or t.shape == shape)):
+        return t.data_ptr()
     if t is None and optional:
         return None
-    p = _dev(t, name)
-    if t.dtype != dtype or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name} must be {dtype}" + ("" if shape is None else f" of shape {list(shape)}"))
-    return p
+    _dev(t, name)
+    raise ValueError(f"{name} must be {dtype}" + ("" if shape is None else f" of shape {list(shape)}"))
 
 
 try:  # the current stream's handle without a Stream object around it

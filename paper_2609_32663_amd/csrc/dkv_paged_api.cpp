@@ -172,8 +172,9 @@ dkv_status dkv_page_extend(int32_t num_units, int32_t num_kv_heads, int32_t page
     return DKV_ERR_INVALID_ARG;
   if (!page_rows_ok(page_rows)) return DKV_ERR_UNSUPPORTED;
   if ((int64_t)num_units * num_kv_heads > 65535) return DKV_ERR_UNSUPPORTED;
-  // one work-item per token and KV head
-  if ((int64_t)max_tokens * num_kv_heads > 0xFFFFFFFFLL - 255) return DKV_ERR_UNSUPPORTED;
+  // two work-items per token of the dispatch, slots counted in 32 bits
+  if (max_tokens > INT32_MAX - 127 || (int64_t)max_tokens * num_kv_heads > 0xFFFFFFFFLL - 255)
+    return DKV_ERR_UNSUPPORTED;
   if (n_free == nullptr || n_free_out == nullptr || tok_off == nullptr) return DKV_ERR_INVALID_ARG;
   if (num_units > 0 && (unit_new == nullptr || unit_len == nullptr || new_len == nullptr || first_pos == nullptr))
     return DKV_ERR_INVALID_ARG;

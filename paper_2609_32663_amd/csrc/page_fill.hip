@@ -9,15 +9,15 @@
 // elementwise: page i of the call is stack[top - 1 - i], token at position pos
 // of segment s has page pos / R, which is one of the call's pages when it
 // starts at or past ceil(len / R) * R and stands in the table otherwise, and
-// slot page * R + pos % R.  So the plan is two scans over the units by one
-// workgroup, and the fill takes one (token, head) per thread: no thread reads
-// what another one writes.  The call has next to no arithmetic; single tokens
-// are bound by the two launches' dependent round trips, prompts by writing
-// the slots.
+// slot page * R + pos % R.  No thread reads what another one writes, so the
+// call has two forms.  With few rows every workgroup sums all units and fills
+// 128 rows, in one launch: such calls are bound by the launch and a chain of
+// dependent reads.  With many rows one workgroup sums the units and a second
+// kernel fills, bound by writing the slots.
 //
 // Release.  The pages to go, in table order, are pushed on the stack: a count
 // per chunk of table words, then every chunk sums the counts before it and
-// places its own.
+// places its own.  One chunk needs no count.
 
 #include "dkv_device.hpp"
 #include "dkv_launch.hpp"
@@ -28,6 +28,32 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kFillThreads = 256;
+
+// Exclusive scan over a workgroup of NT threads, `tmp` NT / 64 words of LDS
+// that nothing else uses: a scan per wave, then every wave sums the waves
+// before it by itself.
+template <int NT>
+__device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t* tmp, int64_t* total) {
+  constexpr int NW = NT / kWave;
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  int64_t x = v;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int64_t y = __shfl_up(x, o, kWave);
+    if (lane >= o) x += y;
+  }
+  if (lane == kWave - 1) tmp[wave] = x;
+  __syncthreads();
+  int64_t t = lane < NW ? tmp[lane] : 0;
+#pragma unroll
+  for (int o = 1; o < NW; o <<= 1) {
+    const int64_t y = __shfl_up(t, o, kWave);
+    if (lane >= o) t += y;
+  }
+  *total = __shfl(t, NW - 1, kWave);
+  const int64_t before = __shfl(t, wave > 0 ? wave - 1 : 0, kWave);
+  return x - v + (wave > 0 ? before : 0);
+}
 
 // ------------------------------------------------------------------- extend
 
@@ -57,20 +83,71 @@ __device__ __forceinline__ int64_t extend_need(const PageExtendParams& p, const 
   return pages_of(grown, p.page_shift) - pages_of(u.len, p.page_shift);
 }
 
+// The new rows of one unit: where they start, the positions held before them,
+// their number and the unit's first page of the call (-1: not served).
+struct ExtendRows {
+  int32_t n, first, len, add, base;
+};
+
+__device__ __forceinline__ void extend_slot(const PageExtendParams& p, const ExtendRows& u, int32_t top, int32_t row,
+                                            int g, int64_t* to) {
+  int64_t slot = -1;
+  if (u.base >= 0) {
+    const int sh = p.page_shift;
+    const int32_t grown = u.len + u.add;
+    const int32_t pos = u.len + (row - u.first);
+    const int32_t lpage = pos >> sh, in_page = pos & ((1 << sh) - 1);
+    const int32_t old = (int32_t)pages_of(u.len, sh);
+    const int64_t s = (int64_t)u.n * p.Hkv + g;
+    int32_t page;
+    if (lpage >= old) {
+      const int32_t per = (int32_t)pages_of(grown, sh) - old;
+      page = p.free_pages[top - 1 - (u.base + g * per + (lpage - old))];
+      if (in_page == 0) p.table[s * p.pages_per_seg + lpage] = page;
+    } else {
+      page = p.table[s * p.pages_per_seg + lpage];
+    }
+    if (page >= 0) slot = ((int64_t)page << sh) + in_page;
+    if (in_page == 0 || row == u.first) {
+      if (p.entries != nullptr && lpage < p.max_entries) {
+        const int64_t end = (int64_t)grown - ((int64_t)lpage << sh);
+        int32_t* e = p.entries + 4 * (s * p.max_entries + lpage);
+        *reinterpret_cast<int4*>(e) = int4{page, lpage, 0, (int32_t)(end < (1 << sh) ? end : (1 << sh))};
+      }
+      if (p.n_entries != nullptr && row == u.first) p.n_entries[s] = (int32_t)pages_of(grown, sh);
+    }
+  }
+  *to = slot;
+}
+
 // Thread t plans units [t * per, t * per + per): sums of its units' rows and
-// pages, a scan of each over the workgroup, and its units again.
+// pages, a scan of each over the workgroup, and its units again.  FILL: the
+// workgroup then fills rows [kBlockRows * block, + kBlockRows); only the first
+// one writes what the units share.
+constexpr int kBlockRows = 128;
+constexpr int kOneLaunchBlocks = 64;
+
+template <bool FILL>
 __global__ __launch_bounds__(kPlanThreads) void page_extend_plan_kernel(PageExtendParams p) {
-  __shared__ int64_t red[kPlanThreads / kWave + 1];
+  __shared__ int64_t red[2][kPlanThreads / kWave];
+  __shared__ int32_t given;  // pages handed out: those of the units before the first that finds too few
+  // FILL: the units of the workgroup's rows, each where its first row lies
+  __shared__ uint32_t head[kBlockRows / 32];
+  __shared__ ExtendRows unit[FILL ? kBlockRows : 1];
   const int tid = threadIdx.x;
   const int N = p.num_units;
   const int per = (N + kPlanThreads - 1) / kPlanThreads;
   const int lo = min(N, tid * per), hi = min(N, lo + per);
+  const bool writes = blockIdx.x == 0;
+  const int64_t row_lo = (int64_t)blockIdx.x * kBlockRows;
   const int32_t height = *p.n_free;
-  const int64_t top = height < 0 ? 0 : (height > p.free_cap ? p.free_cap : height);
+  const int32_t top = height < 0 ? 0 : (height > p.free_cap ? p.free_cap : height);
+  if (tid == 0) given = 0;
+  if (tid < kBlockRows / 32) head[tid] = 0;
   int64_t rows = 0;
   for (int n = lo; n < hi; ++n) rows += extend_unit(p, n).rows;
   int64_t all_rows;
-  const int64_t row0 = block_exclusive_scan<kPlanThreads>(rows, red, &all_rows);
+  const int64_t row0 = plan_scan<kPlanThreads>(rows, red[0], &all_rows);
   int64_t row = row0, pages = 0;
   for (int n = lo; n < hi; ++n) {
     const ExtendUnit u = extend_unit(p, n);
@@ -78,8 +155,7 @@ __global__ __launch_bounds__(kPlanThreads) void page_extend_plan_kernel(PageExte
     if (need > 0) pages += need * p.Hkv;
   }
   int64_t all_pages;
-  int64_t base = block_exclusive_scan<kPlanThreads>(pages, red, &all_pages);
-  int64_t given = 0;
+  int64_t base = plan_scan<kPlanThreads>(pages, red[1], &all_pages);
   row = row0;
   for (int n = lo; n < hi; ++n) {
     const ExtendUnit u = extend_unit(p, n);
@@ -88,27 +164,50 @@ __global__ __launch_bounds__(kPlanThreads) void page_extend_plan_kernel(PageExte
     const int64_t need = extend_need(p, u, row);
     const int64_t all = need > 0 ? need * p.Hkv : 0;
     const bool served = need == 0 || (need > 0 && base + all <= top);
-    p.tok_off[n] = (int32_t)(first < p.max_tokens ? first : p.max_tokens);
-    p.first_pos[n] = served ? u.len : -1;
-    p.base[n] = served ? (int32_t)(base < top ? base : top) : -1;
-    p.new_len[n] = served ? u.len + u.add : u.len;
-    if (served) given += all;
+    const int32_t at = served ? (int32_t)(base < top ? base : top) : -1;
+    if (writes) {
+      p.tok_off[n] = (int32_t)(first < p.max_tokens ? first : p.max_tokens);
+      p.first_pos[n] = served ? u.len : -1;
+      p.new_len[n] = served ? u.len + u.add : u.len;
+      if (!FILL) p.base[n] = at;
+      if (served && all > 0) atomicMax(&given, (int32_t)(base + all));
+    }
+    if (FILL && u.rows > 0 && first < row_lo + kBlockRows && row > row_lo) {
+      const int i = (int)(first > row_lo ? first - row_lo : 0);
+      atomicOr(&head[i >> 5], 1u << (i & 31));
+      unit[i] = ExtendRows{n, (int32_t)first, u.len, u.add, at};
+    }
     base += all;
   }
-  int64_t all_given;
-  block_exclusive_scan<kPlanThreads>(given, red, &all_given);
-  if (tid == 0) {
+  __syncthreads();
+  if (writes && tid == 0) {
     p.tok_off[N] = (int32_t)(all_rows < p.max_tokens ? all_rows : p.max_tokens);
-    p.top[0] = (int32_t)top;
-    p.n_free_out[0] = (int32_t)(top - all_given);
+    if (!FILL) p.top[0] = top;
+    p.n_free_out[0] = top - given;
     if (p.pages_needed != nullptr) p.pages_needed[0] = all_pages;
+  }
+  if constexpr (FILL) {
+    const int slots = (int)min((int64_t)kBlockRows, p.max_tokens - row_lo) * p.Hkv;
+    for (int i = tid; i < slots; i += kPlanThreads) {
+      const int r = (int)((uint32_t)i / (uint32_t)p.Hkv);
+      const int g = i - r * p.Hkv;
+      int64_t* to = p.slots + (row_lo * p.Hkv + i);
+      // the last unit that starts at or before the row, if the row is one of its
+      int w = r >> 5;
+      uint32_t m = head[w] & (0xFFFFFFFFu >> (31 - (r & 31)));
+      while (m == 0 && w > 0) m = head[--w];
+      if (m == 0 || row_lo + r >= all_rows) {
+        *to = -1;
+      } else {
+        extend_slot(p, unit[32 * w + 31 - __clz(m)], top, (int32_t)row_lo + r, g, to);
+      }
+    }
   }
 }
 
 // Number of offsets off[1 .. n] that are <= row, i.e. the unit of a row below
 // off[n] (units without rows are stepped over).
-__device__ __forceinline__ int unit_of(const int32_t* off, int n, int32_t row) {
-  int lo = 0, hi = n;
+__device__ __forceinline__ int unit_of(const int32_t* off, int lo, int hi, int32_t row) {
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
     if (off[mid + 1] <= row) lo = mid + 1;
@@ -117,43 +216,56 @@ __device__ __forceinline__ int unit_of(const int32_t* off, int n, int32_t row) {
   return lo;
 }
 
+// unit_of by a wave: 64 offsets at a time.
+__device__ __forceinline__ int wave_unit_of(const int32_t* off, int n, int32_t row) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int lo = 0, hi = n;  // the answer is in [lo, hi]
+  while (lo < hi) {
+    const int step = (hi - lo + kWave - 1) / kWave;
+    const int64_t at = lo + (int64_t)(lane + 1) * step;  // offsets off[lo + step], ...
+    const bool below = at <= hi && off[at] <= row;
+    const int k = __popcll(__builtin_amdgcn_ballot_w64(below));
+    lo += k * step;
+    hi = min(hi, lo + step - 1);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Rows [kFillRows * block, + kFillRows) of the slots; most blocks of a prompt's
+// rows lie in one unit.
+constexpr int kFillRows = 128;
+
 __global__ __launch_bounds__(kFillThreads) void page_extend_fill_kernel(PageExtendParams p) {
-  const int64_t i = (int64_t)blockIdx.x * kFillThreads + threadIdx.x;
-  if (i >= (int64_t)p.max_tokens * p.Hkv) return;
-  const int32_t row = (int32_t)(i / p.Hkv);
-  const int g = (int)(i - (int64_t)row * p.Hkv);
-  int64_t slot = -1;
-  if (row < p.tok_off[p.num_units]) {
-    const int n = unit_of(p.tok_off, p.num_units, row);
-    const int32_t len = p.first_pos[n];
-    if (len >= 0) {
-      const int sh = p.page_shift;
-      const int32_t first_row = p.tok_off[n];
-      const int32_t grown = len + (p.tok_off[n + 1] - first_row);
-      const int32_t pos = len + (row - first_row);
-      const int32_t lpage = pos >> sh, in_page = pos & ((1 << sh) - 1);
-      const int32_t old = (int32_t)pages_of(len, sh);
-      const int64_t s = (int64_t)n * p.Hkv + g;
-      int32_t page;
-      if (lpage >= old) {
-        const int32_t per = (int32_t)pages_of(grown, sh) - old;
-        page = p.free_pages[p.top[0] - 1 - (p.base[n] + g * per + (lpage - old))];
-        if (in_page == 0) p.table[s * p.pages_per_seg + lpage] = page;
-      } else {
-        page = p.table[s * p.pages_per_seg + lpage];
-      }
-      if (page >= 0) slot = ((int64_t)page << sh) + in_page;
-      if (in_page == 0 || row == first_row) {
-        if (p.entries != nullptr && lpage < p.max_entries) {
-          const int64_t end = (int64_t)grown - ((int64_t)lpage << sh);
-          int32_t* e = p.entries + 4 * (s * p.max_entries + lpage);
-          *reinterpret_cast<int4*>(e) = int4{page, lpage, 0, (int32_t)(end < (1 << sh) ? end : (1 << sh))};
-        }
-        if (p.n_entries != nullptr && row == first_row) p.n_entries[s] = (int32_t)pages_of(grown, sh);
-      }
+  const int32_t total = p.tok_off[p.num_units];
+  const int32_t top = p.top[0];
+  const int64_t row_lo = (int64_t)blockIdx.x * kFillRows;
+  const int rows = (int)min((int64_t)kFillRows, p.max_tokens - row_lo);
+  const int slots = rows * p.Hkv;
+  int64_t* to = p.slots + row_lo * p.Hkv;
+  const int32_t r0 = (int32_t)row_lo;
+  if (r0 >= total) {
+    for (int i = threadIdx.x; i < slots; i += kFillThreads) to[i] = -1;
+    return;
+  }
+  const int32_t r_last = min(r0 + rows, total) - 1;
+  const int u0 = wave_unit_of(p.tok_off, p.num_units, r0);
+  const int32_t off0 = p.tok_off[u0], off1 = p.tok_off[u0 + 1];
+  const ExtendRows one{u0, off0, p.first_pos[u0], off1 - off0, p.base[u0]};
+  const int u1 = off1 > r_last ? u0 : wave_unit_of(p.tok_off, p.num_units, r_last);
+  for (int i = threadIdx.x; i < slots; i += kFillThreads) {
+    const int r = (int)((uint32_t)i / (uint32_t)p.Hkv);
+    const int g = i - r * p.Hkv;
+    const int32_t row = r0 + r;
+    if (row > r_last) {
+      to[i] = -1;
+    } else if (u0 == u1) {
+      extend_slot(p, one, top, row, g, to + i);
+    } else {
+      const int n = unit_of(p.tok_off, u0, u1, row);
+      const int32_t first = p.tok_off[n];
+      extend_slot(p, ExtendRows{n, first, p.first_pos[n], p.tok_off[n + 1] - first, p.base[n]}, top, row, g, to + i);
     }
   }
-  p.slots[i] = slot;
 }
 
 // ------------------------------------------------------------------ release
@@ -171,6 +283,11 @@ __device__ __forceinline__ bool released(const PageReleaseParams& p, int64_t i) 
   return p.table[i] >= 0 && (p.keep == nullptr || p.keep[i] == 0);
 }
 
+__device__ __forceinline__ int32_t release_top(const PageReleaseParams& p) {
+  const int32_t height = *p.n_free;
+  return height < 0 ? 0 : (height > p.free_cap ? p.free_cap : height);
+}
+
 __global__ __launch_bounds__(kReleaseThreads) void page_release_count_kernel(PageReleaseParams p, int64_t chunk) {
   __shared__ int64_t red[kReleaseThreads / kWave + 1];
   const int64_t lo = blockIdx.x * chunk, hi = lo + chunk < p.words ? lo + chunk : p.words;
@@ -180,20 +297,21 @@ __global__ __launch_bounds__(kReleaseThreads) void page_release_count_kernel(Pag
   block_exclusive_scan<kReleaseThreads>(n, red, &all);
   if (threadIdx.x == 0) {
     p.counts[blockIdx.x] = (int32_t)all;
-    if (blockIdx.x == 0) {
-      const int32_t height = *p.n_free;
-      p.top[0] = height < 0 ? 0 : (height > p.free_cap ? p.free_cap : height);
-    }
+    if (blockIdx.x == 0) p.top[0] = release_top(p);
   }
 }
 
 __global__ __launch_bounds__(kReleaseThreads) void page_release_push_kernel(PageReleaseParams p, int64_t chunk) {
   __shared__ int64_t red[kReleaseThreads / kWave + 1];
   const int tid = threadIdx.x;
-  int64_t before = 0, at;
-  for (int c = tid; c < (int)blockIdx.x; c += kReleaseThreads) before += p.counts[c];
-  block_exclusive_scan<kReleaseThreads>(before, red, &at);
-  at += p.top[0];
+  int64_t before = 0, at = 0;
+  if (gridDim.x > 1) {
+    for (int c = tid; c < (int)blockIdx.x; c += kReleaseThreads) before += p.counts[c];
+    block_exclusive_scan<kReleaseThreads>(before, red, &at);
+    at += p.top[0];
+  } else {
+    at = release_top(p);
+  }
   const int64_t lo = blockIdx.x * chunk, hi = lo + chunk < p.words ? lo + chunk : p.words;
   for (int64_t i0 = lo; i0 < hi; i0 += kReleaseThreads) {
     const int64_t i = i0 + tid;
@@ -237,11 +355,17 @@ __global__ __launch_bounds__(kFillThreads) void paged_append_kernel(PagedAppendP
 size_t page_extend_workspace_bytes(int64_t num_units) { return (size_t)(num_units + 1) * sizeof(int32_t); }
 
 hipError_t launch_page_extend(const PageExtendParams& p, hipStream_t stream) {
-  hipLaunchKernelGGL(page_extend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p);
-  const int64_t n = (int64_t)p.max_tokens * p.Hkv;
-  if (n > 0)
-    hipLaunchKernelGGL(page_extend_fill_kernel, dim3((unsigned)((n + kFillThreads - 1) / kFillThreads)),
-                       dim3(kFillThreads), 0, stream, p);
+  // One launch: every workgroup reads all the lengths, so with more than one
+  // of them the outputs must be other buffers.
+  const int64_t blocks = p.max_tokens > kBlockRows ? ((int64_t)p.max_tokens + kBlockRows - 1) / kBlockRows : 1;
+  const bool apart = p.new_len != p.unit_len && p.n_free_out != p.n_free;
+  if (blocks == 1 || (apart && blocks <= kOneLaunchBlocks)) {
+    hipLaunchKernelGGL(page_extend_plan_kernel<true>, dim3((unsigned)blocks), dim3(kPlanThreads), 0, stream, p);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(page_extend_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, stream, p);
+  hipLaunchKernelGGL(page_extend_fill_kernel, dim3((unsigned)(((int64_t)p.max_tokens + kFillRows - 1) / kFillRows)),
+                     dim3(kFillThreads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -253,7 +377,8 @@ size_t page_release_workspace_bytes(int64_t words) {
 hipError_t launch_page_release(const PageReleaseParams& p, hipStream_t stream) {
   const int64_t chunk = release_chunk(p.words);
   const unsigned chunks = p.words > 0 ? (unsigned)((p.words + chunk - 1) / chunk) : 1u;
-  hipLaunchKernelGGL(page_release_count_kernel, dim3(chunks), dim3(kReleaseThreads), 0, stream, p, chunk);
+  if (chunks > 1)
+    hipLaunchKernelGGL(page_release_count_kernel, dim3(chunks), dim3(kReleaseThreads), 0, stream, p, chunk);
   hipLaunchKernelGGL(page_release_push_kernel, dim3(chunks), dim3(kReleaseThreads), 0, stream, p, chunk);
   return hipGetLastError();
 }

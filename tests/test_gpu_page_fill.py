@@ -120,8 +120,9 @@ def test_extend_without_units_and_without_tokens(d):
     Extend(d, [0, 0], [64, 3], np.array([3, 4]), table, 64, 2, 0).run().check(want)
 
 
-@pytest.mark.parametrize("R,long", [(32, 20000), (1024, 40000)])
-def test_extend_one_long_prompt_among_many_units(d, R, long):
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("R,long", [(32, 20000), (1024, 40000), (64, 1000), (128, 7900)])
+def test_extend_one_long_prompt_among_many_units(d, R, long, in_place):
     """Most rows belong to one unit; the others have none or one."""
     rng = np.random.default_rng(R)
     N, Hkv = 300, 4
@@ -129,7 +130,7 @@ def test_extend_one_long_prompt_among_many_units(d, R, long):
     new = (rng.uniform(size=N) < 0.5).astype(np.int64)
     length[177], new[177] = 0, long
     want = pf.page_extend(new, length, stack.tolist(), table, R, Hkv, int(new.sum()))
-    Extend(d, new, length, stack, table, R, Hkv, int(new.sum())).run().check(want)
+    Extend(d, new, length, stack, table, R, Hkv, int(new.sum()), in_place=in_place).run().check(want)
 
 
 @pytest.mark.parametrize("nseg,pps", [(1, 1), (3, 7), (64, 33), (5, 1024), (300, 100), (4100, 1030)])

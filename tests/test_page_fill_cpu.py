@@ -88,7 +88,8 @@ def test_extend_validation():
                 dict(length=NUL), dict(new_len=NUL), dict(free=NUL), dict(nf=NUL), dict(nfo=NUL), dict(table=NUL),
                 dict(off=NUL), dict(pos=NUL), dict(slots=NUL), dict(max_e=3)):
         assert call(**bad) == d.DKV_ERR_INVALID_ARG, bad
-    for bad in (dict(R=100), dict(R=16), dict(R=2048), dict(N=8192, Hkv=8, w_bytes=1 << 20), dict(Hkv=4, most=1 << 30)):
+    for bad in (dict(R=100), dict(R=16), dict(R=2048), dict(N=8192, Hkv=8, w_bytes=1 << 20), dict(Hkv=4, most=1 << 30),
+                dict(Hkv=1, most=(1 << 31) - 127)):
         assert call(**bad) == d.DKV_ERR_UNSUPPORTED, bad
     assert call(ent=MIS, max_e=3) == d.DKV_ERR_MISALIGNED
     assert call(slots=ODD) == d.DKV_ERR_MISALIGNED
