@@ -14,6 +14,7 @@ constexpr float kLazy = 8.f;  // log2 headroom of the lazy running max
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t q_rsrc(const char* base, uint32_t bytes) {
@@ -84,6 +85,13 @@ __device__ __forceinline__ PagedBlock paged_block(const QueryParams& p, int b) {
   return k;
 }
 
+// The same for a uniform b, in scalar registers.
+__device__ __forceinline__ PagedBlock paged_block_uniform(const QueryParams& p, int b) {
+  const PagedBlock k = paged_block(p, b);
+  return PagedBlock{__builtin_amdgcn_readfirstlane(k.tok0), __builtin_amdgcn_readfirstlane(k.n),
+                    __builtin_amdgcn_readfirstlane(k.pos0)};
+}
+
 // Position of token t of a block (positions stop below the largest int32).
 __device__ __forceinline__ int32_t paged_pos(const PagedBlock& k, int32_t t) {
   return k.pos0 > INT32_MAX - 1 - t ? INT32_MAX - 1 : k.pos0 + t;
@@ -100,58 +108,52 @@ __device__ __forceinline__ int32_t paged_entries(const QueryParams& p, int s, in
   return all;
 }
 
-// 64 consecutive entries of a segment in a wave's registers, one per lane; an
-// entry that names a page outside the pool or slots outside a page is empty.
-struct PagedEntries {
-  int32_t page, lpage, lohi;  // lohi: lo | hi << 16
-  int32_t base;               // first entry held (uniform)
-
-  __device__ __forceinline__ void load(const QueryParams& p, int s, int32_t n, int32_t first) {
-    base = first;
-    const int32_t e = first + (int)(threadIdx.x & (kWave - 1));
-    page = lpage = lohi = 0;
-    if (e < n) {
-      const int4 x = *reinterpret_cast<const int4*>(p.entries + 4 * ((int64_t)s * p.max_entries + e));
-      const int32_t rows = 1 << p.page_shift;
-      if (x.x >= 0 && x.x < p.num_pages && x.y >= 0 && x.y <= (INT32_MAX - 1) >> p.page_shift && x.z >= 0 &&
-          x.z < x.w && x.w <= rows) {
-        page = x.x;
-        lpage = x.y;
-        lohi = x.z | x.w << 16;
-      }
-    }
-  }
-};
-
 // A run of 32 rows: the pool row and the position of its first slot, and the
-// slots [lo, hi) of it that hold keys of the segment (none: lo = hi = 0).
+// slots [lo, hi) of it that hold keys of the segment (none: lo = hi = 0).  All
+// uniform, so that it stays in scalar registers.
 struct PagedRun {
   int64_t row;
-  int32_t pos, lo, hi;
+  int32_t pos, lohi;  // lo | hi << 8
+
+  __device__ __forceinline__ int32_t lo() const { return lohi & 0xFF; }
+  __device__ __forceinline__ int32_t hi() const { return lohi >> 8; }
 };
 
-// The run at row r of the segment's row space (uniform, a multiple of 32), with
-// rows from `end` on and positions from `stop` on left out.  `held` moves on
-// when r passes it.
-__device__ __forceinline__ PagedRun paged_run(const QueryParams& p, PagedEntries& held, int s, int32_t n, int32_t r,
-                                              int32_t end, int32_t stop) {
-  PagedRun u{0, 0, 0, 0};
-  if (r >= end) return u;
-  const int32_t e = r >> p.page_shift;
-  if (e - held.base >= kWave) held.load(p, s, n, e);
-  const int li = e - held.base;
-  const int32_t slot = r & ((1 << p.page_shift) - 1);
-  const int32_t lohi = __builtin_amdgcn_readlane(held.lohi, li);
-  u.row = ((int64_t)__builtin_amdgcn_readlane(held.page, li) << p.page_shift) + slot;
-  u.pos = (__builtin_amdgcn_readlane(held.lpage, li) << p.page_shift) + slot;
-  int32_t lo = (lohi & 0xFFFF) - slot, hi = (lohi >> 16) - slot;
-  if (stop - u.pos < hi) hi = stop - u.pos;
+// What a workgroup needs of a segment's entries: the entries (constant while
+// the kernel runs, so a uniform index reads them with scalar loads), their
+// number, and where its rows and positions end.
+struct PagedSegment {
+  const __attribute__((address_space(4))) i32x4* entries;
+  int32_t n, end, stop, shift, pages;
+};
+
+__device__ __forceinline__ PagedSegment paged_segment(const QueryParams& p, int s, int32_t n, int32_t end,
+                                                      int32_t stop) {
+  return PagedSegment{(const __attribute__((address_space(4))) i32x4*)(p.entries + 4 * (int64_t)s * p.max_entries), n, end,
+                      stop, p.page_shift, (int32_t)p.num_pages};
+}
+
+// The entry that holds row r (the last one for rows past them).
+__device__ __forceinline__ i32x4 paged_entry(const PagedSegment& g, int32_t r) {
+  const int32_t e = r >> g.shift;
+  return g.entries[e < g.n ? e : (g.n > 0 ? g.n - 1 : 0)];
+}
+
+// The run at row r (uniform, a multiple of 32) of entry x; empty past the end,
+// for slots past the last position and for an entry that names a page outside
+// the pool or slots outside a page.
+__device__ __forceinline__ PagedRun paged_run(const PagedSegment& g, const i32x4& x, int32_t r) {
+  const int32_t slot = r & ((1 << g.shift) - 1);
+  const bool ok = r < g.end && (uint32_t)x.x < (uint32_t)g.pages &&
+                  (uint32_t)x.y <= (uint32_t)(INT32_MAX - 1) >> g.shift && x.z >= 0 && x.w <= (1 << g.shift);
+  PagedRun u;
+  u.row = ok ? ((int64_t)x.x << g.shift) + slot : 0;
+  u.pos = ok ? (x.y << g.shift) + slot : 0;
+  int32_t lo = x.z - slot, hi = x.w - slot;
+  if (g.stop - u.pos < hi) hi = g.stop - u.pos;
   lo = lo < 0 ? 0 : lo;
   hi = hi > kRun ? kRun : hi;
-  if (lo < hi) {
-    u.lo = lo;
-    u.hi = hi;
-  }
+  u.lohi = ok && lo < hi ? lo | hi << 8 : 0;
   return u;
 }
 

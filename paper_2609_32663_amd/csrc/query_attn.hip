@@ -135,24 +135,31 @@ struct QueryItem {
   int32_t nent;
 };
 
-template <int D, bool PAGED>
-__device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem& item) {
+// kParts: bf16 parts of a probability.
+template <int D, bool PAGED, int kParts>
+__device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem& item, uint16_t* k0, uint16_t* k1,
+                                           uint16_t* v0, uint16_t* v1) {
   using C = QCfg<D>;
-  // two tile buffers per matrix (separate arrays: the compiler then tells the
-  // direct loads into one apart from the reads of the other)
-  __shared__ __align__(1024) uint16_t k0[kQKeys * D], k1[kQKeys * D];
-  __shared__ __align__(1024) uint16_t v0[kQKeys * D], v1[kQKeys * D];
-
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = tid >> 6;
   const int n16 = lane & 15;
   const int kg = lane >> 4;
 
-  const int s = item.s, qt = item.qt;
-  const int64_t t_lo = item.t_lo, t_hi = item.t_hi;
-  const PagedBlock blk = item.blk;
-  const int32_t nent = item.nent;
+  int s = item.s, qt = item.qt;
+  int64_t t_lo = item.t_lo, t_hi = item.t_hi;
+  PagedBlock blk = item.blk;
+  int32_t nent = item.nent;
+  if constexpr (PAGED) {  // uniform: pages are looked up with scalar loads and arithmetic
+    s = __builtin_amdgcn_readfirstlane(s);
+    qt = __builtin_amdgcn_readfirstlane(qt);
+    t_lo = q_uniform64(t_lo);
+    t_hi = q_uniform64(t_hi);
+    blk.tok0 = __builtin_amdgcn_readfirstlane(blk.tok0);
+    blk.n = __builtin_amdgcn_readfirstlane(blk.n);
+    blk.pos0 = __builtin_amdgcn_readfirstlane(blk.pos0);
+    nent = __builtin_amdgcn_readfirstlane(nent);
+  }
   const int rows = PAGED ? blk.n * p.G : p.rows;  // query rows of the segment
   const int bseq = s / p.Hkv;
   const int g = s - bseq * p.Hkv;
@@ -271,22 +278,24 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // Paged: the two 32-row runs of a tile lie in pages of their own, each with
   // a descriptor over its slots [lo, hi): slots outside them (and runs past
   // the range) read zeros.  A wave instruction stays within one run.  `run`
-  // holds the runs of tiles t (parity t % 2) for the masks; K of a tile is
-  // issued before V of it and before anything of the next, so `at` names the
-  // pool rows of the tile issued last.
+  // holds the runs of tile t (parity t % 2) from its K loads on.
   PagedRun run[2][2] = {};
-  PagedEntries held{0, 0, 0, 0};
-  const int32_t pos_stop = PAGED && blk.pos0 >= 0 ? paged_pos(blk, blk.n - 1) + 1 : 0;
+  PagedSegment seg{};
+  i32x4 next[2] = {};  // the entries of the tile that is loaded next
   if constexpr (PAGED) {
-    held.load(p, s, nent, (int32_t)(k_lo >> p.page_shift));
+    seg = paged_segment(p, s, nent, (int32_t)k_hi, blk.pos0 >= 0 ? paged_pos(blk, blk.n - 1) + 1 : 0);
     if (D == 64) {  // one instruction per wave: waves 4-7 fill the second run
       koff -= (uint32_t)((wave_u >> 2) * kRun * C::kRowBytes);
       voff -= (uint32_t)((wave_u >> 2) * kRun * C::kRowBytes);
     }
   }
+  auto fetch_entries = [&](int64_t kt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) next[h] = paged_entry(seg, (int32_t)kt + kRun * h);
+  };
   auto find_runs = [&](PagedRun (&u)[2], int64_t kt) __attribute__((always_inline)) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) u[h] = paged_run(p, held, s, nent, (int32_t)kt + kRun * h, (int32_t)k_hi, pos_stop);
+    for (int h = 0; h < 2; ++h) u[h] = paged_run(seg, next[h], (int32_t)kt + kRun * h);
   };
   auto issue_runs = [&](const void* pool, uint32_t off, const PagedRun (&u)[2], uint16_t* buf)
                         __attribute__((always_inline)) {
@@ -295,10 +304,10 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       const int mi = i * (kQThreads / kWave) + wave_u;
       const bool second = D == 64 ? wave_u >= 4 : i == 1;
       const PagedRun& x = second ? u[1] : u[0];
-      const __amdgpu_buffer_rsrc_t rs = q_rsrc(static_cast<const char*>(pool) + (x.row + x.lo) * C::kRowBytes,
-                                               (uint32_t)(x.hi - x.lo) * C::kRowBytes);
+      const __amdgpu_buffer_rsrc_t rs = q_rsrc(static_cast<const char*>(pool) + (x.row + x.lo()) * C::kRowBytes,
+                                               (uint32_t)(x.hi() - x.lo()) * C::kRowBytes);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(buf + 512 * mi), 16,
-                                               off - (uint32_t)(x.lo * C::kRowBytes), 0, 0, 0);
+                                               off - (uint32_t)(x.lo() * C::kRowBytes), 0, 0, 0);
     }
   };
   auto issue = [&](const char* base, uint32_t off, int64_t kt, uint16_t* buf) __attribute__((always_inline)) {
@@ -358,17 +367,17 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   auto softmax = [&](auto masked, float (&sc)[kRG][2][4], int64_t kh, const PagedRun& u) __attribute__((always_inline)) {
     if constexpr (PAGED) {
       // slots outside the entry, or past the position of one of the wave's rows
-      if (u.lo > 0 || u.hi < kRun || u.pos + kRun > pos_all) {
+      if (u.lohi != kRun << 8 || u.pos + kRun > pos_all) {
         asm volatile("");  // keeps this a branch: the selects would run for every half
 #pragma unroll
         for (int q = 0; q < kRG; ++q) {
-          const int32_t lim = cut[q] - u.pos < u.hi ? cut[q] - u.pos : u.hi;
+          const int32_t lim = cut[q] - u.pos < u.hi() ? cut[q] - u.pos : u.hi();
 #pragma unroll
           for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               const int key = 16 * jj + 4 * kg + v;
-              if (key >= lim || key < u.lo) sc[q][jj][v] = -INFINITY;
+              if (key >= lim || key < u.lo()) sc[q][jj][v] = -INFINITY;
             }
         }
       }
@@ -424,15 +433,17 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // Probabilities of a half as the A operand of P V: K slot e of lane group
   // kg is key 4kg + e (e < 4) or 16 + 4kg + (e - 4) of the half, the lane's
   // scores of its two 16-key blocks; high part and remainder.
-  auto split = [&](const float (&sc)[kRG][2][4], u32x4 (&ph)[kRG], u32x4 (&pl)[kRG]) __attribute__((always_inline)) {
+  auto split = [&](const float (&sc)[kRG][2][4], u32x4 (&pp)[kParts][kRG]) __attribute__((always_inline)) {
 #pragma unroll
     for (int q = 0; q < kRG; ++q)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        uint32_t x, y;
-        bf16_split(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y);
-        ph[q][e] = x;
-        pl[q][e] = y;
+        uint32_t x, y, z = 0;
+        if constexpr (kParts == 3) bf16_split3(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y, z);
+        else bf16_split(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y);
+        pp[0][q][e] = x;
+        pp[1][q][e] = y;
+        if constexpr (kParts == 3) pp[2][q][e] = z;
       }
   };
 
@@ -443,8 +454,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // ((4h + kg / 2) * kRowChunks / 2 + b) * 16 + (4 (kg % 2) + r) * 2 + q / 2.
   // Two V blocks at a time: the high parts of both, then the remainders, so
   // a product never waits for the one just before it.
-  auto pv = [&](const uint16_t* vb, int h, const u32x4 (&ph)[kRG], const u32x4 (&pl)[kRG])
-                __attribute__((always_inline)) {
+  auto pv = [&](const uint16_t* vb, int h, const u32x4 (&pp)[kParts][kRG]) __attribute__((always_inline)) {
     const uint16_t* vr0 = &vb[8 * ((4 * h + (kg >> 1)) * (C::kRowChunks / 2) * 16 + (4 * (kg & 1) + (n16 >> 2)) * 2 +
                                    ((n16 >> 1) & 1)) + 4 * (n16 & 1)];
 #pragma unroll
@@ -461,20 +471,101 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
         vbo[bb] = u32x4{w0.x, w0.y, w1.x, w1.y};
       }
 #pragma unroll
-      for (int part = 0; part < 2; ++part)
+      for (int part = 0; part < kParts; ++part)
 #pragma unroll
         for (int bb = 0; bb < 2; ++bb)
 #pragma unroll
           for (int q = 0; q < kRG; ++q) {
             const int b = b0 + bb;
             f32x4 c = {o[q][b][0], o[q][b][1], o[q][b][2], o[q][b][3]};
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, part ? pl[q] : ph[q]),
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pp[part][q]),
                                                         __builtin_bit_cast(bf16x8, vbo[bb]), c, 0, 0, 0);
             o[q][b][0] = c[0];
             o[q][b][1] = c[1];
             o[q][b][2] = c[2];
             o[q][b][3] = c[3];
           }
+    }
+  };
+
+  // Paged: the products of a phase as one pipeline, every LDS read two groups
+  // of products ahead of its use, so that the matrix unit does not wait for
+  // one: O += P V of half hv (two V blocks at a time), then the scores of half
+  // hk of the tile in kb.  The fences keep the compiler from gathering the
+  // reads in front of their uses again.
+  auto products = [&](const uint16_t* kb, int hk, const uint16_t* vb, int hv, bool do_pv, bool do_qk,
+                      const u32x4 (&pp)[kParts][kRG], float (&sc)[kRG][2][4]) __attribute__((always_inline)) {
+    constexpr int NP = C::kBlocks / 2;  // pairs of V blocks
+    const uint16_t* vr0 = &vb[8 * ((4 * hv + (kg >> 1)) * (C::kRowChunks / 2) * 16 + (4 * (kg & 1) + (n16 >> 2)) * 2 +
+                                   ((n16 >> 1) & 1)) + 4 * (n16 & 1)];
+    auto read_v = [&](int b) __attribute__((always_inline)) {
+      const uint2 w0 = __builtin_bit_cast(
+          uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vr0 + 8 * 16 * b)));
+      const uint2 w1 = __builtin_bit_cast(
+          uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vr0 + 8 * 16 * (2 * (C::kRowChunks / 2) + b))));
+      return u32x4{w0.x, w0.y, w1.x, w1.y};
+    };
+    auto read_k = [&](int jj, int u) __attribute__((always_inline)) {
+      return *reinterpret_cast<const u32x4*>(&kb[8 * (lane + 16 * ((2 * hk + jj) * C::kRowChunks + 4 * u))]);
+    };
+    u32x4 vf[2][2], kf[C::kChunks][2];
+    if (do_pv) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) vf[n][0] = read_v(2 * n), vf[n][1] = read_v(2 * n + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+            for (int q = 0; q < kRG; ++q) {
+              const int b = 2 * n + bb;
+              f32x4 c = {o[q][b][0], o[q][b][1], o[q][b][2], o[q][b][3]};
+              c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pp[part][q]),
+                                                          __builtin_bit_cast(bf16x8, vf[n % 2][bb]), c, 0, 0, 0);
+              o[q][b][0] = c[0];
+              o[q][b][1] = c[1];
+              o[q][b][2] = c[2];
+              o[q][b][3] = c[3];
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        if (n + 2 < NP) {
+          vf[n % 2][0] = read_v(2 * n + 4), vf[n % 2][1] = read_v(2 * n + 5);
+        } else if (do_qk) {
+          kf[n + 2 - NP][0] = read_k(0, n + 2 - NP), kf[n + 2 - NP][1] = read_k(1, n + 2 - NP);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) kf[u][0] = read_k(0, u), kf[u][1] = read_k(1, u);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (do_qk) {
+#pragma unroll
+      for (int u = 2; u < C::kChunks; ++u) kf[u][0] = read_k(0, u), kf[u][1] = read_k(1, u);
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 acc[2][kRG];
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+        for (int q = 0; q < kRG; ++q) acc[jj][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < C::kChunks; ++u)
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+          for (int q = 0; q < kRG; ++q)
+            acc[jj][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[u][jj]),
+                                                                 __builtin_bit_cast(bf16x8, qb[q][u]), acc[jj][q], 0, 0, 0);
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+        for (int q = 0; q < kRG; ++q)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sc[q][jj][v] = acc[jj][q][v];
     }
   };
 
@@ -502,10 +593,14 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   uint16_t* const vbuf[2] = {v0, v1};
   const bool lead = __builtin_amdgcn_readfirstlane(wave < 4 ? 1 : 0) != 0;
   if constexpr (PAGED) {
-    find_runs(run[0], k_lo);
+    if (nent > 0) {
+      fetch_entries(k_lo);
+      find_runs(run[0], k_lo);
+      fetch_entries(k_lo + kQKeys);
+      find_runs(run[1], k_lo + kQKeys);
+    }
     issue_runs(p.k, koff, run[0], kbuf[0]);
     issue_runs(p.v, voff, run[0], vbuf[0]);
-    find_runs(run[1], k_lo + kQKeys);
     issue_runs(p.k, koff, run[1], kbuf[1]);
   } else {
     issue(kbase, koff, k_lo, kbuf[0]);
@@ -515,18 +610,25 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
   __syncthreads();
   float sc[kRG][2][4];
-  u32x4 ph[kRG], pl[kRG];
+  u32x4 pp[kParts][kRG];
   constexpr int kWaitOne = 0x0F70 | C::kDma;  // vmcnt(kDma): the younger of two tiles may still be in flight
   auto vphase = [&](auto masked, int64_t kh, const PagedRun& u) __attribute__((always_inline)) {
     softmax(masked, sc, kh, u);
-    split(sc, ph, pl);
+    split(sc, pp);
+    // entries on their way must not mix with the LDS reads of the next phase
+    if constexpr (PAGED) __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
   };
   // P V first: the probabilities are dead before the new scores are formed
   auto mphase = [&](const uint16_t* kb, int hk, const uint16_t* vb, int hv, bool do_pv) __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
-    if (do_pv) pv(vb, hv, ph, pl);
-    __builtin_amdgcn_sched_barrier(0);
-    qk(kb, hk, sc);
+    if constexpr (PAGED) {
+      if (do_pv) products(kb, hk, vb, hv, true, true, pp, sc);
+      else products(kb, hk, vb, hv, false, true, pp, sc);
+    } else {
+      if (do_pv) pv(vb, hv, pp);
+      __builtin_amdgcn_sched_barrier(0);
+      qk(kb, hk, sc);
+    }
     __builtin_amdgcn_s_setprio(0);
   };
   const int64_t ntile = k_hi > k_lo ? (k_hi - k_lo + kQKeys - 1) / kQKeys : 0;
@@ -556,11 +658,13 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       // 4t + 2: lead: P V of 2t, scores of 2t + 1; follow: vector phase of 2t
       if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
       else issue(vbase, voff, kt + kQKeys, vbuf[1 - i]);
+      if (PAGED && !L) fetch_entries(kt + 2 * kQKeys);
       if (L) mphase(kbuf[i], 1, vbuf[i], 0, true);
       else vphase(masked, kt, run[i][0]);
       meet();
       // 4t + 3: lead: vector phase of 2t + 1; follow: P V of 2t, scores of 2t + 1
       const PagedRun second = run[i][1];
+      if (PAGED && L) fetch_entries(kt + 2 * kQKeys);
       if (L) vphase(masked, kt + 32, second);
       else mphase(kbuf[i], 1, vbuf[i], 0, true);
       __builtin_amdgcn_s_waitcnt(kWaitOne);  // K of tile t + 1
@@ -582,11 +686,12 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     constexpr bool L = decltype(leadc)::value;
     if (L) mphase(kbuf[0], 0, vbuf[0], 0, false);  // scores of half 0
     meet();
-    for (int64_t rd = 0; rd < nclear; ++rd) tile_pair(std::false_type{}, leadc);
+    if constexpr (!PAGED)
+      for (int64_t rd = 0; rd < nclear; ++rd) tile_pair(std::false_type{}, leadc);
     for (int64_t rd = nclear; rd < nround; ++rd) tile_pair(std::true_type{}, leadc);
     // the follow group's P V products of the last half (tiles past k_hi hold
     // zeros and all their keys are masked, so the lead's last scores are unused)
-    if (!L && nround > 0) pv(vbuf[1], 1, ph, pl);
+    if (!L && nround > 0) pv(vbuf[1], 1, pp);
   };
   if (lead) walk(std::true_type{});
   else walk(std::false_type{});
@@ -625,8 +730,15 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   }
 }
 
+// Two tile buffers per matrix (separate arrays: the compiler then tells the
+// direct loads into one apart from the reads of the other).
+#define DKV_QUERY_TILES(D)                                          \
+  __shared__ __align__(1024) uint16_t k0[kQKeys * D], k1[kQKeys * D]; \
+  __shared__ __align__(1024) uint16_t v0[kQKeys * D], v1[kQKeys * D]
+
 template <int D>
 __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
+  DKV_QUERY_TILES(D);
   // ---- this workgroup's item: segment, query tile, key tiles ---------------
   int item, s, qt;
   bool single;             // the segment has one range: write the output
@@ -664,8 +776,8 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
     t_lo = (int64_t)r * tiles / nr;
     t_hi = (int64_t)(r + 1) * tiles / nr;
   }
-  query_item<D, false>(p, QueryItem{s, qt, t_lo, t_hi, single, p.rec + (int64_t)item * kQRows * QCfg<D>::kRec,
-                                    PagedBlock{0, 0, 0}, 0});
+  query_item<D, false, 2>(p, QueryItem{s, qt, t_lo, t_hi, single, p.rec + (int64_t)item * kQRows * QCfg<D>::kRec,
+                                       PagedBlock{0, 0, 0}, 0}, k0, k1, v0, v1);
 }
 
 // ---------------------------------------------------------------------------
@@ -779,38 +891,65 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
   }
 }
 
+// A probability is used as three bf16 parts, its 24 bits, where the query rows
+// see at most this many rows, and as two, 17 bits, beyond.  The kernel runs at
+// the rate that the matrix units reach under the power limit, so the third
+// product costs what it computes (512 tokens at 32K 354 us with two parts, 430
+// with three; 256 tokens over 45K rows 291 and 351).  Two parts err by 2.6e-6
+// of the output's norm at any length, three by 1.7e-7 at 1K keys and 1.0e-6 at
+// 32K; attention in plain fp32 by 2.8e-7 and 2.3e-6.
+constexpr int64_t kThreePartRows = 32768;
+
 template <int D>
 __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
-  if (p.plan == nullptr) {  // too few keys to split: one workgroup per (segment, query tile)
-    const int s = blockIdx.x / p.qtiles;
-    const int qt = blockIdx.x - s * p.qtiles;
-    const PagedBlock blk = paged_block(p, s / p.Hkv);
-    if ((int64_t)qt * kQRows >= (int64_t)blk.n * p.G) return;
-    const int32_t nent = __builtin_amdgcn_readfirstlane(unit_entries(p, blk, s, qt));
-    query_item<D, true>(p, QueryItem{s, qt, 0, unit_tiles(p, nent), true, nullptr, blk, nent});
-    return;
-  }
+  DKV_QUERY_TILES(D);
+  // Without a plan (too few keys to split) one workgroup per (segment, query
+  // tile): the loop's only unit.
+  const bool split = p.plan != nullptr;
   const PagedPlan plan = paged_plan_of(p.plan, p.max_items);
-  const int P = plan.slices[0], units = plan.slices[1];
-  const int64_t total = plan.total[0];
-  const int w = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;  // the grid is a multiple of 8
-  if (w >= P) return;
-  const int64_t lo = q_uniform64((int64_t)w * total / P), hi = q_uniform64((int64_t)(w + 1) * total / P);
-  int64_t end;
-  for (int u = plan.first[w]; u < units; ++u) {
-    const int64_t from = q_uniform64(plan.start[u]) + kUnitTiles;  // the unit's first key tile
-    end = q_uniform64(plan.start[u + 1]);
-    if (from - kUnitTiles >= hi) break;
-    const bool empty = from == end;  // no keys: zeros, by the slice that holds its start
-    const int64_t a = lo > from ? lo : from, b = hi < end ? hi : end;
-    if (empty ? from - kUnitTiles < lo : a >= b) continue;
-    const PagedUnit x = plan.unit[u];
-    const int s = __builtin_amdgcn_readfirstlane(x.s);
-    const int qt = __builtin_amdgcn_readfirstlane(x.qt);
-    const int32_t nent = __builtin_amdgcn_readfirstlane(x.nent);
-    float* rec = p.rec + (int64_t)(2 * w + (from > lo ? 1 : 0)) * kQRows * QCfg<D>::kRec;
-    query_item<D, true>(p, QueryItem{s, qt, a - from, b - from, empty || (a == from && b == end), rec,
-                                     paged_block(p, s / p.Hkv), nent});
+  int w = 0, u = 0, units = 1;
+  int64_t lo = 0, hi = 0;
+  if (split) {
+    const int P = __builtin_amdgcn_readfirstlane(plan.slices[0]);
+    const int64_t total = q_uniform64(plan.total[0]);
+    w = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;  // the grid is a multiple of 8
+    if (w >= P) return;
+    lo = q_uniform64((int64_t)w * total / P);
+    hi = q_uniform64((int64_t)(w + 1) * total / P);
+    u = __builtin_amdgcn_readfirstlane(plan.first[w]);
+    units = __builtin_amdgcn_readfirstlane(plan.slices[1]);
+  }
+  for (; u < units; ++u) {
+    QueryItem x;
+    if (split) {
+      const int64_t from = q_uniform64(plan.start[u]) + kUnitTiles;  // the unit's first key tile
+      const int64_t end = q_uniform64(plan.start[u + 1]);
+      if (from - kUnitTiles >= hi) break;
+      const bool empty = from == end;  // no keys: zeros, by the slice that holds its start
+      const int64_t a = lo > from ? lo : from, b = hi < end ? hi : end;
+      if (empty ? from - kUnitTiles < lo : a >= b) continue;
+      const PagedUnit unit = plan.unit[u];
+      x.s = __builtin_amdgcn_readfirstlane(unit.s);
+      x.qt = __builtin_amdgcn_readfirstlane(unit.qt);
+      x.nent = __builtin_amdgcn_readfirstlane(unit.nent);
+      x.blk = paged_block(p, x.s / p.Hkv);
+      x.t_lo = a - from;
+      x.t_hi = b - from;
+      x.single = empty || (a == from && b == end);
+      x.rec = p.rec + (int64_t)(2 * w + (from > lo ? 1 : 0)) * kQRows * QCfg<D>::kRec;
+    } else {
+      x.s = __builtin_amdgcn_readfirstlane(blockIdx.x / p.qtiles);
+      x.qt = blockIdx.x - x.s * p.qtiles;
+      x.blk = paged_block(p, x.s / p.Hkv);
+      if ((int64_t)x.qt * kQRows >= (int64_t)x.blk.n * p.G) return;
+      x.nent = __builtin_amdgcn_readfirstlane(unit_entries(p, x.blk, x.s, x.qt));
+      x.t_lo = 0;
+      x.t_hi = unit_tiles(p, x.nent);
+      x.single = true;
+      x.rec = nullptr;
+    }
+    if ((int64_t)x.nent << p.page_shift <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1);
+    else query_item<D, true, 2>(p, x, k0, k1, v0, v1);
     __syncthreads();  // the tile buffers are free for the next unit
   }
 }

@@ -218,17 +218,15 @@ void query_short_kernel(QueryParams p) {
     // paged: the sequence's block, the entries held, and where the piece ends
     // in the segment's rows and positions
     PagedBlock blk{0, 0, 0};
-    PagedEntries held{0, 0, 0, 0};
-    int32_t nent = 0, row_lo = 0, row_hi = 0, pos_stop = 0, pos_all = 0;
+    PagedSegment seg{};
+    int32_t row_lo = 0, pos_all = 0;
     int rows = p.rows;
     if constexpr (PAGED) {
-      nent = (int32_t)q_uniform64((split ? seg_hi - seg_lo : bnd) >> (p.page_shift - 5));
       row_lo = (int32_t)q_uniform64(a * kUnit);
-      row_hi = (int32_t)q_uniform64(bnd * kUnit);
-      held.load(p, s, nent, row_lo >> p.page_shift);
-      blk = paged_block(p, bseq);
+      blk = paged_block_uniform(p, bseq);
       rows = blk.n * p.G;
-      pos_stop = paged_pos(blk, blk.n - 1) + 1;
+      seg = paged_segment(p, s, (int32_t)q_uniform64((split ? seg_hi - seg_lo : bnd) >> (p.page_shift - 5)),
+                          (int32_t)q_uniform64(bnd * kUnit), paged_pos(blk, blk.n - 1) + 1);
       pos_all = paged_pos(blk, min(16 * RG * rw, rows - 1) / p.G) + 1;  // the wave's first row's position, past it
     }
     PagedRun ring[S] = {};
@@ -249,10 +247,11 @@ void query_short_kernel(QueryParams p) {
       int64_t from = nk > 0 ? t * kSKeys * C::kRowBytes : 0;
       uint32_t skip = 0;
       if constexpr (PAGED) {
-        run = paged_run(p, held, s, nent, row_lo + (int32_t)t * kSKeys, row_hi, pos_stop);
-        nk = (uint32_t)(run.hi - run.lo);
-        from = (run.row + run.lo) * C::kRowBytes;
-        skip = (uint32_t)(run.lo * C::kRowBytes);
+        const int32_t r = row_lo + (int32_t)t * kSKeys;
+        run = paged_run(seg, paged_entry(seg, r), r);
+        nk = (uint32_t)(run.hi() - run.lo());
+        from = (run.row + run.lo()) * C::kRowBytes;
+        skip = (uint32_t)(run.lo() * C::kRowBytes);
       }
       const __amdgpu_buffer_rsrc_t ks = q_rsrc(kbase + from, nk * C::kRowBytes);
       const __amdgpu_buffer_rsrc_t vs = q_rsrc(vbase + from, nk * C::kRowBytes);
@@ -342,18 +341,18 @@ void query_short_kernel(QueryParams p) {
       const int64_t key0 = t * kSKeys;
       if constexpr (PAGED) {
         // slots outside the entry, or past the position of one of the wave's rows
-        if (run.lo > 0 || run.hi < kRun || run.pos + kRun > pos_all) {
+        if (run.lohi != kRun << 8 || run.pos + kRun > pos_all) {
           asm volatile("");
 #pragma unroll
           for (int q = 0; q < RG; ++q) {
             const int32_t rel = (int32_t)cut[q] - run.pos;
-            const int32_t lim = rel < run.hi ? rel : run.hi;
+            const int32_t lim = rel < run.hi() ? rel : run.hi();
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
               for (int v = 0; v < 4; ++v) {
                 const int key = 16 * j + 4 * kg + v;
-                if (key >= lim || key < run.lo) sc[q][j][v] = -INFINITY;
+                if (key >= lim || key < run.lo()) sc[q][j][v] = -INFINITY;
               }
           }
         }
