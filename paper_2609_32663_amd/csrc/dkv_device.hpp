@@ -104,6 +104,32 @@ __device__ __forceinline__ int64_t block_exclusive_scan(int64_t v, int64_t* tmp,
   return excl;
 }
 
+// Exclusive scan over a workgroup of NT threads, `tmp` NT / 64 words of LDS
+// that nothing else uses: a scan per wave, then every wave sums the waves
+// before it by itself.
+template <int NT>
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* tmp, int64_t* total) {
+  constexpr int NW = NT / kWave;
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  int64_t x = v;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int64_t y = __shfl_up(x, o, kWave);
+    if (lane >= o) x += y;
+  }
+  if (lane == kWave - 1) tmp[wave] = x;
+  __syncthreads();
+  int64_t t = lane < NW ? tmp[lane] : 0;
+#pragma unroll
+  for (int o = 1; o < NW; o <<= 1) {
+    const int64_t y = __shfl_up(t, o, kWave);
+    if (lane >= o) t += y;
+  }
+  *total = __shfl(t, NW - 1, kWave);
+  const int64_t before = __shfl(t, wave > 0 ? wave - 1 : 0, kWave);
+  return x - v + (wave > 0 ? before : 0);
+}
+
 // Workgroup that owns flat row x when `total` rows are cut into P slices
 // [floor(w*total/P), floor((w+1)*total/P)).
 // The quotient comes from an fp64 division (the numerator is below 2^53) and

@@ -102,10 +102,10 @@ __device__ __forceinline__ int32_t paged_pos(const PagedBlock& k, int32_t t) {
 // behind it (as in an unpruned cache), the ones before that.
 __device__ __forceinline__ int32_t paged_entries(const QueryParams& p, int s, int32_t last) {
   const int32_t n = p.n_entries[s];
-  const int32_t all = n < 0 ? 0 : (n > p.max_entries ? p.max_entries : n);
   const int32_t x = (last >> p.page_shift) + 1;
-  if (x < all && p.entries[4 * ((int64_t)s * p.max_entries + x) + 1] > (last >> p.page_shift)) return x;
-  return all;
+  const int32_t page = x < p.max_entries ? p.entries[4 * ((int64_t)s * p.max_entries + x) + 1] : 0;  // read beside n
+  const int32_t all = n < 0 ? 0 : (n > p.max_entries ? p.max_entries : n);
+  return x < all && page > (last >> p.page_shift) ? x : all;
 }
 
 // A run of 32 rows: the pool row and the position of its first slot, and the

@@ -29,32 +29,6 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kFillThreads = 256;
 
-// Exclusive scan over a workgroup of NT threads, `tmp` NT / 64 words of LDS
-// that nothing else uses: a scan per wave, then every wave sums the waves
-// before it by itself.
-template <int NT>
-__device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t* tmp, int64_t* total) {
-  constexpr int NW = NT / kWave;
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  int64_t x = v;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int64_t y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
-  }
-  if (lane == kWave - 1) tmp[wave] = x;
-  __syncthreads();
-  int64_t t = lane < NW ? tmp[lane] : 0;
-#pragma unroll
-  for (int o = 1; o < NW; o <<= 1) {
-    const int64_t y = __shfl_up(t, o, kWave);
-    if (lane >= o) t += y;
-  }
-  *total = __shfl(t, NW - 1, kWave);
-  const int64_t before = __shfl(t, wave > 0 ? wave - 1 : 0, kWave);
-  return x - v + (wave > 0 ? before : 0);
-}
-
 // ------------------------------------------------------------------- extend
 
 struct ExtendUnit {
@@ -147,7 +121,7 @@ __global__ __launch_bounds__(kPlanThreads) void page_extend_plan_kernel(PageExte
   int64_t rows = 0;
   for (int n = lo; n < hi; ++n) rows += extend_unit(p, n).rows;
   int64_t all_rows;
-  const int64_t row0 = plan_scan<kPlanThreads>(rows, red[0], &all_rows);
+  const int64_t row0 = block_scan<kPlanThreads>(rows, red[0], &all_rows);
   int64_t row = row0, pages = 0;
   for (int n = lo; n < hi; ++n) {
     const ExtendUnit u = extend_unit(p, n);
@@ -155,7 +129,7 @@ __global__ __launch_bounds__(kPlanThreads) void page_extend_plan_kernel(PageExte
     if (need > 0) pages += need * p.Hkv;
   }
   int64_t all_pages;
-  int64_t base = plan_scan<kPlanThreads>(pages, red[1], &all_pages);
+  int64_t base = block_scan<kPlanThreads>(pages, red[1], &all_pages);
   row = row0;
   for (int n = lo; n < hi; ++n) {
     const ExtendUnit u = extend_unit(p, n);

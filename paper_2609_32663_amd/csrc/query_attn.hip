@@ -693,7 +693,29 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     // zeros and all their keys are masked, so the lead's last scores are unused)
     if (!L && nround > 0) pv(vbuf[1], 1, pp);
   };
-  if (lead) walk(std::true_type{});
+  // Paged: waves without rows (a sequence of few tokens) load and meet only;
+  // the others then have the matrix units and the power to themselves.
+  auto attend_none = [&]() __attribute__((always_inline)) {
+    meet();
+    for (int64_t rd = 0; rd < nround; ++rd) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        __builtin_amdgcn_s_waitcnt(kWaitOne);
+        meet();
+        issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
+        fetch_entries(kt + 2 * kQKeys);
+        meet();
+        __builtin_amdgcn_s_waitcnt(kWaitOne);
+        meet();
+        find_runs(run[i], kt + 2 * kQKeys);
+        issue_runs(p.k, koff, run[i], kbuf[i]);
+        meet();
+        kt += kQKeys;
+      }
+    }
+  };
+  if (PAGED && qt * kQRows + 16 * kRG * wave_u >= rows) attend_none();
+  else if (lead) walk(std::true_type{});
   else walk(std::false_type{});
   // no direct load may still be writing LDS when the workgroup ends
   __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -791,31 +813,57 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
 // and the head of the unit it ends in (2w + 1; a unit that starts with the
 // slice is in slot 2w), and a combine kernel folds a unit's records in slice
 // order.  Consecutive slices, which share keys, go to the same L2 domain.
+//
+// Prompts have many units, none longer than a slice.  There the plan deals the
+// units by falling length, P at a time, the longest of a round to the workgroup
+// with the least so far: when the longest share is at most kWholeTiles above
+// the mean, units stay whole and no record is written (two 4K prompts of an 8B
+// layer: 255 split units' records and their combine cost 35 us of 309).
 // ---------------------------------------------------------------------------
 constexpr int kUnitTiles = 2;
+constexpr int kWholeTiles = 10;
+constexpr int kSortBuckets = 1024;
 
 struct PagedUnit {
   int32_t s, qt, nent, pad;
 };
 
-// Words of the plan: the slice count, the units' total length, each slice's
-// first unit, each unit's start and what it is.
-struct PagedPlan {
-  int32_t* slices;      // [2]: P, spare
-  int64_t* total;
-  int32_t* first;       // [kPagedSlices + 1] unit that holds the slice's start
-  int64_t* start;       // [units + 1]
-  PagedUnit* unit;      // [units]
+// Words of the plan: slices and units, whether units stay whole, the units'
+// total length, each slice's first unit, the units that several slices share,
+// what each unit is, where it starts, and for whole units the workgroups' units,
+// round by round (-1: none).
+struct PagedShared {
+  int32_t slot, parts;  // slot of the first record, records (the others at slots 2w of the next slices)
+  int32_t s, qt, tok0, rows, pad[2];
 };
+
+struct PagedPlan {
+  int32_t* head;        // [4]: P, units, whole, shared units
+  int64_t* total;
+  int32_t* first;       // [kPagedSlices] unit that holds the slice's start
+  PagedShared* shared;  // [kPagedSlices]
+  PagedUnit* unit;      // [units]
+  int64_t* start;       // [units + 1]
+  int32_t* order;       // [units, rounded up to rounds of kPagedSlices]
+};
+
+constexpr int kPagedPlanHead = 8;  // words before `first`
 
 __host__ __device__ __forceinline__ PagedPlan paged_plan_of(int32_t* words, int64_t units) {
   PagedPlan x;
-  x.slices = words;
-  x.total = reinterpret_cast<int64_t*>(words + 2);
-  x.first = words + 4;
-  x.unit = reinterpret_cast<PagedUnit*>(words + 4 + kPagedSlices + 4);
+  x.head = words;
+  x.total = reinterpret_cast<int64_t*>(words + 4);
+  x.first = words + kPagedPlanHead;
+  x.shared = reinterpret_cast<PagedShared*>(x.first + kPagedSlices);
+  x.unit = reinterpret_cast<PagedUnit*>(x.shared + kPagedSlices);
   x.start = reinterpret_cast<int64_t*>(x.unit + units);
+  x.order = reinterpret_cast<int32_t*>(x.start + units + 1);
   return x;
+}
+
+size_t paged_plan_bytes(int64_t units) {
+  return (sizeof(int32_t) * (kPagedPlanHead + 2 * kPagedSlices + units) + sizeof(PagedShared) * kPagedSlices + sizeof(PagedUnit) * units +
+          sizeof(int64_t) * (units + 1) + 255) / 256 * 256;
 }
 
 __device__ __forceinline__ int64_t unit_tiles(const QueryParams& p, int32_t nent) {
@@ -829,9 +877,21 @@ __device__ __forceinline__ int32_t unit_entries(const QueryParams& p, const Page
   return paged_entries(p, s, paged_pos(k, (int32_t)((last - 1) / p.G)));
 }
 
+// One workgroup; bound by the chain of its dependent reads (offsets, counts)
+// and scans, so what later steps read again stays in LDS.
+constexpr int kPlanUnits = 4096;  // units whose starts fit LDS
+constexpr int kWholeRounds = 32;  // rounds of whole units at most
+
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p) {
-  __shared__ int64_t red[kPlanThreads / kWave + 1];
+  __shared__ int64_t red[3][kPlanThreads / kWave];
   __shared__ int32_t pre[DKV_MAX_SEGMENTS + 1];  // query tiles of the sequences before
+  __shared__ int32_t blk_n[DKV_MAX_SEGMENTS], blk_pos[DKV_MAX_SEGMENTS];
+  __shared__ int64_t start[kPlanUnits + 1];
+  __shared__ int32_t bucket[kSortBuckets];       // whole units: units per length, then where they go
+  __shared__ int32_t order[kPlanUnits];
+  __shared__ __align__(16) int32_t load[kPagedSlices];
+  static_assert(kPlanThreads == 4 * kPagedSlices, "four threads rank a workgroup's load");
+  __shared__ int32_t longest, share, nshared;
   const int tid = threadIdx.x;
   const int B = p.nseg / p.Hkv;
   const PagedPlan plan = paged_plan_of(p.plan, p.max_items);
@@ -839,16 +899,27 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
   for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
     const int b = b0 + tid;
     int64_t tiles = 0, sum;
-    if (b < B) tiles = ((int64_t)paged_block(p, b).n * p.G + kQRows - 1) / kQRows;
-    const int64_t ex = block_exclusive_scan<kPlanThreads>(tiles, red, &sum);
+    if (b < B) {
+      const PagedBlock k = paged_block(p, b);
+      blk_n[b] = k.n;
+      blk_pos[b] = k.pos0;
+      tiles = ((int64_t)k.n * p.G + kQRows - 1) / kQRows;
+    }
+    if (b0 > 0) __syncthreads();
+    const int64_t ex = block_scan<kPlanThreads>(tiles, red[0], &sum);
     if (b < B) pre[b] = (int32_t)(base + ex);
     base += sum;
   }
-  if (tid == 0) pre[B] = (int32_t)base;
+  if (tid == 0) {
+    pre[B] = (int32_t)base;
+    longest = share = nshared = 0;
+  }
   __syncthreads();
   // offsets that overlap could name more units than the workspace holds
   const int64_t units = base * p.Hkv < p.max_items ? base * p.Hkv : p.max_items;
+  const bool near = units <= kPlanUnits;
   int64_t len = 0;
+  int32_t most = 0;
   for (int64_t u0 = 0; u0 < units; u0 += kPlanThreads) {
     const int64_t u = u0 + tid;
     int64_t mine = 0, sum;
@@ -863,32 +934,109 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
       const int in = (int)(u - (int64_t)pre[lo] * p.Hkv);
       const int g = in / tiles, qt = in - g * tiles;
       const int s = lo * p.Hkv + g;
-      const int32_t nent = unit_entries(p, paged_block(p, lo), s, qt);
+      const int32_t nent = unit_entries(p, PagedBlock{0, blk_n[lo], blk_pos[lo]}, s, qt);
       plan.unit[u] = PagedUnit{s, qt, nent, 0};
-      mine = unit_tiles(p, nent) + kUnitTiles;
+      mine = unit_tiles(p, nent) + kUnitTiles;  // below 2^25
+      most = max(most, (int32_t)mine);
     }
-    const int64_t ex = block_exclusive_scan<kPlanThreads>(mine, red, &sum);
-    if (u < units) plan.start[u] = len + ex;
+    if (u0 > 0) __syncthreads();
+    const int64_t ex = block_scan<kPlanThreads>(mine, red[1], &sum);
+    if (u < units) {
+      plan.start[u] = len + ex;
+      if (near) start[u] = len + ex;
+    }
     len += sum;
   }
+  const int64_t P = len < p.P ? len : p.P;
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, kWave));
+  if ((tid & (kWave - 1)) == 0) atomicMax(&longest, most);
   if (tid == 0) {
     plan.start[units] = len;
-    plan.slices[0] = (int32_t)(len < p.P ? len : p.P);
-    plan.slices[1] = (int32_t)units;
+    if (near) start[units] = len;
+    plan.head[0] = (int32_t)P;
+    plan.head[1] = (int32_t)units;
     plan.total[0] = len;
   }
   __syncthreads();
-  const int64_t P = len < p.P ? len : p.P;
-  if (tid < P) {
+  bool whole = near && units > P && longest <= len / p.P && units <= (int64_t)kWholeRounds * p.P;
+  if (whole) {
+    const int rounds = (int)((units + p.P - 1) / p.P);
+    for (int i = tid; i < kSortBuckets; i += kPlanThreads) bucket[i] = 0;
+    if (tid < kPagedSlices) load[tid] = tid < p.P ? 0 : INT32_MAX;
+    __syncthreads();
+    // a counting sort
+    const float scale = (float)(kSortBuckets - 1) / (float)longest;
+    auto bucket_of = [&](int64_t u) {
+      const int b = (int)((float)(longest - (int32_t)(start[u + 1] - start[u])) * scale);
+      return b < kSortBuckets ? b : kSortBuckets - 1;
+    };
+    for (int u = tid; u < units; u += kPlanThreads) atomicAdd(&bucket[bucket_of(u)], 1);
+    __syncthreads();
+    int64_t sum;
+    const int64_t ex = block_scan<kPlanThreads>(tid < kSortBuckets ? bucket[tid] : 0, red[2], &sum);
+    if (tid < kSortBuckets) bucket[tid] = (int32_t)ex;
+    __syncthreads();
+    for (int u = tid; u < units; u += kPlanThreads) order[atomicAdd(&bucket[bucket_of(u)], 1)] = u;
+    __syncthreads();
+    const int mine_of = tid / 4;  // the workgroup that this thread ranks, with its three neighbours
+    for (int r = 0; r < rounds; ++r) {
+      const int32_t mine = load[mine_of];
+      // workgroups with less so far (or as much, and before this one): none in
+      // the first round, all behind it in the second
+      int rank = r == 0 ? mine_of : p.P - 1 - mine_of;
+      if (r > 1) {
+        rank = 0;
+#pragma unroll
+        for (int k = 0; k < kPagedSlices / 4; k += 4) {
+          const int j = (tid & 3) * (kPagedSlices / 4) + k;
+          const int4 x = *reinterpret_cast<const int4*>(&load[j]);
+          rank += (x.x < mine || (x.x == mine && j < mine_of)) + (x.y < mine || (x.y == mine && j + 1 < mine_of)) +
+                  (x.z < mine || (x.z == mine && j + 2 < mine_of)) + (x.w < mine || (x.w == mine && j + 3 < mine_of));
+        }
+        rank += __shfl_xor(rank, 1, kWave);
+        rank += __shfl_xor(rank, 2, kWave);
+      }
+      const int i = r * p.P + rank;
+      const int32_t unit = mine_of < p.P && i < units ? order[i] : -1;
+      __syncthreads();
+      if ((tid & 3) == 0 && mine_of < p.P) {
+        if (unit >= 0) load[mine_of] = mine + (int32_t)(start[unit + 1] - start[unit]);
+        plan.order[r * p.P + mine_of] = unit;
+      }
+      __syncthreads();
+    }
+    int32_t top = tid < p.P ? load[tid] : 0;
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, kWave));
+    if (tid < kPagedSlices && (tid & (kWave - 1)) == 0) atomicMax(&share, top);
+    __syncthreads();
+    whole = share <= len / p.P + kWholeTiles;
+  }
+  if (tid == 0) plan.head[2] = whole ? 1 : 0;
+  if (!whole && tid < P) {
     const int64_t x = (int64_t)tid * len / P;
     int64_t lo = 0, hi = units;
     while (hi - lo > 1) {
       const int64_t mid = (lo + hi) >> 1;
-      if (plan.start[mid] <= x) lo = mid;
+      if ((near ? start[mid] : plan.start[mid]) <= x) lo = mid;
       else hi = mid;
     }
     plan.first[tid] = (int32_t)lo;
+    // the unit that this slice continues, by the first slice to do so
+    const int64_t from = (near ? start[lo] : plan.start[lo]) + kUnitTiles;
+    const int64_t before = (int64_t)(tid - 1) * len / P;  // start of the slice before
+    if (tid > 0 && from < x && from >= before) {
+      const int64_t end = near ? start[lo + 1] : plan.start[lo + 1];
+      const int i = atomicAdd(&nshared, 1);
+      const PagedUnit u = plan.unit[lo];
+      const PagedBlock k = paged_block(p, u.s / p.Hkv);
+      plan.shared[i] = PagedShared{2 * (tid - 1) + (from > before ? 1 : 0), (int)owner_of(end - 1, len, P) - tid + 2,
+                                   u.s, u.qt, k.tok0, k.n * p.G, {0, 0}};
+    }
   }
+  __syncthreads();
+  if (tid == 0) plan.head[3] = nshared;
 }
 
 // A probability is used as three bf16 parts, its 24 bits, where the query rows
@@ -907,21 +1055,39 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
   // tile): the loop's only unit.
   const bool split = p.plan != nullptr;
   const PagedPlan plan = paged_plan_of(p.plan, p.max_items);
-  int w = 0, u = 0, units = 1;
+  int w = blockIdx.x, u = 0, units = 1;
   int64_t lo = 0, hi = 0;
+  bool whole = false;
   if (split) {
-    const int P = __builtin_amdgcn_readfirstlane(plan.slices[0]);
-    const int64_t total = q_uniform64(plan.total[0]);
-    w = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;  // the grid is a multiple of 8
-    if (w >= P) return;
-    lo = q_uniform64((int64_t)w * total / P);
-    hi = q_uniform64((int64_t)(w + 1) * total / P);
-    u = __builtin_amdgcn_readfirstlane(plan.first[w]);
-    units = __builtin_amdgcn_readfirstlane(plan.slices[1]);
+    units = __builtin_amdgcn_readfirstlane(plan.head[1]);
+    whole = __builtin_amdgcn_readfirstlane(plan.head[2]) != 0;
+    if (!whole) {
+      const int P = __builtin_amdgcn_readfirstlane(plan.head[0]);
+      const int64_t total = q_uniform64(plan.total[0]);
+      w = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;  // the grid is a multiple of 8
+      if (w >= P) return;
+      lo = q_uniform64((int64_t)w * total / P);
+      hi = q_uniform64((int64_t)(w + 1) * total / P);
+      u = __builtin_amdgcn_readfirstlane(plan.first[w]);
+    }
   }
-  for (; u < units; ++u) {
+  for (int r = 0;; ++r, ++u) {
     QueryItem x;
-    if (split) {
+    if (whole) {
+      if (r * (int)gridDim.x >= units) break;
+      const int v = __builtin_amdgcn_readfirstlane(plan.order[r * gridDim.x + w]);
+      if (v < 0) continue;
+      const PagedUnit unit = plan.unit[v];
+      x.s = unit.s;
+      x.qt = unit.qt;
+      x.nent = unit.nent;
+      x.blk = paged_block(p, unit.s / p.Hkv);
+      x.t_lo = 0;
+      x.t_hi = unit_tiles(p, unit.nent);
+      x.single = true;
+      x.rec = nullptr;
+    } else if (split) {
+      if (u >= units) break;
       const int64_t from = q_uniform64(plan.start[u]) + kUnitTiles;  // the unit's first key tile
       const int64_t end = q_uniform64(plan.start[u + 1]);
       if (from - kUnitTiles >= hi) break;
@@ -938,6 +1104,7 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.single = empty || (a == from && b == end);
       x.rec = p.rec + (int64_t)(2 * w + (from > lo ? 1 : 0)) * kQRows * QCfg<D>::kRec;
     } else {
+      if (r > 0) break;
       x.s = __builtin_amdgcn_readfirstlane(blockIdx.x / p.qtiles);
       x.qt = blockIdx.x - x.s * p.qtiles;
       x.blk = paged_block(p, x.s / p.Hkv);
@@ -948,7 +1115,8 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.single = true;
       x.rec = nullptr;
     }
-    if ((int64_t)x.nent << p.page_shift <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1);
+    const int64_t rows = (int64_t)__builtin_amdgcn_readfirstlane(x.nent) << p.page_shift;
+    if (rows <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1);
     else query_item<D, true, 2>(p, x, k0, k1, v0, v1);
     __syncthreads();  // the tile buffers are free for the next unit
   }
@@ -1023,28 +1191,26 @@ __global__ __launch_bounds__(kMergeThreads) void query_merge_kernel(QueryParams 
   *reinterpret_cast<f32x4*>(orow + 4 * c4) = A * inv;
 }
 
-// Combine kernel of paged calls: a unit that several slices share is folded by
-// the workgroups of the first of them.
+// Combine kernel of paged calls: kParts workgroups per unit that several slices
+// share, as the plan lists them.
 template <int D>
-__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(QueryParams p) {
+__global__ __launch_bounds__(kMergeThreads, 5) void paged_merge_kernel(QueryParams p) {
   using C = QCfg<D>;
   constexpr int kParts = kQRows * (D / 4) / kMergeThreads;
-  const int w = blockIdx.x / kParts;
+  const int i = blockIdx.x / kParts;
   const PagedPlan plan = paged_plan_of(p.plan, p.max_items);
-  const int64_t P = plan.slices[0], total = plan.total[0];
-  if (w + 1 >= P) return;
-  const int64_t lo = (int64_t)w * total / P, hi = (int64_t)(w + 1) * total / P;
-  const int u = plan.first[w + 1];  // holds hi
-  const int64_t from = plan.start[u] + kUnitTiles, end = plan.start[u + 1];
-  if (from < lo || from >= hi || end <= hi) return;  // starts in another slice, or ends with this one
-  const int nr = (int)owner_of(end - 1, total, P) - w + 1;
-  const PagedUnit x = plan.unit[u];
-  const PagedBlock blk = paged_block(p, x.s / p.Hkv);
-  const int it = (blockIdx.x - w * kParts) * kMergeThreads + threadIdx.x;
+  if (i >= plan.head[3]) return;
+  const PagedShared x = plan.shared[i];
+  const int nr = x.parts;
+  const int it = (blockIdx.x - i * kParts) * kMergeThreads + threadIdx.x;
   const int rr = it / (D / 4);
   const int c4 = it - rr * (D / 4);
   const int rq = x.qt * kQRows + rr;
-  if (rq >= blk.n * p.G) return;
+  if (rq >= x.rows) return;
+  // record k: slot x.slot for the first, 2w of the slices after its own for the others
+  constexpr int64_t kSlot = (int64_t)kQRows * C::kRec;
+  const float* head = p.rec + x.slot * kSlot + (int64_t)rr * C::kRec;
+  const float* recs = p.rec + (x.slot & ~1) * kSlot + (int64_t)rr * C::kRec;
   float M = -INFINITY, L = 0.f;
   f32x4 A = {0.f, 0.f, 0.f, 0.f};
   for (int k0 = 0; k0 < nr; k0 += kMergeBatch) {
@@ -1056,8 +1222,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(QueryParams 
       lk[k] = 0.f;
       ak[k] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (k0 + k < nr) {
-        const int slot = 2 * (w + k0 + k) + (k0 + k == 0 && from > lo ? 1 : 0);
-        const float* r = p.rec + (int64_t)slot * kQRows * C::kRec + (int64_t)rr * C::kRec;
+        const float* r = k0 + k == 0 ? head : recs + (k0 + k) * 2 * kSlot;
         mk[k] = r[0];
         lk[k] = r[1];
         ak[k] = *reinterpret_cast<const f32x4*>(r + 2 + 4 * c4);
@@ -1081,7 +1246,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(QueryParams 
   const float inv = L > 0.f ? 1.f / L : 0.f;
   const int tq = rq / p.G;
   const int g = x.s % p.Hkv;
-  float* orow = p.out + (((int64_t)blk.tok0 + tq) * p.Hq + (int64_t)g * p.G + (rq - tq * p.G)) * D;
+  float* orow = p.out + (((int64_t)x.tok0 + tq) * p.Hq + (int64_t)g * p.G + (rq - tq * p.G)) * D;
   *reinterpret_cast<f32x4*>(orow + 4 * c4) = A * inv;
 }
 
@@ -1172,8 +1337,7 @@ PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t h
   }
   const int64_t P = sh.units * seg / kQueryMinTiles;
   sh.slices = (int32_t)((P < kPagedSlices ? P + 7 : kPagedSlices) / 8 * 8);
-  sh.plan_bytes = ((size_t)(4 + kPagedSlices + 4) * sizeof(int32_t) + (size_t)sh.units * sizeof(PagedUnit) +
-                   (size_t)(sh.units + 1) * sizeof(int64_t) + 255) / 256 * 256;
+  sh.plan_bytes = paged_plan_bytes(sh.units);
   sh.rec_bytes = (size_t)(2 * sh.slices) * kQRows * (head_dim + 2) * sizeof(float);
   return sh;
 }
