@@ -186,15 +186,17 @@ def _rows(t, name, heads, dim, dtype):
     return t.data_ptr(), per_token if tokens > 1 else heads * dim
 
 
-def _typed(t, name, dtype, shape=None, optional=False):
-    """_dev of a tensor of this element type (and shape)."""
-    if (type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.is_contiguous()
-            and (shape is None or t.shape == shape)):
+def _typed(t, name, dtype, count=None, shape=None):
+    """_dev of a tensor of this element type (and number of elements, or shape)."""
+    if (type(t) is _Tensor and t.dtype is dtype and t.is_cuda and t.is_contiguous()
+            and (count is None or t.numel() == count) and (shape is None or t.shape == shape)):
         return t.data_ptr()
-    if t is None and optional:
-        return None
     _dev(t, name)
-    raise ValueError(f"{name} must be {dtype}" + ("" if shape is None else f" of shape {list(shape)}"))
+    want = "" if count is None else f" of {count} elements"
+    raise ValueError(f"{name} must be {dtype}" + (want if shape is None else f" of shape {list(shape)}"))
+
+
+_Tensor, _i32 = torch.Tensor, torch.int32
 
 
 try:  # the current stream's handle without a Stream object around it
@@ -209,6 +211,13 @@ def _stream(stream):
     if _raw_stream is None or not torch.cuda.is_initialized():
         return torch.cuda.current_stream().cuda_stream
     return _raw_stream(_current_device())
+
+
+def _stream_of_device(stream):
+    """_stream where a device tensor has been seen, so that the device is initialised."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(_current_device())
 
 
 def _check(fn, status):
@@ -467,21 +476,23 @@ def dkv_page_extend(unit_new, unit_len, free_pages, n_free, page_table, page_row
     [N*Hkv][pages_per_seg]; tok_off: int32 [N+1], first_pos: int32 [N], slots: int64 [max_tokens][Hkv] (out);
     new_len, n_free_out: unit_len and n_free in place when not given; entries: optional int32
     [N*Hkv][max_entries][4], n_entries: optional int32 [N*Hkv]; pages_needed: optional int64 [1]."""
-    N, Hkv, i32 = unit_len.shape[0], int(num_kv_heads), torch.int32
+    N, Hkv = unit_len.shape[0], int(num_kv_heads)
     nseg, pps = page_table.shape
-    if nseg != N * Hkv or slots.dim() != 2 or slots.shape[1] != Hkv:
+    rows, heads = slots.shape
+    if nseg != N * Hkv or heads != Hkv:
         raise ValueError("page_table must have N * Hkv rows and slots Hkv columns")
-    max_entries = 0 if entries is None else entries.shape[1]
+    most = 0 if entries is None else entries.shape[1]
     _check("dkv_page_extend", library().dkv_page_extend(
-        N, Hkv, int(page_rows), _typed(unit_new, "unit_new", i32, (N,)), _typed(unit_len, "unit_len", i32, (N,)),
-        _typed(unit_len if new_len is None else new_len, "new_len", i32, (N,)),
-        _typed(free_pages, "free_pages", i32), free_pages.numel(), _typed(n_free, "n_free", i32, (1,)),
-        _typed(n_free if n_free_out is None else n_free_out, "n_free_out", i32, (1,)),
-        _typed(page_table, "page_table", i32), pps, _typed(tok_off, "tok_off", i32, (N + 1,)),
-        _typed(first_pos, "first_pos", i32, (N,)), _typed(slots, "slots", torch.int64), slots.shape[0],
-        _typed(entries, "entries", i32, (nseg, max_entries, 4), True), _typed(n_entries, "n_entries", i32, (nseg,), True),
-        max_entries, _typed(pages_needed, "pages_needed", torch.int64, (1,), True), _dev(workspace, "workspace"),
-        workspace.nbytes, _stream(stream)))
+        N, Hkv, int(page_rows), _typed(unit_new, "unit_new", _i32, N), _typed(unit_len, "unit_len", _i32),
+        _typed(unit_len if new_len is None else new_len, "new_len", _i32, N), _typed(free_pages, "free_pages", _i32),
+        free_pages.numel(), _typed(n_free, "n_free", _i32, 1),
+        _typed(n_free if n_free_out is None else n_free_out, "n_free_out", _i32, 1),
+        _typed(page_table, "page_table", _i32), pps, _typed(tok_off, "tok_off", _i32, N + 1),
+        _typed(first_pos, "first_pos", _i32, N), _typed(slots, "slots", torch.int64), rows,
+        None if entries is None else _typed(entries, "entries", _i32, None, (nseg, most, 4)),
+        None if n_entries is None else _typed(n_entries, "n_entries", _i32, nseg), most,
+        None if pages_needed is None else _typed(pages_needed, "pages_needed", torch.int64, 1),
+        _dev(workspace, "workspace"), workspace.nbytes, _stream_of_device(stream)))
 
 
 def dkv_page_release_workspace_bytes(num_segments, pages_per_seg):
@@ -491,15 +502,15 @@ def dkv_page_release_workspace_bytes(num_segments, pages_per_seg):
 def dkv_page_release(page_table, free_pages, n_free, workspace, keep=None, table_out=None, n_free_out=None, stream=None):
     """page_table: int32 [nseg][pages_per_seg]; free_pages: int32 stack, n_free: int32 [1] its height; keep: optional
     uint8 of page_table's shape (None: every page goes); table_out, n_free_out: in place when not given."""
-    shape, i32 = tuple(page_table.shape), torch.int32
-    if len(shape) != 2:
-        raise ValueError("page_table must be [nseg][pages_per_seg]")
+    shape = page_table.shape
+    nseg, pps = shape
     _check("dkv_page_release", library().dkv_page_release(
-        shape[0], shape[1], _typed(page_table, "page_table", i32), _typed(keep, "keep", torch.uint8, shape, True),
-        _typed(page_table if table_out is None else table_out, "table_out", i32, shape),
-        _typed(free_pages, "free_pages", i32), free_pages.numel(), _typed(n_free, "n_free", i32, (1,)),
-        _typed(n_free if n_free_out is None else n_free_out, "n_free_out", i32, (1,)), _dev(workspace, "workspace"),
-        workspace.nbytes, _stream(stream)))
+        nseg, pps, _typed(page_table, "page_table", _i32),
+        None if keep is None else _typed(keep, "keep", torch.uint8, None, shape),
+        _typed(page_table if table_out is None else table_out, "table_out", _i32, None, shape),
+        _typed(free_pages, "free_pages", _i32), free_pages.numel(), _typed(n_free, "n_free", _i32, 1),
+        _typed(n_free if n_free_out is None else n_free_out, "n_free_out", _i32, 1), _dev(workspace, "workspace"),
+        workspace.nbytes, _stream_of_device(stream)))
 
 
 def dkv_paged_append(k_new, v_new, slots, k_pages, v_pages, stream=None):
@@ -507,14 +518,16 @@ def dkv_paged_append(k_new, v_new, slots, k_pages, v_pages, stream=None):
     [tokens][Hkv]; k_pages, v_pages: [num_pages][page_rows][d]."""
     num_pages, page_rows, dim = k_pages.shape
     tokens, Hkv = slots.shape
-    k_ptr, stride = _rows(k_new, "k_new", Hkv, dim, k_pages.dtype)
-    v_ptr, v_stride = _rows(v_new, "v_new", Hkv, dim, k_pages.dtype)
-    if k_new.shape[0] != tokens or v_new.shape[0] != tokens or v_stride != stride:
-        raise ValueError("k_new and v_new must have a row per row of slots, evenly spaced alike")
+    dtype = k_pages.dtype
+    k_ptr, stride = _rows(k_new, "k_new", Hkv, dim, dtype)
+    if (type(v_new) is not _Tensor or v_new.dtype is not dtype or not v_new.is_cuda or v_new.shape != k_new.shape
+            or (v_new.stride() != k_new.stride() and tokens > 1) or k_new.shape[0] != tokens):
+        raise ValueError("k_new and v_new must be device tensors alike, with a row per row of slots, evenly spaced alike")
+    v_ptr, _ = (v_new.data_ptr(), stride) if tokens > 1 else _rows(v_new, "v_new", Hkv, dim, dtype)
     _check("dkv_paged_append", library().dkv_paged_append(
-        dtype_code(k_pages.dtype), tokens, Hkv, dim, k_ptr, v_ptr, stride, _typed(slots, "slots", torch.int64),
-        _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", k_pages.dtype, (num_pages, page_rows, dim)), num_pages,
-        page_rows, _stream(stream)))
+        dtype_code(dtype), tokens, Hkv, dim, k_ptr, v_ptr, stride, _typed(slots, "slots", torch.int64),
+        _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", dtype, None, k_pages.shape), num_pages, page_rows,
+        _stream_of_device(stream)))
 
 
 def dkv_paged_query_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q, rows_hint=0):
@@ -529,15 +542,16 @@ def dkv_paged_query_attn(q, tok_off, first_pos, k_pages, v_pages, entries, n_ent
     n_entries: int32 [B*Hkv]; out: fp32 [tokens][Hq][d]; max_q: the longest chunk; workspace: device tensor of
     dkv_paged_query_workspace_bytes(...) bytes, or None when that is 0."""
     tokens, Hq, dim = q.shape
-    B, Hkv, i32 = first_pos.shape[0], int(num_kv_heads), torch.int32
-    num_pages, page_rows, _ = k_pages.shape
-    q_ptr, stride = _rows(q, "q", Hq, dim, k_pages.dtype)
+    B, Hkv, dtype = first_pos.shape[0], int(num_kv_heads), k_pages.dtype
+    num_pages, page_rows, depth = pool = k_pages.shape
+    nseg, most, four = entries.shape
+    if depth != dim or nseg != B * Hkv or four != 4:
+        raise ValueError("k_pages must hold rows of q's size and entries B * Hkv lists of four int32 each")
+    q_ptr, stride = _rows(q, "q", Hq, dim, dtype)
     ws_ptr, ws_bytes = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.nbytes)
     _check("dkv_paged_query_attn", library().dkv_paged_query_attn(
-        dtype_code(k_pages.dtype), B, Hq, Hkv, dim, tokens, int(max_q), q_ptr, stride,
-        _typed(tok_off, "tok_off", i32, (B + 1,)), _typed(first_pos, "first_pos", i32),
-        _typed(k_pages, "k_pages", k_pages.dtype, (num_pages, page_rows, dim)),
-        _typed(v_pages, "v_pages", k_pages.dtype, (num_pages, page_rows, dim)), num_pages, page_rows,
-        _typed(entries, "entries", i32, (B * Hkv, entries.shape[1], 4)), _typed(n_entries, "n_entries", i32, (B * Hkv,)),
-        entries.shape[1], float(sm_scale), int(rows_hint), _typed(out, "out", torch.float32, (tokens, Hq, dim)), ws_ptr,
-        ws_bytes, _stream(stream)))
+        dtype_code(dtype), B, Hq, Hkv, dim, tokens, int(max_q), q_ptr, stride, _typed(tok_off, "tok_off", _i32, B + 1),
+        _typed(first_pos, "first_pos", _i32), _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", dtype, None, pool),
+        num_pages, page_rows, _typed(entries, "entries", _i32), _typed(n_entries, "n_entries", _i32, nseg), most,
+        float(sm_scale), int(rows_hint), _typed(out, "out", torch.float32, None, (tokens, Hq, dim)), ws_ptr, ws_bytes,
+        _stream_of_device(stream)))

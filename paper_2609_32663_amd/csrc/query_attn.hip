@@ -1324,7 +1324,7 @@ PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t h
   sh.plan_bytes = sh.rec_bytes = 0;
   const int64_t rows = (int64_t)max_q * G;
   sh.rec_rows = (int32_t)((rows + 3) / 4 * 4);
-  sh.shorts = rows <= kShortRows / 4;
+  sh.shorts = paged_takes_short(nseg, rows, rows_hint);
   // segments of fewer than two ranges' worth of keys on average: no split
   if (seg < 2 * kQueryMinTiles) return sh;
   if (sh.shorts) {

@@ -151,7 +151,7 @@ def test_prompts_from_their_first_token(d, n, R):
 
 
 @pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("new", [[1], [4], [9, 1], [30], [65], [200, 1, 3]])
+@pytest.mark.parametrize("new", [[1], [4], [9, 1], [20], [30, 2], [50], [61, 33], [65], [200, 1, 3]])
 def test_long_contexts(d, dim, new):
     """The keys of a segment are split; unequal lengths, and hints that are wrong."""
     rng = np.random.default_rng([dim, len(new), new[0]])
