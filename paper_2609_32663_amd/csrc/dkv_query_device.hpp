@@ -41,16 +41,18 @@ __device__ __forceinline__ void bf16_split(float x0, float x1, uint32_t& a, uint
   b = __builtin_bit_cast(uint32_t, l);
 }
 
-// The same in three bf16 pairs: a + b + c carries all 24 bits of x.
-__device__ __forceinline__ void bf16_split3(float x0, float x1, uint32_t& a, uint32_t& b, uint32_t& c) {
-  const f32x2 x = {x0, x1};
-  const bf16x2 h = __builtin_convertvector(x, bf16x2);
-  const f32x2 r = x - __builtin_convertvector(h, f32x2);
-  const bf16x2 l = __builtin_convertvector(r, bf16x2);
-  const bf16x2 t = __builtin_convertvector(r - __builtin_convertvector(l, f32x2), bf16x2);
-  a = __builtin_bit_cast(uint32_t, h);
-  b = __builtin_bit_cast(uint32_t, l);
-  c = __builtin_bit_cast(uint32_t, t);
+// Two probabilities as N bf16 pairs, each the rounding of what the ones before
+// left out: two carry 17 bits, three all 24.  (Remainders by dot products with
+// (-1, 0), half the instructions, made a vector phase a tenth longer.)
+template <int N>
+__device__ __forceinline__ void bf16_parts(float x0, float x1, uint32_t (&part)[N]) {
+  f32x2 x = {x0, x1};
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bf16x2 h = __builtin_convertvector(x, bf16x2);
+    part[i] = __builtin_bit_cast(uint32_t, h);
+    if (i + 1 < N) x = x - __builtin_convertvector(h, f32x2);
+  }
 }
 
 // Maximum over the lanes that share (lane % 16).
@@ -144,8 +146,9 @@ __device__ __forceinline__ i32x4 paged_entry(const PagedSegment& g, int32_t r) {
 // the pool or slots outside a page.
 __device__ __forceinline__ PagedRun paged_run(const PagedSegment& g, const i32x4& x, int32_t r) {
   const int32_t slot = r & ((1 << g.shift) - 1);
-  const bool ok = r < g.end && (uint32_t)x.x < (uint32_t)g.pages &&
-                  (uint32_t)x.y <= (uint32_t)(INT32_MAX - 1) >> g.shift && x.z >= 0 && x.w <= (1 << g.shift);
+  // without branches: a chain of scalar selects
+  const bool ok = (r < g.end) & ((uint32_t)x.x < (uint32_t)g.pages) &
+                  ((uint32_t)x.y <= (uint32_t)(INT32_MAX - 1) >> g.shift) & (x.z >= 0) & (x.w <= (1 << g.shift));
   PagedRun u;
   u.row = ok ? ((int64_t)x.x << g.shift) + slot : 0;
   u.pos = ok ? (x.y << g.shift) + slot : 0;
@@ -153,7 +156,7 @@ __device__ __forceinline__ PagedRun paged_run(const PagedSegment& g, const i32x4
   if (g.stop - u.pos < hi) hi = g.stop - u.pos;
   lo = lo < 0 ? 0 : lo;
   hi = hi > kRun ? kRun : hi;
-  u.lohi = ok && lo < hi ? lo | hi << 8 : 0;
+  u.lohi = ok & (lo < hi) ? lo | hi << 8 : 0;
   return u;
 }
 

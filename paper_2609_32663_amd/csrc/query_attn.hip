@@ -135,10 +135,32 @@ struct QueryItem {
   int32_t nent;
 };
 
+// Paged: the next kTableRuns runs of a segment's rows, decoded side by side into
+// LDS before they are walked: a wave's scalar instructions take its issue slots
+// like any other, and finding a tile's pages entry by entry (some 200 of them)
+// took a seventh of its time.  A word is the run's byte offset in the pools
+// (48 bits), its first and last slot, its first position and its bytes.
+constexpr int kTableRuns = 2048;
+constexpr int kTablePad = 8;  // empty runs behind the span: tiles are read ahead
+
+struct TileRun {
+  uint32_t off, off_hi, pos, bytes;  // off_hi: offset bits 32 .. 47 | lo << 16 | hi << 24
+
+  __device__ __forceinline__ uint32_t lo() const { return (off_hi >> 16) & 0xFF; }
+  __device__ __forceinline__ uint32_t hi() const { return off_hi >> 24; }
+  __device__ __forceinline__ bool whole() const { return off_hi >> 16 == kRun << 8; }
+};
+
+__device__ __forceinline__ u32x4 tile_run_word(const PagedRun& u, int row_bytes) {
+  const uint64_t off = (uint64_t)(u.row + u.lo()) * row_bytes;
+  return u32x4{(uint32_t)off, (uint32_t)(off >> 32) | (uint32_t)u.lohi << 16, (uint32_t)u.pos,
+               (uint32_t)((u.hi() - u.lo()) * row_bytes)};
+}
+
 // kParts: bf16 parts of a probability.
 template <int D, bool PAGED, int kParts>
 __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem& item, uint16_t* k0, uint16_t* k1,
-                                           uint16_t* v0, uint16_t* v1) {
+                                           uint16_t* v0, uint16_t* v1, u32x4* table) {
   using C = QCfg<D>;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -278,36 +300,55 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // Paged: the two 32-row runs of a tile lie in pages of their own, each with
   // a descriptor over its slots [lo, hi): slots outside them (and runs past
   // the range) read zeros.  A wave instruction stays within one run.  `run`
-  // holds the runs of tile t (parity t % 2) from its K loads on.
-  PagedRun run[2][2] = {};
-  PagedSegment seg{};
-  i32x4 next[2] = {};  // the entries of the tile that is loaded next
-  if constexpr (PAGED) {
-    seg = paged_segment(p, s, nent, (int32_t)k_hi, blk.pos0 >= 0 ? paged_pos(blk, blk.n - 1) + 1 : 0);
-    if (D == 64) {  // one instruction per wave: waves 4-7 fill the second run
-      koff -= (uint32_t)((wave_u >> 2) * kRun * C::kRowBytes);
-      voff -= (uint32_t)((wave_u >> 2) * kRun * C::kRowBytes);
-    }
+  // holds the runs of tile t (parity t % 2) from its K loads on, in scalar
+  // registers.
+  TileRun run[2][2] = {};
+  TileRun ahead[2] = {};  // the runs of the tile whose K is loaded next
+  u32x4 coming[2];        // the same, on their way from the table
+  const PagedSegment seg = PAGED ? paged_segment(p, s, nent, (int32_t)k_hi,
+                                                 blk.pos0 >= 0 ? paged_pos(blk, blk.n - 1) + 1 : 0)
+                                 : PagedSegment{};
+  if (PAGED && D == 64) {  // one instruction per wave: waves 4-7 fill the second run
+    koff -= (uint32_t)((wave_u >> 2) * kRun * C::kRowBytes);
+    voff -= (uint32_t)((wave_u >> 2) * kRun * C::kRowBytes);
   }
-  auto fetch_entries = [&](int64_t kt) __attribute__((always_inline)) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) next[h] = paged_entry(seg, (int32_t)kt + kRun * h);
+  // the runs from row `from` on, up to the range's end and kTablePad empty ones
+  auto fill_table = [&](int64_t from) __attribute__((always_inline)) {
+    const int64_t left = (k_hi - from + kRun - 1) / kRun;
+    const int n = (int)(left < 0 ? 0 : (left < kTableRuns ? left : kTableRuns));
+    const i32x4* entries = reinterpret_cast<const i32x4*>(p.entries) + (int64_t)s * p.max_entries;
+    for (int i = tid; i < n + kTablePad; i += kQThreads) {
+      u32x4 w = {0u, 0u, 0u, 0u};
+      if (i < n) {
+        const int32_t r = (int32_t)from + i * kRun;
+        if (r >> seg.shift < nent) w = tile_run_word(paged_run(seg, entries[r >> seg.shift], r), C::kRowBytes);
+      }
+      table[i] = w;
+    }
   };
-  auto find_runs = [&](PagedRun (&u)[2], int64_t kt) __attribute__((always_inline)) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) u[h] = paged_run(seg, next[h], (int32_t)kt + kRun * h);
+  auto read_runs = [&](int at) __attribute__((always_inline)) {
+    coming[0] = table[at];
+    coming[1] = table[at + 1];
   };
-  auto issue_runs = [&](const void* pool, uint32_t off, const PagedRun (&u)[2], uint16_t* buf)
+  auto take_runs = [&](TileRun (&u)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      u[h] = TileRun{(uint32_t)__builtin_amdgcn_readfirstlane(coming[h][0]),
+                     (uint32_t)__builtin_amdgcn_readfirstlane(coming[h][1]),
+                     (uint32_t)__builtin_amdgcn_readfirstlane(coming[h][2]),
+                     (uint32_t)__builtin_amdgcn_readfirstlane(coming[h][3])};
+  };
+  auto issue_runs = [&](const void* pool, uint32_t off, const TileRun (&u)[2], uint16_t* buf)
                         __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < C::kDma; ++i) {
       const int mi = i * (kQThreads / kWave) + wave_u;
       const bool second = D == 64 ? wave_u >= 4 : i == 1;
-      const PagedRun& x = second ? u[1] : u[0];
-      const __amdgpu_buffer_rsrc_t rs = q_rsrc(static_cast<const char*>(pool) + (x.row + x.lo()) * C::kRowBytes,
-                                               (uint32_t)(x.hi() - x.lo()) * C::kRowBytes);
+      const TileRun& x = second ? u[1] : u[0];
+      const __amdgpu_buffer_rsrc_t rs =
+          q_rsrc(static_cast<const char*>(pool) + ((uint64_t)(x.off_hi & 0xFFFF) << 32 | x.off), x.bytes);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(buf + 512 * mi), 16,
-                                               off - (uint32_t)(x.lo() * C::kRowBytes), 0, 0, 0);
+                                               off - x.lo() * C::kRowBytes, 0, 0, 0);
     }
   };
   auto issue = [&](const char* base, uint32_t off, int64_t kt, uint16_t* buf) __attribute__((always_inline)) {
@@ -364,20 +405,20 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // as well, 16 instructions fewer per half, gave nothing: the kernel runs at the
   // power limit).
   const int32_t pos_all = PAGED ? paged_pos(blk, min(qt * kQRows + 16 * kRG * wave_u, rows - 1) / p.G) + 1 : 0;
-  auto softmax = [&](auto masked, float (&sc)[kRG][2][4], int64_t kh, const PagedRun& u) __attribute__((always_inline)) {
+  auto softmax = [&](auto masked, float (&sc)[kRG][2][4], int64_t kh, const TileRun& u) __attribute__((always_inline)) {
     if constexpr (PAGED) {
       // slots outside the entry, or past the position of one of the wave's rows
-      if (u.lohi != kRun << 8 || u.pos + kRun > pos_all) {
+      if (!u.whole() || (int32_t)u.pos + kRun > pos_all) {
         asm volatile("");  // keeps this a branch: the selects would run for every half
 #pragma unroll
         for (int q = 0; q < kRG; ++q) {
-          const int32_t lim = cut[q] - u.pos < u.hi() ? cut[q] - u.pos : u.hi();
+          const int32_t see = cut[q] - (int32_t)u.pos, last = (int32_t)u.hi(), lim = see < last ? see : last;
 #pragma unroll
           for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               const int key = 16 * jj + 4 * kg + v;
-              if (key >= lim || key < u.lo()) sc[q][jj][v] = -INFINITY;
+              if (key >= lim || key < (int32_t)u.lo()) sc[q][jj][v] = -INFINITY;
             }
         }
       }
@@ -438,12 +479,11 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     for (int q = 0; q < kRG; ++q)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        uint32_t x, y, z = 0;
-        if constexpr (kParts == 3) bf16_split3(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y, z);
-        else bf16_split(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y);
-        pp[0][q][e] = x;
-        pp[1][q][e] = y;
-        if constexpr (kParts == 3) pp[2][q][e] = z;
+        uint32_t x[kParts];
+        if constexpr (PAGED) bf16_parts(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x);
+        else bf16_split(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x[0], x[1]);
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) pp[part][q][e] = x[part];
       }
   };
 
@@ -592,31 +632,19 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   uint16_t* const kbuf[2] = {k0, k1};
   uint16_t* const vbuf[2] = {v0, v1};
   const bool lead = __builtin_amdgcn_readfirstlane(wave < 4 ? 1 : 0) != 0;
-  if constexpr (PAGED) {
-    if (nent > 0) {
-      fetch_entries(k_lo);
-      find_runs(run[0], k_lo);
-      fetch_entries(k_lo + kQKeys);
-      find_runs(run[1], k_lo + kQKeys);
-    }
-    issue_runs(p.k, koff, run[0], kbuf[0]);
-    issue_runs(p.v, voff, run[0], vbuf[0]);
-    issue_runs(p.k, koff, run[1], kbuf[1]);
-  } else {
-    issue(kbase, koff, k_lo, kbuf[0]);
-    issue(vbase, voff, k_lo, vbuf[0]);
-    issue(kbase, koff, k_lo + kQKeys, kbuf[1]);
-  }
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-  __syncthreads();
   float sc[kRG][2][4];
   u32x4 pp[kParts][kRG];
   constexpr int kWaitOne = 0x0F70 | C::kDma;  // vmcnt(kDma): the younger of two tiles may still be in flight
-  auto vphase = [&](auto masked, int64_t kh, const PagedRun& u) __attribute__((always_inline)) {
+  auto vphase = [&](auto masked, int64_t kh, const TileRun& u) __attribute__((always_inline)) {
     softmax(masked, sc, kh, u);
     split(sc, pp);
-    // entries on their way must not mix with the LDS reads of the next phase
-    if constexpr (PAGED) __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    if constexpr (PAGED) {
+      // the parts are formed here, not sunk into the product phase
+#pragma unroll
+      for (int part = 0; part < kParts; ++part)
+#pragma unroll
+        for (int q = 0; q < kRG; ++q) asm volatile("" : "+v"(pp[part][q]));
+    }
   };
   // P V first: the probabilities are dead before the new scores are formed
   auto mphase = [&](const uint16_t* kb, int hk, const uint16_t* vb, int hv, bool do_pv) __attribute__((always_inline)) {
@@ -631,8 +659,26 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     }
     __builtin_amdgcn_s_setprio(0);
   };
+  if constexpr (PAGED) {
+    fill_table(k_lo);
+    __syncthreads();
+    read_runs(0);
+    take_runs(run[0]);
+    read_runs(2);
+    take_runs(run[1]);
+    issue_runs(p.k, koff, run[0], kbuf[0]);
+    issue_runs(p.v, voff, run[0], vbuf[0]);
+    issue_runs(p.k, koff, run[1], kbuf[1]);
+  } else {
+    issue(kbase, koff, k_lo, kbuf[0]);
+    issue(vbase, voff, k_lo, vbuf[0]);
+    issue(kbase, koff, k_lo + kQKeys, kbuf[1]);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  __syncthreads();
   const int64_t ntile = k_hi > k_lo ? (k_hi - k_lo + kQKeys - 1) / kQKeys : 0;
   const int64_t nround = q_uniform64((ntile + 1) / 2);
+  int at = 4;  // paged: where the table holds the tile whose K is loaded next
   // pairs of tiles whose halves (up to 32 keys past the pair) all lie below
   // every row's limit need no masking
   const int64_t clear = all_see - k_lo - 5 * 32;
@@ -651,28 +697,32 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       // 4t + 1: lead: vector phase of half 2t; follow: P V of half 2t - 1, scores of 2t
+      if (PAGED && L) read_runs(at);
       if (L) vphase(masked, kt, run[i][0]);
       else mphase(kbuf[i], 0, vbuf[1 - i], 1, i == 1 || kt != k_lo);
+      if (PAGED && L) take_runs(ahead);
       __builtin_amdgcn_s_waitcnt(kWaitOne);  // V of tile t
       meet();
       // 4t + 2: lead: P V of 2t, scores of 2t + 1; follow: vector phase of 2t
       if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
       else issue(vbase, voff, kt + kQKeys, vbuf[1 - i]);
-      if (PAGED && !L) fetch_entries(kt + 2 * kQKeys);
+      if (PAGED && !L) read_runs(at);
       if (L) mphase(kbuf[i], 1, vbuf[i], 0, true);
       else vphase(masked, kt, run[i][0]);
+      if (PAGED && !L) take_runs(ahead);
       meet();
       // 4t + 3: lead: vector phase of 2t + 1; follow: P V of 2t, scores of 2t + 1
-      const PagedRun second = run[i][1];
-      if (PAGED && L) fetch_entries(kt + 2 * kQKeys);
+      const TileRun second = run[i][1];
       if (L) vphase(masked, kt + 32, second);
       else mphase(kbuf[i], 1, vbuf[i], 0, true);
       __builtin_amdgcn_s_waitcnt(kWaitOne);  // K of tile t + 1
       meet();
       // 4t + 4: lead: P V of 2t + 1, scores of 2t + 2; follow: vector phase of 2t + 1
       if constexpr (PAGED) {
-        find_runs(run[i], kt + 2 * kQKeys);
+        run[i][0] = ahead[0];
+        run[i][1] = ahead[1];
         issue_runs(p.k, koff, run[i], kbuf[i]);
+        at += 2;
       } else {
         issue(kbase, koff, kt + 2 * kQKeys, kbuf[i]);
       }
@@ -682,13 +732,24 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       kt += kQKeys;
     }
   };
+  // Between two pairs of tiles nobody reads the table: the last reads were two
+  // meetings ago.
+  auto next_table = [&]() __attribute__((always_inline)) {
+    fill_table(kt + 2 * kQKeys);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    meet();
+    at = 0;
+  };
   auto walk = [&](auto leadc) __attribute__((always_inline)) {
     constexpr bool L = decltype(leadc)::value;
     if (L) mphase(kbuf[0], 0, vbuf[0], 0, false);  // scores of half 0
     meet();
     if constexpr (!PAGED)
       for (int64_t rd = 0; rd < nclear; ++rd) tile_pair(std::false_type{}, leadc);
-    for (int64_t rd = nclear; rd < nround; ++rd) tile_pair(std::true_type{}, leadc);
+    for (int64_t rd = nclear; rd < nround; ++rd) {
+      if (PAGED && at + 4 > kTableRuns) next_table();
+      tile_pair(std::true_type{}, leadc);
+    }
     // the follow group's P V products of the last half (tiles past k_hi hold
     // zeros and all their keys are masked, so the lead's last scores are unused)
     if (!L && nround > 0) pv(vbuf[1], 1, pp);
@@ -698,16 +759,18 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   auto attend_none = [&]() __attribute__((always_inline)) {
     meet();
     for (int64_t rd = 0; rd < nround; ++rd) {
+      if (at + 4 > kTableRuns) next_table();
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         __builtin_amdgcn_s_waitcnt(kWaitOne);
         meet();
         issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
-        fetch_entries(kt + 2 * kQKeys);
+        read_runs(at);
+        take_runs(run[i]);
+        at += 2;
         meet();
         __builtin_amdgcn_s_waitcnt(kWaitOne);
         meet();
-        find_runs(run[i], kt + 2 * kQKeys);
         issue_runs(p.k, koff, run[i], kbuf[i]);
         meet();
         kt += kQKeys;
@@ -799,7 +862,7 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
     t_hi = (int64_t)(r + 1) * tiles / nr;
   }
   query_item<D, false, 2>(p, QueryItem{s, qt, t_lo, t_hi, single, p.rec + (int64_t)item * kQRows * QCfg<D>::kRec,
-                                       PagedBlock{0, 0, 0}, 0}, k0, k1, v0, v1);
+                                       PagedBlock{0, 0, 0}, 0}, k0, k1, v0, v1, nullptr);
 }
 
 // ---------------------------------------------------------------------------
@@ -1051,6 +1114,7 @@ constexpr int64_t kThreePartRows = 32768;
 template <int D>
 __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
   DKV_QUERY_TILES(D);
+  __shared__ __align__(16) u32x4 table[kTableRuns + kTablePad];
   // Without a plan (too few keys to split) one workgroup per (segment, query
   // tile): the loop's only unit.
   const bool split = p.plan != nullptr;
@@ -1116,8 +1180,8 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.rec = nullptr;
     }
     const int64_t rows = (int64_t)__builtin_amdgcn_readfirstlane(x.nent) << p.page_shift;
-    if (rows <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1);
-    else query_item<D, true, 2>(p, x, k0, k1, v0, v1);
+    if (rows <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1, table);
+    else query_item<D, true, 2>(p, x, k0, k1, v0, v1, table);
     __syncthreads();  // the tile buffers are free for the next unit
   }
 }

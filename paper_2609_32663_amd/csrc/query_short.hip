@@ -414,12 +414,11 @@ void query_short_kernel(QueryParams p) {
         asm volatile("" : "+v"(l[q]));  // the sum is formed here, not sunk into a later phase
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          uint32_t x, y, z = 0;
-          if constexpr (kParts == 3) bf16_split3(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y, z);
-          else bf16_split(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x, y);
-          pp[0][q][e] = x;
-          pp[1][q][e] = y;
-          if constexpr (kParts == 3) pp[2][q][e] = z;
+          uint32_t x[kParts];
+          if constexpr (PAGED) bf16_parts(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x);
+          else bf16_split(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x[0], x[1]);
+#pragma unroll
+          for (int part = 0; part < kParts; ++part) pp[part][q][e] = x[part];
         }
       }
     };
