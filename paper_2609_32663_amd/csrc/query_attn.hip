@@ -1374,6 +1374,8 @@ hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, h
   return head_dim == 64 ? launch_d<64>(p, grid, stream) : launch_d<128>(p, grid, stream);
 }
 
+constexpr int64_t kWholeTileRows = 2048, kWholeShortRows = 4096;
+
 PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t head_dim, int32_t num_tokens,
                                 int32_t max_q, int64_t rows_hint) {
   PagedPlanShape sh;
@@ -1389,8 +1391,14 @@ PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t h
   const int64_t rows = (int64_t)max_q * G;
   sh.rec_rows = (int32_t)((rows + 3) / 4 * 4);
   sh.shorts = paged_takes_short(nseg, rows, rows_hint);
-  // segments of fewer than two ranges' worth of keys on average: no split
-  if (seg < 2 * kQueryMinTiles) return sh;
+  // No split for segments of fewer than two ranges' worth of keys on average,
+  // where it saves two launches or one, unless all sequences together have so
+  // many rows that one long one among them would be a workgroup's alone (us,
+  // whole / split, 32 query heads on 8, 8 prompts of 256 tokens 30 / 41, of 512
+  // 75 / 68, 64 of 256 199 / 216; steps of 8 sequences at 300 rows 15.5 / 18.6, of
+  // 64 at 100 22.6 / 26.1; 4,096 rows of one sequence are 180 in query tiles and
+  // 45 in the kernels for short blocks).
+  if (seg < 2 * kQueryMinTiles && hint / hkv <= (sh.shorts ? kWholeShortRows : kWholeTileRows)) return sh;
   if (sh.shorts) {
     // at least 128 keys per workgroup, up to 256 workgroups
     const int64_t P = hint > 0 && hint < kPagedSlices * 128 ? (hint + 127) / 128 : kPagedSlices;
@@ -1399,8 +1407,8 @@ PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t h
     sh.rec_bytes = (size_t)(P + nseg) * sh.rec_rows * (head_dim + 2) * sizeof(float);
     return sh;
   }
-  const int64_t P = sh.units * seg / kQueryMinTiles;
-  sh.slices = (int32_t)((P < kPagedSlices ? P + 7 : kPagedSlices) / 8 * 8);
+  const int64_t P = sh.units * (seg + kUnitTiles) / kQueryMinTiles;
+  sh.slices = (int32_t)((P < kPagedSlices ? P + 8 : kPagedSlices) / 8 * 8);
   sh.plan_bytes = paged_plan_bytes(sh.units);
   sh.rec_bytes = (size_t)(2 * sh.slices) * kQRows * (head_dim + 2) * sizeof(float);
   return sh;

@@ -430,3 +430,134 @@ def test_a_server_from_prompts_to_release(d, R):
     slots = torch.empty((R + 1, Hkv), dtype=torch.int64, device=DEV)
     d.dkv_page_extend(_dev([R + 1]), new_len, stack, n_free, t2, R, Hkv, off2, pos2, slots, ews)
     assert int(n_free) == want_free - 2 * Hkv and int(pos2) == 0 and (slots >= 0).all()
+
+
+@pytest.mark.parametrize("dim,G,Hkv,B,new", [(64, 4, 2, 40, 300), (128, 4, 2, 40, 300), (128, 7, 4, 13, 260),
+                                             (64, 8, 8, 256, 66)])
+@pytest.mark.parametrize("held", [0, 90])
+def test_many_prompts(d, dim, G, Hkv, B, new, held):
+    """More query tiles than compute units, none with more than a workgroup's share of the keys; more of them than a
+    workgroup sorts."""
+    rng = np.random.default_rng([dim, B, new, held])
+    new = rng.integers(new - new // 10, new + 1, size=B)
+    Batch(rng, rng.integers(0, held + 1, size=B), new, Hkv, G, dim, 64, pad=1).check(d)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("held", [32768 - 70, 32768 - 16, 33000])
+def test_contexts_around_the_third_part(d, dim, held):
+    """Query tiles that see 32,768 rows and more, in which a probability has two parts instead of three."""
+    rng = np.random.default_rng([dim, held])
+    Batch(rng, [held, 40], [17, 20], 1, 16, dim, 1024).check(d)
+
+
+@pytest.mark.parametrize("dim,R", [(64, 32), (128, 32), (128, 64)])
+@pytest.mark.parametrize("new", [17, 20, 33])
+def test_one_workgroup_walks_a_long_context(d, dim, R, new):
+    """A hint of one row: no split, and more runs than their table holds at a time; last tiles of one row group to
+    all."""
+    rng = np.random.default_rng([dim, R, new])
+    x = Batch(rng, [80001 * R // 32, 5], [new, 18], 1, 16, dim, R)
+    got = x.check(d, hint=1)
+    split = x.run(d).cpu().numpy()
+    assert row_rel_err(split.reshape(-1, dim), got.reshape(-1, dim)) <= np.sqrt(x.keys) * 2.0 ** -17
+
+
+@pytest.mark.parametrize("new", [[70] + [66] * 9, [1] * 20, [9] + [3] * 30])
+@pytest.mark.parametrize("long", [2100, 25000])
+def test_one_long_sequence_among_short_ones(d, new, long):
+    rng = np.random.default_rng([len(new), long])
+    held = rng.integers(0, 40, size=len(new))
+    held[len(new) // 2] = long
+    Batch(rng, held, new, 2, 4, 128, 64).check(d)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("R", [32, 256])
+@pytest.mark.parametrize("B,n,held", [(1, 64, 9000), (3, 30, 2500), (12, 31, 3000), (30, 17, 600), (4, 40, 5000)])
+def test_blocks_between_the_kernels(d, dim, R, B, n, held):
+    """65 to 256 query rows of few long and of many short segments."""
+    rng = np.random.default_rng([dim, R, B])
+    new = rng.integers(1, n + 1, size=B)
+    new[0] = n
+    Batch(rng, rng.integers(held // 2, held + 1, size=B), new, 2, 4, dim, R).check(d)
+
+
+@pytest.mark.parametrize("new,held", [([1] * 5, 3000), ([80, 3], 9000), ([30, 10], 4000), ([300] * 40, 0), ([200], 0)])
+@pytest.mark.parametrize("hint", [None, 0, 1, 50000])
+def test_writes_stay_in_the_workspace_and_the_output(d, new, held, hint):
+    rng = np.random.default_rng([len(new), held])
+    x = Batch(rng, [held] * len(new), new, 2, 4, 64, 64)
+    h = int(x.n_entries.sum()) * 64 if hint is None else hint
+    need = d.dkv_paged_query_workspace_bytes(len(new), 8, 2, 64, x.tokens, x.max_q, h)
+    ws = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    buf = torch.full((x.tokens + 8, 8, 64), KEEP, device=DEV)
+    x.run(d, hint=hint, ws=ws[:max(need, 16)], out=buf[4:4 + x.tokens])
+    assert (ws[max(need, 16):] == 0xA5).all()
+    assert (buf[:4] == KEEP).all() and (buf[-4:] == KEEP).all()
+    assert torch.equal(buf[4:-4], x.run(d, hint=hint))
+
+
+def test_two_calls_at_once(d):
+    """Two streams, workspaces of their own: each gives what it gives alone."""
+    rng = np.random.default_rng(21)
+    x = Batch(rng, [9000, 20, 300], [150, 1, 9], 2, 4, 128, 64)
+    y = Batch(rng, [7000, 5000], [40, 40], 2, 4, 128, 32)
+    want = [z.run(d) for z in (x, y)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(6):
+        for z, s in zip((x, y), streams):
+            with torch.cuda.stream(s):
+                got.append(z.run(d))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert torch.equal(g, want[i % 2]), i
+
+
+def test_a_sequence_listed_twice(d):
+    """Two sequences that read the same pages, as requests with a common prefix do, at different positions."""
+    rng = np.random.default_rng(22)
+    x = Batch(rng, [3000, 3000], [50, 50], 2, 4, 128, 64)
+    x.entries[2:] = x.entries[:2]
+    x.first_pos[1] = 1500
+    x.check(d)
+
+
+@pytest.mark.parametrize("n", [1, 40, 300])
+def test_a_padded_batch_replayed_with_other_lengths(d, n):
+    """One captured call whose offsets, positions and lists are rewritten between replays: sequences come and go, rows
+    behind the last one stay."""
+    rng = np.random.default_rng([23, n])
+    shapes = [([900, 40, 7], [n, 1, 1]), ([0, 0, 0], [0, 0, n]), ([3000, 1, 2000], [1, n, 0]), ([5, 5, 5], [0, 0, 0])]
+    batches = [Batch(rng, h, w, 2, 4, 128, 64, pad=n + 2 - sum(w), fused=False) for h, w in shapes]
+    pages, wide = max(b.pages for b in batches), max(b.entries.shape[1] for b in batches)
+    hold = [torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV),
+            torch.zeros((pages, 64, 128), dtype=torch.bfloat16, device=DEV),
+            torch.zeros((pages, 64, 128), dtype=torch.bfloat16, device=DEV),
+            torch.zeros((6, wide, 4), dtype=torch.int32, device=DEV), torch.zeros(6, dtype=torch.int32, device=DEV)]
+    q = torch.zeros((n + 2, 8, 128), dtype=torch.bfloat16, device=DEV)
+    out = torch.zeros((n + 2, 8, 128), device=DEV)
+    ws = torch.empty(d.dkv_paged_query_workspace_bytes(3, 8, 2, 128, n + 2, n, 0), dtype=torch.uint8, device=DEV)
+    call = lambda: d.dkv_paged_query_attn(q, *hold, 1.0 / np.sqrt(128), out, ws, 2, n)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for i in (0, 1, 2, 3, 2, 0):
+        b = batches[i]
+        q.copy_(b.q_dev)
+        hold[0].copy_(_dev(b.tok_off))
+        hold[1].copy_(_dev(b.first_pos))
+        hold[2][:b.pages].copy_(b.k)
+        hold[3][:b.pages].copy_(b.v)
+        hold[4][:, :b.entries.shape[1]].copy_(_dev(b.entries))
+        hold[5].copy_(_dev(b.n_entries))
+        out.fill_(KEEP)
+        g.replay()
+        got = out.cpu().numpy()
+        b.max_q = n
+        err = row_rel_err(got.reshape(-1, 128), b.want().reshape(-1, 128))
+        assert np.isfinite(got).all() and err <= np.sqrt(3100) * 2.0 ** -17, (i, err)
