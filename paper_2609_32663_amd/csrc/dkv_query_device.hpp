@@ -99,15 +99,27 @@ __device__ __forceinline__ int32_t paged_pos(const PagedBlock& k, int32_t t) {
   return k.pos0 > INT32_MAX - 1 - t ? INT32_MAX - 1 : k.pos0 + t;
 }
 
-// Entries of segment s that a token at position `last` can see any slot of:
-// all of them, or, when the one after that position's page number starts
-// behind it (as in an unpruned cache), the ones before that.
-__device__ __forceinline__ int32_t paged_entries(const QueryParams& p, int s, int32_t last) {
+// Rows of segment s up to the last that a token at position `last` can see, in
+// whole runs.  It sees slots of all entries, or, when the one after that
+// position's page number starts behind it (as in an unpruned cache), of the
+// ones before that; and the last of them up to its end or that position (half a
+// page less to walk on average).
+__device__ __forceinline__ int32_t paged_rows(const QueryParams& p, int s, int32_t last) {
+  const int32_t x = last >> p.page_shift;
+  const i32x4* list = reinterpret_cast<const i32x4*>(p.entries) + (int64_t)s * p.max_entries;
+  // an unpruned cache's last entry is x: these loads wait for nothing
   const int32_t n = p.n_entries[s];
-  const int32_t x = (last >> p.page_shift) + 1;
-  const int32_t page = x < p.max_entries ? p.entries[4 * ((int64_t)s * p.max_entries + x) + 1] : 0;  // read beside n
+  const int32_t page = x + 1 < p.max_entries ? list[x + 1][1] : 0;
+  i32x4 e = list[x < p.max_entries ? x : 0];
   const int32_t all = n < 0 ? 0 : (n > p.max_entries ? p.max_entries : n);
-  return x < all && page > (last >> p.page_shift) ? x : all;
+  const int32_t held = x + 1 < all && page > x ? x + 1 : all;
+  if (held == 0) return 0;
+  if (held != x + 1) e = list[held - 1];
+  // positions from 2^31 on are beyond every token
+  const int64_t start = (int64_t)e[1] << p.page_shift;
+  int64_t slots = last + 1 - start < e[3] ? last + 1 - start : e[3];
+  slots = slots < 0 ? 0 : (slots > 1 << p.page_shift ? 1 << p.page_shift : slots);
+  return (int32_t)(((int64_t)(held - 1) << p.page_shift) + (slots + kRun - 1) / kRun * kRun);
 }
 
 // A run of 32 rows: the pool row and the position of its first slot, and the

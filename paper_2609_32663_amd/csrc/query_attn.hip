@@ -131,8 +131,8 @@ struct QueryItem {
   int64_t t_lo, t_hi;
   bool single;
   float* rec;
-  PagedBlock blk;  // paged: the sequence's block, and the entries that the tile's rows see
-  int32_t nent;
+  PagedBlock blk;  // paged: the sequence's block, and the segment's rows that the tile's rows see
+  int32_t seen;
 };
 
 // Paged: the next kTableRuns runs of a segment's rows, decoded side by side into
@@ -171,7 +171,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   int s = item.s, qt = item.qt;
   int64_t t_lo = item.t_lo, t_hi = item.t_hi;
   PagedBlock blk = item.blk;
-  int32_t nent = item.nent;
+  int32_t seen = item.seen;
   if constexpr (PAGED) {  // uniform: pages are looked up with scalar loads and arithmetic
     s = __builtin_amdgcn_readfirstlane(s);
     qt = __builtin_amdgcn_readfirstlane(qt);
@@ -180,7 +180,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     blk.tok0 = __builtin_amdgcn_readfirstlane(blk.tok0);
     blk.n = __builtin_amdgcn_readfirstlane(blk.n);
     blk.pos0 = __builtin_amdgcn_readfirstlane(blk.pos0);
-    nent = __builtin_amdgcn_readfirstlane(nent);
+    seen = __builtin_amdgcn_readfirstlane(seen);
   }
   const int rows = PAGED ? blk.n * p.G : p.rows;  // query rows of the segment
   const int bseq = s / p.Hkv;
@@ -218,7 +218,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // this workgroup's keys: the range, up to what its last row sees
   // (all workgroup-uniform; readfirstlane keeps them in scalar registers)
   const int r_last = min(rows - 1, qt * kQRows + kQRows - 1);
-  const int64_t lim_max = PAGED ? (int64_t)nent << p.page_shift : base_len + r_last / p.G + 1;
+  const int64_t lim_max = PAGED ? (int64_t)seen : base_len + r_last / p.G + 1;
   const int64_t k_lo = q_uniform64(t_lo * kQKeys);
   const int64_t k_end = t_hi * kQKeys < lim_max ? t_hi * kQKeys : lim_max;
   const int64_t k_hi = q_uniform64(k_end > k_lo ? k_end : k_lo);
@@ -305,7 +305,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   TileRun run[2][2] = {};
   TileRun ahead[2] = {};  // the runs of the tile whose K is loaded next
   u32x4 coming[2];        // the same, on their way from the table
-  const PagedSegment seg = PAGED ? paged_segment(p, s, nent, (int32_t)k_hi,
+  const PagedSegment seg = PAGED ? paged_segment(p, s, 0, (int32_t)k_hi,
                                                  blk.pos0 >= 0 ? paged_pos(blk, blk.n - 1) + 1 : 0)
                                  : PagedSegment{};
   if (PAGED && D == 64) {  // one instruction per wave: waves 4-7 fill the second run
@@ -321,7 +321,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       u32x4 w = {0u, 0u, 0u, 0u};
       if (i < n) {
         const int32_t r = (int32_t)from + i * kRun;
-        if (r >> seg.shift < nent) w = tile_run_word(paged_run(seg, entries[r >> seg.shift], r), C::kRowBytes);
+        w = tile_run_word(paged_run(seg, entries[r >> seg.shift], r), C::kRowBytes);
       }
       table[i] = w;
     }
@@ -677,7 +677,8 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
   __syncthreads();
   const int64_t ntile = k_hi > k_lo ? (k_hi - k_lo + kQKeys - 1) / kQKeys : 0;
-  const int64_t nround = q_uniform64((ntile + 1) / 2);
+  const int64_t nround = q_uniform64((ntile + (PAGED ? 0 : 1)) / 2);
+  const bool odd = PAGED && (ntile & 1) != 0;  // a last tile without a second
   int at = 4;  // paged: where the table holds the tile whose K is loaded next
   // pairs of tiles whose halves (up to 32 keys past the pair) all lie below
   // every row's limit need no masking
@@ -692,45 +693,47 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // its own copy of the loop, so no phase branches on the group (a branch
   // gave the accumulators a second register set).  Both groups meet equally
   // often: every wave passes the same number of barriers.
-  auto tile_pair = [&](auto masked, auto leadc) __attribute__((always_inline)) {
+  auto one_tile = [&](auto masked, auto leadc, auto par) __attribute__((always_inline)) {
     constexpr bool L = decltype(leadc)::value;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      // 4t + 1: lead: vector phase of half 2t; follow: P V of half 2t - 1, scores of 2t
-      if (PAGED && L) read_runs(at);
-      if (L) vphase(masked, kt, run[i][0]);
-      else mphase(kbuf[i], 0, vbuf[1 - i], 1, i == 1 || kt != k_lo);
-      if (PAGED && L) take_runs(ahead);
-      __builtin_amdgcn_s_waitcnt(kWaitOne);  // V of tile t
-      meet();
-      // 4t + 2: lead: P V of 2t, scores of 2t + 1; follow: vector phase of 2t
-      if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
-      else issue(vbase, voff, kt + kQKeys, vbuf[1 - i]);
-      if (PAGED && !L) read_runs(at);
-      if (L) mphase(kbuf[i], 1, vbuf[i], 0, true);
-      else vphase(masked, kt, run[i][0]);
-      if (PAGED && !L) take_runs(ahead);
-      meet();
-      // 4t + 3: lead: vector phase of 2t + 1; follow: P V of 2t, scores of 2t + 1
-      const TileRun second = run[i][1];
-      if (L) vphase(masked, kt + 32, second);
-      else mphase(kbuf[i], 1, vbuf[i], 0, true);
-      __builtin_amdgcn_s_waitcnt(kWaitOne);  // K of tile t + 1
-      meet();
-      // 4t + 4: lead: P V of 2t + 1, scores of 2t + 2; follow: vector phase of 2t + 1
-      if constexpr (PAGED) {
-        run[i][0] = ahead[0];
-        run[i][1] = ahead[1];
-        issue_runs(p.k, koff, run[i], kbuf[i]);
-        at += 2;
-      } else {
-        issue(kbase, koff, kt + 2 * kQKeys, kbuf[i]);
-      }
-      if (L) mphase(kbuf[1 - i], 0, vbuf[i], 1, true);
-      else vphase(masked, kt + 32, second);
-      meet();
-      kt += kQKeys;
+    constexpr int i = decltype(par)::value;  // tile t's parity
+    // 4t + 1: lead: vector phase of half 2t; follow: P V of half 2t - 1, scores of 2t
+    if (PAGED && L) read_runs(at);
+    if (L) vphase(masked, kt, run[i][0]);
+    else mphase(kbuf[i], 0, vbuf[1 - i], 1, i == 1 || kt != k_lo);
+    if (PAGED && L) take_runs(ahead);
+    __builtin_amdgcn_s_waitcnt(kWaitOne);  // V of tile t
+    meet();
+    // 4t + 2: lead: P V of 2t, scores of 2t + 1; follow: vector phase of 2t
+    if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
+    else issue(vbase, voff, kt + kQKeys, vbuf[1 - i]);
+    if (PAGED && !L) read_runs(at);
+    if (L) mphase(kbuf[i], 1, vbuf[i], 0, true);
+    else vphase(masked, kt, run[i][0]);
+    if (PAGED && !L) take_runs(ahead);
+    meet();
+    // 4t + 3: lead: vector phase of 2t + 1; follow: P V of 2t, scores of 2t + 1
+    const TileRun second = run[i][1];
+    if (L) vphase(masked, kt + 32, second);
+    else mphase(kbuf[i], 1, vbuf[i], 0, true);
+    __builtin_amdgcn_s_waitcnt(kWaitOne);  // K of tile t + 1
+    meet();
+    // 4t + 4: lead: P V of 2t + 1, scores of 2t + 2; follow: vector phase of 2t + 1
+    if constexpr (PAGED) {
+      run[i][0] = ahead[0];
+      run[i][1] = ahead[1];
+      issue_runs(p.k, koff, run[i], kbuf[i]);
+      at += 2;
+    } else {
+      issue(kbase, koff, kt + 2 * kQKeys, kbuf[i]);
     }
+    if (L) mphase(kbuf[1 - i], 0, vbuf[i], 1, true);
+    else vphase(masked, kt + 32, second);
+    meet();
+    kt += kQKeys;
+  };
+  auto tile_pair = [&](auto masked, auto leadc) __attribute__((always_inline)) {
+    one_tile(masked, leadc, std::integral_constant<int, 0>{});
+    one_tile(masked, leadc, std::integral_constant<int, 1>{});
   };
   // Between two pairs of tiles nobody reads the table: the last reads were two
   // meetings ago.
@@ -750,6 +753,11 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       if (PAGED && at + 4 > kTableRuns) next_table();
       tile_pair(std::true_type{}, leadc);
     }
+    if (PAGED && odd) {
+      one_tile(std::true_type{}, leadc, std::integral_constant<int, 0>{});
+      if (!L) pv(vbuf[0], 1, pp);
+      return;
+    }
     // the follow group's P V products of the last half (tiles past k_hi hold
     // zeros and all their keys are masked, so the lead's last scores are unused)
     if (!L && nround > 0) pv(vbuf[1], 1, pp);
@@ -758,24 +766,27 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // the others then have the matrix units and the power to themselves.
   auto attend_none = [&]() __attribute__((always_inline)) {
     meet();
+    auto none = [&](auto par) __attribute__((always_inline)) {
+      constexpr int i = decltype(par)::value;
+      __builtin_amdgcn_s_waitcnt(kWaitOne);
+      meet();
+      issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
+      read_runs(at);
+      take_runs(run[i]);
+      at += 2;
+      meet();
+      __builtin_amdgcn_s_waitcnt(kWaitOne);
+      meet();
+      issue_runs(p.k, koff, run[i], kbuf[i]);
+      meet();
+      kt += kQKeys;
+    };
     for (int64_t rd = 0; rd < nround; ++rd) {
       if (at + 4 > kTableRuns) next_table();
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        __builtin_amdgcn_s_waitcnt(kWaitOne);
-        meet();
-        issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
-        read_runs(at);
-        take_runs(run[i]);
-        at += 2;
-        meet();
-        __builtin_amdgcn_s_waitcnt(kWaitOne);
-        meet();
-        issue_runs(p.k, koff, run[i], kbuf[i]);
-        meet();
-        kt += kQKeys;
-      }
+      none(std::integral_constant<int, 0>{});
+      none(std::integral_constant<int, 1>{});
     }
+    if (odd) none(std::integral_constant<int, 0>{});
   };
   if (PAGED && qt * kQRows + 16 * kRG * wave_u >= rows) attend_none();
   else if (lead) walk(std::true_type{});
@@ -888,7 +899,7 @@ constexpr int kWholeTiles = 10;
 constexpr int kSortBuckets = 1024;
 
 struct PagedUnit {
-  int32_t s, qt, nent, pad;
+  int32_t s, qt, rows, pad;  // rows: of the segment, up to the last that the tile sees
 };
 
 // Words of the plan: slices and units, whether units stay whole, the units'
@@ -929,15 +940,15 @@ size_t paged_plan_bytes(int64_t units) {
           sizeof(int64_t) * (units + 1) + 255) / 256 * 256;
 }
 
-__device__ __forceinline__ int64_t unit_tiles(const QueryParams& p, int32_t nent) {
-  return (((int64_t)nent << p.page_shift) + kQKeys - 1) / kQKeys;
+__device__ __forceinline__ int64_t unit_tiles(int32_t rows) {
+  return ((int64_t)rows + kQKeys - 1) / kQKeys;
 }
 
-// Entries that query tile qt of a block sees.
-__device__ __forceinline__ int32_t unit_entries(const QueryParams& p, const PagedBlock& k, int s, int qt) {
-  if (k.pos0 < 0) return 0;
+// Rows of segment s that query tile qt of a block sees.
+__device__ __forceinline__ int32_t unit_rows(const QueryParams& p, const PagedBlock& k, int s, int qt) {
+  if (k.pos0 < 0 || p.max_entries == 0) return 0;
   const int64_t last = (int64_t)(qt + 1) * kQRows < (int64_t)k.n * p.G ? (int64_t)(qt + 1) * kQRows : (int64_t)k.n * p.G;
-  return paged_entries(p, s, paged_pos(k, (int32_t)((last - 1) / p.G)));
+  return paged_rows(p, s, paged_pos(k, (int32_t)((last - 1) / p.G)));
 }
 
 // One workgroup; bound by the chain of its dependent reads (offsets, counts)
@@ -997,9 +1008,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
       const int in = (int)(u - (int64_t)pre[lo] * p.Hkv);
       const int g = in / tiles, qt = in - g * tiles;
       const int s = lo * p.Hkv + g;
-      const int32_t nent = unit_entries(p, PagedBlock{0, blk_n[lo], blk_pos[lo]}, s, qt);
-      plan.unit[u] = PagedUnit{s, qt, nent, 0};
-      mine = unit_tiles(p, nent) + kUnitTiles;  // below 2^25
+      const int32_t rows = unit_rows(p, PagedBlock{0, blk_n[lo], blk_pos[lo]}, s, qt);
+      plan.unit[u] = PagedUnit{s, qt, rows, 0};
+      mine = unit_tiles(rows) + kUnitTiles;  // below 2^25
       most = max(most, (int32_t)mine);
     }
     if (u0 > 0) __syncthreads();
@@ -1109,7 +1120,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
 // with three; 256 tokens over 45K rows 291 and 351).  Two parts err by 2.6e-6
 // of the output's norm at any length, three by 1.7e-7 at 1K keys and 1.0e-6 at
 // 32K; attention in plain fp32 by 2.8e-7 and 2.3e-6.
-constexpr int64_t kThreePartRows = 32768;
+constexpr int32_t kThreePartRows = 32768;
 
 template <int D>
 __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
@@ -1144,10 +1155,10 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       const PagedUnit unit = plan.unit[v];
       x.s = unit.s;
       x.qt = unit.qt;
-      x.nent = unit.nent;
+      x.seen = unit.rows;
       x.blk = paged_block(p, unit.s / p.Hkv);
       x.t_lo = 0;
-      x.t_hi = unit_tiles(p, unit.nent);
+      x.t_hi = unit_tiles(unit.rows);
       x.single = true;
       x.rec = nullptr;
     } else if (split) {
@@ -1161,7 +1172,7 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       const PagedUnit unit = plan.unit[u];
       x.s = __builtin_amdgcn_readfirstlane(unit.s);
       x.qt = __builtin_amdgcn_readfirstlane(unit.qt);
-      x.nent = __builtin_amdgcn_readfirstlane(unit.nent);
+      x.seen = __builtin_amdgcn_readfirstlane(unit.rows);
       x.blk = paged_block(p, x.s / p.Hkv);
       x.t_lo = a - from;
       x.t_hi = b - from;
@@ -1173,14 +1184,13 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.qt = blockIdx.x - x.s * p.qtiles;
       x.blk = paged_block(p, x.s / p.Hkv);
       if ((int64_t)x.qt * kQRows >= (int64_t)x.blk.n * p.G) return;
-      x.nent = __builtin_amdgcn_readfirstlane(unit_entries(p, x.blk, x.s, x.qt));
+      x.seen = __builtin_amdgcn_readfirstlane(unit_rows(p, x.blk, x.s, x.qt));
       x.t_lo = 0;
-      x.t_hi = unit_tiles(p, x.nent);
+      x.t_hi = unit_tiles(x.seen);
       x.single = true;
       x.rec = nullptr;
     }
-    const int64_t rows = (int64_t)__builtin_amdgcn_readfirstlane(x.nent) << p.page_shift;
-    if (rows <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1, table);
+    if (__builtin_amdgcn_readfirstlane(x.seen) <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1, table);
     else query_item<D, true, 2>(p, x, k0, k1, v0, v1, table);
     __syncthreads();  // the tile buffers are free for the next unit
   }
