@@ -878,11 +878,15 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
 
 // ---------------------------------------------------------------------------
 // Paged calls.  A unit is one query tile of one segment (of a sequence's own
-// number of them); its length is its key tiles (up to what its last row sees)
-// plus kUnitTiles for its fixed cost.  The lengths of all units, laid end to
-// end, are cut into P equal slices, one per workgroup: however unequal the
-// chunks and the contexts, every workgroup has the same work and all run at
-// once.  A unit that lies in one slice is written directly.  A slice holds at
+// number of them); its length is the cost of its key tiles (up to what its last
+// row sees) and kUnitTiles more for what it takes by itself.  A tile costs
+// kHalfCost where only the lead waves have rows (at most 128), which leaves a
+// SIMD to one wave, and else kTileCost: 32 sequences of 8,000 keys, 8 heads, walked
+// at 2.1 us a tile with 4 to 64 rows, 2.4 with 128, 3.1 with 160, 3.8 with 256.
+// The lengths of all units, laid end to end, are cut into P equal slices (up to
+// the next whole tile), one per workgroup: however unequal the chunks and the
+// contexts, every workgroup has the same work and all run at once.  A unit that
+// lies in one slice is written directly.  A slice holds at
 // most two parts of others, the rest of the unit it starts in (record slot 2w)
 // and the head of the unit it ends in (2w + 1; a unit that starts with the
 // slice is in slot 2w), and a combine kernel folds a unit's records in slice
@@ -895,16 +899,19 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
 // layer: 255 split units' records and their combine cost 35 us of 309).
 // ---------------------------------------------------------------------------
 constexpr int kUnitTiles = 2;
+constexpr int kTileCost = 4, kHalfCost = 3;
 constexpr int kWholeTiles = 10;
 constexpr int kSortBuckets = 1024;
 
 struct PagedUnit {
-  int32_t s, qt, rows, pad;  // rows: of the segment, up to the last that the tile sees
+  int32_t s, qt;
+  int32_t rows;  // of the segment, up to the last that the tile sees
+  int32_t cost;  // of a key tile
 };
 
-// Words of the plan: slices and units, whether units stay whole, the units'
-// total length, each slice's first unit, the units that several slices share,
-// what each unit is, where it starts, and for whole units the workgroups' units,
+// Words of the plan: slices and units, whether units stay whole,
+// each slice's first unit and where it starts, the units that several slices
+// share, what each unit is, where it starts, and for whole units the workgroups' units,
 // round by round (-1: none).
 struct PagedShared {
   int32_t slot, parts;  // slot of the first record, records (the others at slots 2w of the next slices)
@@ -913,8 +920,8 @@ struct PagedShared {
 
 struct PagedPlan {
   int32_t* head;        // [4]: P, units, whole, shared units
-  int64_t* total;
   int32_t* first;       // [kPagedSlices] unit that holds the slice's start
+  int64_t* cut;         // [kPagedSlices + 2] where each slice starts, the last one's end
   PagedShared* shared;  // [kPagedSlices]
   PagedUnit* unit;      // [units]
   int64_t* start;       // [units + 1]
@@ -926,9 +933,9 @@ constexpr int kPagedPlanHead = 8;  // words before `first`
 __host__ __device__ __forceinline__ PagedPlan paged_plan_of(int32_t* words, int64_t units) {
   PagedPlan x;
   x.head = words;
-  x.total = reinterpret_cast<int64_t*>(words + 4);
   x.first = words + kPagedPlanHead;
-  x.shared = reinterpret_cast<PagedShared*>(x.first + kPagedSlices);
+  x.cut = reinterpret_cast<int64_t*>(x.first + kPagedSlices);
+  x.shared = reinterpret_cast<PagedShared*>(x.cut + kPagedSlices + 2);
   x.unit = reinterpret_cast<PagedUnit*>(x.shared + kPagedSlices);
   x.start = reinterpret_cast<int64_t*>(x.unit + units);
   x.order = reinterpret_cast<int32_t*>(x.start + units + 1);
@@ -936,8 +943,8 @@ __host__ __device__ __forceinline__ PagedPlan paged_plan_of(int32_t* words, int6
 }
 
 size_t paged_plan_bytes(int64_t units) {
-  return (sizeof(int32_t) * (kPagedPlanHead + 2 * kPagedSlices + units) + sizeof(PagedShared) * kPagedSlices + sizeof(PagedUnit) * units +
-          sizeof(int64_t) * (units + 1) + 255) / 256 * 256;
+  return (sizeof(int32_t) * (kPagedPlanHead + 2 * kPagedSlices + units) + sizeof(PagedShared) * kPagedSlices +
+          sizeof(PagedUnit) * units + sizeof(int64_t) * (kPagedSlices + units + 3) + 255) / 256 * 256;
 }
 
 __device__ __forceinline__ int64_t unit_tiles(int32_t rows) {
@@ -961,6 +968,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
   __shared__ int32_t pre[DKV_MAX_SEGMENTS + 1];  // query tiles of the sequences before
   __shared__ int32_t blk_n[DKV_MAX_SEGMENTS], blk_pos[DKV_MAX_SEGMENTS];
   __shared__ int64_t start[kPlanUnits + 1];
+  __shared__ int64_t cut[kPagedSlices + 1];
   __shared__ int32_t bucket[kSortBuckets];       // whole units: units per length, then where they go
   __shared__ int32_t order[kPlanUnits];
   __shared__ __align__(16) int32_t load[kPagedSlices];
@@ -1009,8 +1017,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
       const int g = in / tiles, qt = in - g * tiles;
       const int s = lo * p.Hkv + g;
       const int32_t rows = unit_rows(p, PagedBlock{0, blk_n[lo], blk_pos[lo]}, s, qt);
-      plan.unit[u] = PagedUnit{s, qt, rows, 0};
-      mine = unit_tiles(rows) + kUnitTiles;  // below 2^25
+      const int32_t cost = (int64_t)blk_n[lo] * p.G - (int64_t)qt * kQRows <= kQRows / 2 ? kHalfCost : kTileCost;
+      plan.unit[u] = PagedUnit{s, qt, rows, cost};
+      mine = (unit_tiles(rows) + kUnitTiles) * cost;  // below 2^27
       most = max(most, (int32_t)mine);
     }
     if (u0 > 0) __syncthreads();
@@ -1021,7 +1030,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
     }
     len += sum;
   }
-  const int64_t P = len < p.P ? len : p.P;
+  // slices of two tiles at least, so that each has its own start
+  const int64_t most_slices = len == 0 ? 0 : (len < 4 * kTileCost ? 1 : len / (2 * kTileCost));
+  const int64_t P = most_slices < p.P ? most_slices : p.P;
 #pragma unroll
   for (int o = kWave / 2; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, kWave));
   if ((tid & (kWave - 1)) == 0) atomicMax(&longest, most);
@@ -1030,10 +1041,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
     if (near) start[units] = len;
     plan.head[0] = (int32_t)P;
     plan.head[1] = (int32_t)units;
-    plan.total[0] = len;
   }
   __syncthreads();
-  bool whole = near && units > P && longest <= len / p.P && units <= (int64_t)kWholeRounds * p.P;
+  bool whole = near && units > P && len <= INT32_MAX && longest <= len / p.P && units <= (int64_t)kWholeRounds * p.P;
   if (whole) {
     const int rounds = (int)((units + p.P - 1) / p.P);
     for (int i = tid; i < kSortBuckets; i += kPlanThreads) bucket[i] = 0;
@@ -1085,28 +1095,40 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
     for (int o = kWave / 2; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, kWave));
     if (tid < kPagedSlices && (tid & (kWave - 1)) == 0) atomicMax(&share, top);
     __syncthreads();
-    whole = share <= len / p.P + kWholeTiles;
+    whole = share <= len / p.P + kWholeTiles * kTileCost;
   }
-  if (tid == 0) plan.head[2] = whole ? 1 : 0;
-  if (!whole && tid < P) {
-    const int64_t x = (int64_t)tid * len / P;
-    int64_t lo = 0, hi = units;
+  if (tid == 0) plan.head[2] = whole ? 1 : 0, plan.head[3] = 0;
+  if (whole) return;
+  int64_t x = 0, lo = 0, from = 0;  // this thread's slice: its start, the unit there, that unit's first tile
+  PagedUnit u{};
+  if (tid < P) {
+    x = (int64_t)tid * len / P;
+    int64_t hi = units;
     while (hi - lo > 1) {
       const int64_t mid = (lo + hi) >> 1;
       if ((near ? start[mid] : plan.start[mid]) <= x) lo = mid;
       else hi = mid;
     }
+    u = plan.unit[lo];
+    from = (near ? start[lo] : plan.start[lo]) + kUnitTiles * u.cost;
+    if (x > from) x = from + (x - from + u.cost - 1) / u.cost * u.cost;
+    cut[tid] = x;
     plan.first[tid] = (int32_t)lo;
+    plan.cut[tid] = x;
+  }
+  if (tid == 0) plan.cut[P] = len;
+  __syncthreads();
+  if (tid > 0 && tid < P) {
     // the unit that this slice continues, by the first slice to do so
-    const int64_t from = (near ? start[lo] : plan.start[lo]) + kUnitTiles;
-    const int64_t before = (int64_t)(tid - 1) * len / P;  // start of the slice before
-    if (tid > 0 && from < x && from >= before) {
-      const int64_t end = near ? start[lo + 1] : plan.start[lo + 1];
+    const int64_t end = near ? start[lo + 1] : plan.start[lo + 1];
+    const int64_t before = cut[tid - 1];
+    if (from < x && x < end && from >= before) {
+      int64_t last = owner_of(end - 1, len, P);
+      if (cut[last] >= end) --last;
       const int i = atomicAdd(&nshared, 1);
-      const PagedUnit u = plan.unit[lo];
       const PagedBlock k = paged_block(p, u.s / p.Hkv);
-      plan.shared[i] = PagedShared{2 * (tid - 1) + (from > before ? 1 : 0), (int)owner_of(end - 1, len, P) - tid + 2,
-                                   u.s, u.qt, k.tok0, k.n * p.G, {0, 0}};
+      plan.shared[i] = PagedShared{2 * (tid - 1) + (from > before ? 1 : 0), (int)last - tid + 2, u.s, u.qt, k.tok0,
+                                   k.n * p.G, {0, 0}};
     }
   }
   __syncthreads();
@@ -1138,11 +1160,10 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
     whole = __builtin_amdgcn_readfirstlane(plan.head[2]) != 0;
     if (!whole) {
       const int P = __builtin_amdgcn_readfirstlane(plan.head[0]);
-      const int64_t total = q_uniform64(plan.total[0]);
       w = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;  // the grid is a multiple of 8
       if (w >= P) return;
-      lo = q_uniform64((int64_t)w * total / P);
-      hi = q_uniform64((int64_t)(w + 1) * total / P);
+      lo = q_uniform64(plan.cut[w]);
+      hi = q_uniform64(plan.cut[w + 1]);
       u = __builtin_amdgcn_readfirstlane(plan.first[w]);
     }
   }
@@ -1163,19 +1184,20 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.rec = nullptr;
     } else if (split) {
       if (u >= units) break;
-      const int64_t from = q_uniform64(plan.start[u]) + kUnitTiles;  // the unit's first key tile
-      const int64_t end = q_uniform64(plan.start[u + 1]);
-      if (from - kUnitTiles >= hi) break;
+      const PagedUnit unit = plan.unit[u];
+      const int64_t begin = q_uniform64(plan.start[u]), end = q_uniform64(plan.start[u + 1]);
+      const int32_t cost = __builtin_amdgcn_readfirstlane(unit.cost);
+      const int64_t from = begin + kUnitTiles * cost;  // the unit's first key tile
+      if (begin >= hi) break;
       const bool empty = from == end;  // no keys: zeros, by the slice that holds its start
       const int64_t a = lo > from ? lo : from, b = hi < end ? hi : end;
-      if (empty ? from - kUnitTiles < lo : a >= b) continue;
-      const PagedUnit unit = plan.unit[u];
+      if (empty ? begin < lo : a >= b) continue;
       x.s = __builtin_amdgcn_readfirstlane(unit.s);
       x.qt = __builtin_amdgcn_readfirstlane(unit.qt);
       x.seen = __builtin_amdgcn_readfirstlane(unit.rows);
       x.blk = paged_block(p, x.s / p.Hkv);
-      x.t_lo = a - from;
-      x.t_hi = b - from;
+      x.t_lo = (uint32_t)(a - from) / (uint32_t)cost;  // below 2^27
+      x.t_hi = (uint32_t)(b - from) / (uint32_t)cost;
       x.single = empty || (a == from && b == end);
       x.rec = p.rec + (int64_t)(2 * w + (from > lo ? 1 : 0)) * kQRows * QCfg<D>::kRec;
     } else {
