@@ -907,6 +907,8 @@ struct PagedUnit {
   int32_t s, qt;
   int32_t rows;  // of the segment, up to the last that the tile sees
   int32_t cost;  // of a key tile
+  PagedBlock blk;
+  int32_t pad;
 };
 
 // Words of the plan: slices and units, whether units stay whole,
@@ -966,7 +968,7 @@ constexpr int kWholeRounds = 32;  // rounds of whole units at most
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p) {
   __shared__ int64_t red[3][kPlanThreads / kWave];
   __shared__ int32_t pre[DKV_MAX_SEGMENTS + 1];  // query tiles of the sequences before
-  __shared__ int32_t blk_n[DKV_MAX_SEGMENTS], blk_pos[DKV_MAX_SEGMENTS];
+  __shared__ PagedBlock blk[DKV_MAX_SEGMENTS];
   __shared__ int64_t start[kPlanUnits + 1];
   __shared__ int64_t cut[kPagedSlices + 1];
   __shared__ int32_t bucket[kSortBuckets];       // whole units: units per length, then where they go
@@ -983,8 +985,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
     int64_t tiles = 0, sum;
     if (b < B) {
       const PagedBlock k = paged_block(p, b);
-      blk_n[b] = k.n;
-      blk_pos[b] = k.pos0;
+      blk[b] = k;
       tiles = ((int64_t)k.n * p.G + kQRows - 1) / kQRows;
     }
     if (b0 > 0) __syncthreads();
@@ -1016,9 +1017,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
       const int in = (int)(u - (int64_t)pre[lo] * p.Hkv);
       const int g = in / tiles, qt = in - g * tiles;
       const int s = lo * p.Hkv + g;
-      const int32_t rows = unit_rows(p, PagedBlock{0, blk_n[lo], blk_pos[lo]}, s, qt);
-      const int32_t cost = (int64_t)blk_n[lo] * p.G - (int64_t)qt * kQRows <= kQRows / 2 ? kHalfCost : kTileCost;
-      plan.unit[u] = PagedUnit{s, qt, rows, cost};
+      const int32_t rows = unit_rows(p, blk[lo], s, qt);
+      const int32_t cost = (int64_t)blk[lo].n * p.G - (int64_t)qt * kQRows <= kQRows / 2 ? kHalfCost : kTileCost;
+      plan.unit[u] = PagedUnit{s, qt, rows, cost, blk[lo], 0};
       mine = (unit_tiles(rows) + kUnitTiles) * cost;  // below 2^27
       most = max(most, (int32_t)mine);
     }
@@ -1126,9 +1127,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
       int64_t last = owner_of(end - 1, len, P);
       if (cut[last] >= end) --last;
       const int i = atomicAdd(&nshared, 1);
-      const PagedBlock k = paged_block(p, u.s / p.Hkv);
-      plan.shared[i] = PagedShared{2 * (tid - 1) + (from > before ? 1 : 0), (int)last - tid + 2, u.s, u.qt, k.tok0,
-                                   k.n * p.G, {0, 0}};
+      plan.shared[i] = PagedShared{2 * (tid - 1) + (from > before ? 1 : 0), (int)last - tid + 2, u.s, u.qt, u.blk.tok0,
+                                   u.blk.n * p.G, {0, 0}};
     }
   }
   __syncthreads();
@@ -1148,17 +1148,26 @@ template <int D>
 __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
   DKV_QUERY_TILES(D);
   __shared__ __align__(16) u32x4 table[kTableRuns + kTablePad];
+  __shared__ PagedUnit own[kWholeRounds];  // whole units: this workgroup's
   // Without a plan (too few keys to split) one workgroup per (segment, query
   // tile): the loop's only unit.
   const bool split = p.plan != nullptr;
   const PagedPlan plan = paged_plan_of(p.plan, p.max_items);
-  int w = blockIdx.x, u = 0, units = 1;
+  int w = blockIdx.x, u = 0, units = 1, rounds = 0;
   int64_t lo = 0, hi = 0;
   bool whole = false;
   if (split) {
     units = __builtin_amdgcn_readfirstlane(plan.head[1]);
     whole = __builtin_amdgcn_readfirstlane(plan.head[2]) != 0;
-    if (!whole) {
+    if (whole) {
+      rounds = (units + (int)gridDim.x - 1) / (int)gridDim.x;
+      for (int i = threadIdx.x; i < rounds; i += kQThreads) {
+        const int v = plan.order[i * gridDim.x + w];
+        if (v >= 0) own[i] = plan.unit[v];
+        else own[i].s = -1;
+      }
+      __syncthreads();
+    } else {
       const int P = __builtin_amdgcn_readfirstlane(plan.head[0]);
       w = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;  // the grid is a multiple of 8
       if (w >= P) return;
@@ -1170,14 +1179,13 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
   for (int r = 0;; ++r, ++u) {
     QueryItem x;
     if (whole) {
-      if (r * (int)gridDim.x >= units) break;
-      const int v = __builtin_amdgcn_readfirstlane(plan.order[r * gridDim.x + w]);
-      if (v < 0) continue;
-      const PagedUnit unit = plan.unit[v];
+      if (r >= rounds) break;
+      const PagedUnit unit = own[r];
+      if (__builtin_amdgcn_readfirstlane(unit.s) < 0) continue;
       x.s = unit.s;
       x.qt = unit.qt;
       x.seen = unit.rows;
-      x.blk = paged_block(p, unit.s / p.Hkv);
+      x.blk = unit.blk;
       x.t_lo = 0;
       x.t_hi = unit_tiles(unit.rows);
       x.single = true;
@@ -1195,7 +1203,7 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.s = __builtin_amdgcn_readfirstlane(unit.s);
       x.qt = __builtin_amdgcn_readfirstlane(unit.qt);
       x.seen = __builtin_amdgcn_readfirstlane(unit.rows);
-      x.blk = paged_block(p, x.s / p.Hkv);
+      x.blk = unit.blk;
       x.t_lo = (uint32_t)(a - from) / (uint32_t)cost;  // below 2^27
       x.t_hi = (uint32_t)(b - from) / (uint32_t)cost;
       x.single = empty || (a == from && b == end);
