@@ -625,7 +625,7 @@ size_t dkv_page_extend_workspace_bytes(int32_t num_units);
  * needs no page is not held up by the ones before it.
  * DKV_ERR_UNSUPPORTED when N * Hkv > 65535, max_tokens > 2^31 - 128 or
  * max_tokens * Hkv > 2^32 - 256.
- * The call enqueues one kernel when max_tokens is at most 128, or at most 8,192
+ * The call enqueues one kernel when max_tokens is at most 128, or at most 32,768
  * and neither new_len nor n_free_out is updated in place; otherwise one over
  * the units and one over the tokens.
  */
@@ -669,7 +669,8 @@ dkv_status dkv_page_release(int32_t num_segments, int32_t pages_per_seg, const i
  *               fused projection's rows can be passed where they are).
  * slots         int64 [num_tokens][Hkv] as dkv_page_extend writes them; a
  *               token and head with a slot outside [0, num_pages * page_rows)
- *               is skipped.  Two rows with the same slot leave either of them.
+ *               is skipped.  What rows with the same slot leave there is
+ *               unspecified.
  * k_pages, v_pages  the pools, [num_pages][page_rows][d].
  */
 dkv_status dkv_paged_append(dkv_dtype dtype, int32_t num_tokens, int32_t num_kv_heads,
@@ -694,6 +695,7 @@ size_t dkv_paged_query_workspace_bytes(int32_t batch, int32_t num_q_heads, int32
  * tok_off   int32 [B + 1]: sequence b's chunk is rows [tok_off[b],
  *           tok_off[b + 1]); taken within [0, num_tokens], and of a chunk
  *           longer than max_q only the first max_q tokens are attended.
+ *           Chunks must not share rows.
  * first_pos int32 [B]: position of the chunk's first token; a negative one
  *           marks a sequence that attends nothing (its outputs are zeros).
  * entries, n_entries, max_entries  the pages of the B * Hkv segments, from
@@ -717,6 +719,12 @@ size_t dkv_paged_query_workspace_bytes(int32_t batch, int32_t num_q_heads, int32
  *           and must equal the value given to dkv_paged_query_workspace_bytes.
  * workspace dkv_paged_query_workspace_bytes(...) bytes, no initial contents
  *           required, or NULL when that is 0.
+ * Scores, maxima and sums are fp32; a probability enters its product with V as
+ * three bf16 parts (24 bits); in chunks of more query rows per KV head than the
+ * short-block kernels take (64 to 256, by the segments' number and length), as
+ * two (17 bits) for rows that see over 32,768 slots.
+ * The call enqueues one kernel without a workspace; with one, an attention and
+ * a combine kernel, and a plan kernel before them for such chunks.
  * Only DKV_BF16 is supported (DKV_ERR_UNSUPPORTED otherwise); head_dim 64 or
  * 128; DKV_ERR_UNSUPPORTED also when max_entries * page_rows > 2^30 or a
  * dispatch would exceed 2^32 work-items.

@@ -114,14 +114,15 @@ hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, h
 // Whether the kernels for short blocks take a paged call, whose longest block has
 // `rows` query rows per segment; query tiles / short, us, attention with plan
 // and combine, 128-row pages.
-//   * Up to 64 rows: always.
+//   * Up to 64 rows: always (64 rows: 128 segments of 1,000 keys 47 / 46, of 4,000
+//     94 / 89).
 //   * Up to 128 rows: but for many segments of few keys (64 query heads on 8,
-//     128 rows: 128 segments of 1,000 keys 54 / 70, 64 of 4,000 71 / 71, 256 of
-//     4,000 188 / 153, 8 of 130,000 176 / 145; 64 dimensions, 128 of 1,000 43 / 68).
+//     128 rows: 128 segments of 1,000 keys 52 / 72, 64 of 4,000 65 / 70, 256 of
+//     4,000 167 / 150, 8 of 130,000 153 / 139; 64 dimensions, 128 of 1,000 38 / 65).
 //   * More rows: few segments and keys, where the plan and a tile's chain of
-//     phases weigh most (28 heads on 4, 252 rows: 4 of 1,000 42 / 31, of 65,000
-//     93 / 85, of 130,000 140 / 141; 64 on 8, 256 rows: 8 of 16,000 66 / 57, of 65,000
-//     131 / 144; 32 of 4,000 with 133 rows 57 / 61).
+//     phases weigh most (28 heads on 4, 252 rows: 4 of 1,000 35 / 30, of 65,000
+//     91 / 88, of 130,000 128 / 134; 64 on 8, 256 rows: 8 of 16,000 62 / 55, of 65,000
+//     119 / 141; 32 of 4,000 with 133 rows 52 / 60).
 inline bool paged_takes_short(int64_t nseg, int64_t rows, int64_t rows_hint) {
   if (rows <= kShortRows / 4) return true;
   if (rows <= kShortRows / 2) return nseg < kShortManySegments || rows_hint <= 0 || rows_hint / kShortFewKeys >= nseg;

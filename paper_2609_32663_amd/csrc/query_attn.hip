@@ -45,6 +45,16 @@
 // dense contraction (G * n_q query rows against every key), so it is MFMA
 // work, unlike the one-query decode step.
 //
+// Paged calls (dkv_paged_query_attn) run the same tiles over a segment's pages,
+// for sequences whose chunks differ in length: the split into slices and the
+// kernel that plans it are described further down, tile addresses come from a
+// table of 32-row runs in LDS, the products of a phase are one pipeline of LDS
+// reads and matrix instructions, and a probability has two or three bf16 parts.
+// With three a workgroup takes 6,540 cycles for a 64-key tile, of which its
+// matrix instructions fill 4,096: 512 tokens of an 8B layer over 32K keys, two
+// parts, 349 us (794 TFLOP/s of the 4 d flops per query row and key, 1,190 with
+// the second part's), two prompts of 4K, three parts, 262 us (563 and 1,126).
+//
 // This file is compiled with IEEE mode off and no NaN semantics
 // (-mno-amdgpu-ieee -fno-honor-nans): the maxima then need no NaN
 // canonicalisation.  With finite inputs no NaN arises anywhere (masked keys
@@ -895,12 +905,15 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
 // Prompts have many units, none longer than a slice.  There the plan deals the
 // units by falling length, P at a time, the longest of a round to the workgroup
 // with the least so far: when the longest share is at most kWholeTiles above
-// the mean, units stay whole and no record is written (two 4K prompts of an 8B
-// layer: 255 split units' records and their combine cost 35 us of 309).
+// the mean, units stay whole and no record is written (us, whole / slices, 32
+// query heads on 8: two prompts of 4,096 tokens 436 / 490, eight of 1,500 304 / 324,
+// of 1,000 162 / 174).  Not for units of fewer than kWholeMean tiles on average:
+// a slice's many small units read the same keys, one after another (16 prompts of
+// 700 207 / 188, 32 of 512 241 / 224).
 // ---------------------------------------------------------------------------
 constexpr int kUnitTiles = 2;
 constexpr int kTileCost = 4, kHalfCost = 3;
-constexpr int kWholeTiles = 10;
+constexpr int kWholeTiles = 10, kWholeMean = 8;
 constexpr int kSortBuckets = 1024;
 
 struct PagedUnit {
@@ -1044,7 +1057,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
     plan.head[1] = (int32_t)units;
   }
   __syncthreads();
-  bool whole = near && units > P && len <= INT32_MAX && longest <= len / p.P && units <= (int64_t)kWholeRounds * p.P;
+  bool whole = near && units > P && len <= INT32_MAX && longest <= len / p.P &&
+               units <= (int64_t)kWholeRounds * p.P && len >= units * (kWholeMean + kUnitTiles) * kTileCost;
   if (whole) {
     const int rounds = (int)((units + p.P - 1) / p.P);
     for (int i = tid; i < kSortBuckets; i += kPlanThreads) bucket[i] = 0;
@@ -1138,8 +1152,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
 // A probability is used as three bf16 parts, its 24 bits, where the query rows
 // see at most this many rows, and as two, 17 bits, beyond.  The kernel runs at
 // the rate that the matrix units reach under the power limit, so the third
-// product costs what it computes (512 tokens at 32K 354 us with two parts, 430
-// with three; 256 tokens over 45K rows 291 and 351).  Two parts err by 2.6e-6
+// product costs what it computes (512 tokens at 32K 344 us with two parts, 416
+// with three; 256 tokens over 45K rows 239 and 289).  Two parts err by 2.6e-6
 // of the output's norm at any length, three by 1.7e-7 at 1K keys and 1.0e-6 at
 // 32K; attention in plain fp32 by 2.8e-7 and 2.3e-6.
 constexpr int32_t kThreePartRows = 32768;
@@ -1434,10 +1448,10 @@ PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t h
   // No split for segments of fewer than two ranges' worth of keys on average,
   // where it saves two launches or one, unless all sequences together have so
   // many rows that one long one among them would be a workgroup's alone (us,
-  // whole / split, 32 query heads on 8, 8 prompts of 256 tokens 30 / 41, of 512
-  // 75 / 68, 64 of 256 199 / 216; steps of 8 sequences at 300 rows 15.5 / 18.6, of
-  // 64 at 100 22.6 / 26.1; 4,096 rows of one sequence are 180 in query tiles and
-  // 45 in the kernels for short blocks).
+  // whole / split, 32 query heads on 8: 8 prompts of 256 tokens 29 / 50, of 512
+  // 75 / 64; steps of 8 sequences at 300 rows 15.0 / 18.1, of 64 at 100 21.9 /
+  // 25.2; 4,096 rows of one sequence are 180 in query tiles and 45 in the kernels
+  // for short blocks).
   if (seg < 2 * kQueryMinTiles && hint / hkv <= (sh.shorts ? kWholeShortRows : kWholeTileRows)) return sh;
   if (sh.shorts) {
     // at least 128 keys per workgroup, up to 256 workgroups

@@ -443,6 +443,14 @@ def test_many_prompts(d, dim, G, Hkv, B, new, held):
     Batch(rng, rng.integers(0, held + 1, size=B), new, Hkv, G, dim, 64, pad=1).check(d)
 
 
+@pytest.mark.parametrize("dim,G,B,new,held", [(64, 16, 40, 320, 700), (128, 7, 64, 290, 500)])
+def test_many_long_query_tiles(d, dim, G, B, new, held):
+    """Enough tiles of enough keys that workgroups take them whole, round by round."""
+    rng = np.random.default_rng([dim, B, held])
+    new = rng.integers(new - 60, new + 1, size=B)
+    Batch(rng, rng.integers(held - 100, held + 1, size=B), new, 1, G, dim, 128).check(d)
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("held", [32768 - 70, 32768 - 16, 33000])
 def test_contexts_around_the_third_part(d, dim, held):
