@@ -415,13 +415,13 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // as well, 16 instructions fewer per half, gave nothing: the kernel runs at the
   // power limit).
   const int32_t pos_all = PAGED ? paged_pos(blk, min(qt * kQRows + 16 * kRG * wave_u, rows - 1) / p.G) + 1 : 0;
-  auto softmax = [&](auto masked, float (&sc)[kRG][2][4], int64_t kh, const TileRun& u) __attribute__((always_inline)) {
+  auto softmax = [&](auto masked, auto rgs, float (&sc)[kRG][2][4], int64_t kh, const TileRun& u) __attribute__((always_inline)) {
     if constexpr (PAGED) {
       // slots outside the entry, or past the position of one of the wave's rows
       if (!u.whole() || (int32_t)u.pos + kRun > pos_all) {
         asm volatile("");  // keeps this a branch: the selects would run for every half
 #pragma unroll
-        for (int q = 0; q < kRG; ++q) {
+        for (int q = 0; q < decltype(rgs)::value; ++q) {
           const int32_t see = cut[q] - (int32_t)u.pos, last = (int32_t)u.hi(), lim = see < last ? see : last;
 #pragma unroll
           for (int jj = 0; jj < 2; ++jj)
@@ -434,7 +434,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       }
     }
 #pragma unroll
-    for (int q = 0; q < kRG; ++q) {
+    for (int q = 0; q < decltype(rgs)::value; ++q) {
       // keys past a row's causal limit or past the range: only in the
       // halves that reach min over rows of that limit
       if (!PAGED && decltype(masked)::value && kh + 32 > all_see) {
@@ -484,9 +484,9 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // Probabilities of a half as the A operand of P V: K slot e of lane group
   // kg is key 4kg + e (e < 4) or 16 + 4kg + (e - 4) of the half, the lane's
   // scores of its two 16-key blocks; high part and remainder.
-  auto split = [&](const float (&sc)[kRG][2][4], u32x4 (&pp)[kParts][kRG]) __attribute__((always_inline)) {
+  auto split = [&](auto rgs, const float (&sc)[kRG][2][4], u32x4 (&pp)[kParts][kRG]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int q = 0; q < kRG; ++q)
+    for (int q = 0; q < decltype(rgs)::value; ++q)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         uint32_t x[kParts];
@@ -543,7 +543,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // one: O += P V of half hv (two V blocks at a time), then the scores of half
   // hk of the tile in kb.  The fences keep the compiler from gathering the
   // reads in front of their uses again.
-  auto products = [&](const uint16_t* kb, int hk, const uint16_t* vb, int hv, bool do_pv, bool do_qk,
+  auto products = [&](auto rgs, const uint16_t* kb, int hk, const uint16_t* vb, int hv, bool do_pv, bool do_qk,
                       const u32x4 (&pp)[kParts][kRG], float (&sc)[kRG][2][4]) __attribute__((always_inline)) {
     constexpr int NP = C::kBlocks / 2;  // pairs of V blocks
     const uint16_t* vr0 = &vb[8 * ((4 * hv + (kg >> 1)) * (C::kRowChunks / 2) * 16 + (4 * (kg & 1) + (n16 >> 2)) * 2 +
@@ -570,7 +570,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
 #pragma unroll
           for (int bb = 0; bb < 2; ++bb)
 #pragma unroll
-            for (int q = 0; q < kRG; ++q) {
+            for (int q = 0; q < decltype(rgs)::value; ++q) {
               const int b = 2 * n + bb;
               f32x4 c = {o[q][b][0], o[q][b][1], o[q][b][2], o[q][b][3]};
               c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pp[part][q]),
@@ -601,19 +601,19 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
 #pragma unroll
       for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
-        for (int q = 0; q < kRG; ++q) acc[jj][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int q = 0; q < decltype(rgs)::value; ++q) acc[jj][q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < C::kChunks; ++u)
 #pragma unroll
         for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
-          for (int q = 0; q < kRG; ++q)
+          for (int q = 0; q < decltype(rgs)::value; ++q)
             acc[jj][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[u][jj]),
                                                                  __builtin_bit_cast(bf16x8, qb[q][u]), acc[jj][q], 0, 0, 0);
 #pragma unroll
       for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
-        for (int q = 0; q < kRG; ++q)
+        for (int q = 0; q < decltype(rgs)::value; ++q)
 #pragma unroll
           for (int v = 0; v < 4; ++v) sc[q][jj][v] = acc[jj][q][v];
     }
@@ -645,23 +645,23 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   float sc[kRG][2][4];
   u32x4 pp[kParts][kRG];
   constexpr int kWaitOne = 0x0F70 | C::kDma;  // vmcnt(kDma): the younger of two tiles may still be in flight
-  auto vphase = [&](auto masked, int64_t kh, const TileRun& u) __attribute__((always_inline)) {
-    softmax(masked, sc, kh, u);
-    split(sc, pp);
+  auto vphase = [&](auto masked, auto rgs, int64_t kh, const TileRun& u) __attribute__((always_inline)) {
+    softmax(masked, rgs, sc, kh, u);
+    split(rgs, sc, pp);
     if constexpr (PAGED) {
       // the parts are formed here, not sunk into the product phase
 #pragma unroll
       for (int part = 0; part < kParts; ++part)
 #pragma unroll
-        for (int q = 0; q < kRG; ++q) asm volatile("" : "+v"(pp[part][q]));
+        for (int q = 0; q < decltype(rgs)::value; ++q) asm volatile("" : "+v"(pp[part][q]));
     }
   };
   // P V first: the probabilities are dead before the new scores are formed
-  auto mphase = [&](const uint16_t* kb, int hk, const uint16_t* vb, int hv, bool do_pv) __attribute__((always_inline)) {
+  auto mphase = [&](auto rgs, const uint16_t* kb, int hk, const uint16_t* vb, int hv, bool do_pv) __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
     if constexpr (PAGED) {
-      if (do_pv) products(kb, hk, vb, hv, true, true, pp, sc);
-      else products(kb, hk, vb, hv, false, true, pp, sc);
+      if (do_pv) products(rgs, kb, hk, vb, hv, true, true, pp, sc);
+      else products(rgs, kb, hk, vb, hv, false, true, pp, sc);
     } else {
       if (do_pv) pv(vb, hv, pp);
       __builtin_amdgcn_sched_barrier(0);
@@ -703,13 +703,13 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // its own copy of the loop, so no phase branches on the group (a branch
   // gave the accumulators a second register set).  Both groups meet equally
   // often: every wave passes the same number of barriers.
-  auto one_tile = [&](auto masked, auto leadc, auto par) __attribute__((always_inline)) {
+  auto one_tile = [&](auto masked, auto leadc, auto rgs, auto par) __attribute__((always_inline)) {
     constexpr bool L = decltype(leadc)::value;
     constexpr int i = decltype(par)::value;  // tile t's parity
     // 4t + 1: lead: vector phase of half 2t; follow: P V of half 2t - 1, scores of 2t
     if (PAGED && L) read_runs(at);
-    if (L) vphase(masked, kt, run[i][0]);
-    else mphase(kbuf[i], 0, vbuf[1 - i], 1, i == 1 || kt != k_lo);
+    if (L) vphase(masked, rgs, kt, run[i][0]);
+    else mphase(rgs, kbuf[i], 0, vbuf[1 - i], 1, i == 1 || kt != k_lo);
     if (PAGED && L) take_runs(ahead);
     __builtin_amdgcn_s_waitcnt(kWaitOne);  // V of tile t
     meet();
@@ -717,14 +717,14 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
     else issue(vbase, voff, kt + kQKeys, vbuf[1 - i]);
     if (PAGED && !L) read_runs(at);
-    if (L) mphase(kbuf[i], 1, vbuf[i], 0, true);
-    else vphase(masked, kt, run[i][0]);
+    if (L) mphase(rgs, kbuf[i], 1, vbuf[i], 0, true);
+    else vphase(masked, rgs, kt, run[i][0]);
     if (PAGED && !L) take_runs(ahead);
     meet();
     // 4t + 3: lead: vector phase of 2t + 1; follow: P V of 2t, scores of 2t + 1
     const TileRun second = run[i][1];
-    if (L) vphase(masked, kt + 32, second);
-    else mphase(kbuf[i], 1, vbuf[i], 0, true);
+    if (L) vphase(masked, rgs, kt + 32, second);
+    else mphase(rgs, kbuf[i], 1, vbuf[i], 0, true);
     __builtin_amdgcn_s_waitcnt(kWaitOne);  // K of tile t + 1
     meet();
     // 4t + 4: lead: P V of 2t + 1, scores of 2t + 2; follow: vector phase of 2t + 1
@@ -736,14 +736,14 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     } else {
       issue(kbase, koff, kt + 2 * kQKeys, kbuf[i]);
     }
-    if (L) mphase(kbuf[1 - i], 0, vbuf[i], 1, true);
-    else vphase(masked, kt + 32, second);
+    if (L) mphase(rgs, kbuf[1 - i], 0, vbuf[i], 1, true);
+    else vphase(masked, rgs, kt + 32, second);
     meet();
     kt += kQKeys;
   };
-  auto tile_pair = [&](auto masked, auto leadc) __attribute__((always_inline)) {
-    one_tile(masked, leadc, std::integral_constant<int, 0>{});
-    one_tile(masked, leadc, std::integral_constant<int, 1>{});
+  auto tile_pair = [&](auto masked, auto leadc, auto rgs) __attribute__((always_inline)) {
+    one_tile(masked, leadc, rgs, std::integral_constant<int, 0>{});
+    one_tile(masked, leadc, rgs, std::integral_constant<int, 1>{});
   };
   // Between two pairs of tiles nobody reads the table: the last reads were two
   // meetings ago.
@@ -753,18 +753,18 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     meet();
     at = 0;
   };
-  auto walk = [&](auto leadc) __attribute__((always_inline)) {
+  auto walk = [&](auto leadc, auto rgs) __attribute__((always_inline)) {
     constexpr bool L = decltype(leadc)::value;
-    if (L) mphase(kbuf[0], 0, vbuf[0], 0, false);  // scores of half 0
+    if (L) mphase(rgs, kbuf[0], 0, vbuf[0], 0, false);  // scores of half 0
     meet();
     if constexpr (!PAGED)
-      for (int64_t rd = 0; rd < nclear; ++rd) tile_pair(std::false_type{}, leadc);
+      for (int64_t rd = 0; rd < nclear; ++rd) tile_pair(std::false_type{}, leadc, rgs);
     for (int64_t rd = nclear; rd < nround; ++rd) {
       if (PAGED && at + 4 > kTableRuns) next_table();
-      tile_pair(std::true_type{}, leadc);
+      tile_pair(std::true_type{}, leadc, rgs);
     }
     if (PAGED && odd) {
-      one_tile(std::true_type{}, leadc, std::integral_constant<int, 0>{});
+      one_tile(std::true_type{}, leadc, rgs, std::integral_constant<int, 0>{});
       if (!L) pv(vbuf[0], 1, pp);
       return;
     }
@@ -799,8 +799,9 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     if (odd) none(std::integral_constant<int, 0>{});
   };
   if (PAGED && qt * kQRows + 16 * kRG * wave_u >= rows) attend_none();
-  else if (lead) walk(std::true_type{});
-  else walk(std::false_type{});
+  else if (PAGED && qt * kQRows + 16 >= rows) walk(std::true_type{}, std::integral_constant<int, 1>{});
+  else if (lead) walk(std::true_type{}, std::integral_constant<int, kRG>{});
+  else walk(std::false_type{}, std::integral_constant<int, kRG>{});
   // no direct load may still be writing LDS when the workgroup ends
   __builtin_amdgcn_s_waitcnt(0x0F70);
 
@@ -912,7 +913,7 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
 // 700 207 / 188, 32 of 512 241 / 224).
 // ---------------------------------------------------------------------------
 constexpr int kUnitTiles = 2;
-constexpr int kTileCost = 4, kHalfCost = 3;
+constexpr int kTileCost = 4, kHalfCost = 3, kThinCost = 2;
 constexpr int kWholeTiles = 10, kWholeMean = 8;
 constexpr int kSortBuckets = 1024;
 
@@ -1031,7 +1032,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
       const int g = in / tiles, qt = in - g * tiles;
       const int s = lo * p.Hkv + g;
       const int32_t rows = unit_rows(p, blk[lo], s, qt);
-      const int32_t cost = (int64_t)blk[lo].n * p.G - (int64_t)qt * kQRows <= kQRows / 2 ? kHalfCost : kTileCost;
+      const int64_t left = (int64_t)blk[lo].n * p.G - (int64_t)qt * kQRows;
+      const int32_t cost = left <= 16 ? kThinCost : (left <= kQRows / 2 ? kHalfCost : kTileCost);
       plan.unit[u] = PagedUnit{s, qt, rows, cost, blk[lo], 0};
       mine = (unit_tiles(rows) + kUnitTiles) * cost;  // below 2^27
       most = max(most, (int32_t)mine);
