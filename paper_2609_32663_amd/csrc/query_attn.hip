@@ -214,14 +214,17 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // where the block starts in the token-major arrays
   const int64_t tok_row0 = PAGED ? (int64_t)blk.tok0 : (int64_t)bseq * p.n_q;
 
+  // Paged: up to 128 rows are spread over the waves, one row group each.
+  const bool spread = PAGED && rows - qt * kQRows <= kQRows / 2;
+  const int wave_rows = spread ? 16 : 16 * kRG;
   // this lane's query rows (one per row group) in the score layout, and the keys they see
   int r[kRG], tok[kRG];
   bool row_ok[kRG];
   int64_t limit[kRG];
 #pragma unroll
   for (int q = 0; q < kRG; ++q) {
-    r[q] = qt * kQRows + wave * 16 * kRG + 16 * q + n16;
-    row_ok[q] = r[q] < rows;
+    r[q] = qt * kQRows + wave * wave_rows + 16 * q + n16;
+    row_ok[q] = r[q] < rows && 16 * q < wave_rows;
     tok[q] = row_ok[q] ? r[q] / p.G : 0;
     limit[q] = base_len + tok[q] + 1;
   }
@@ -414,7 +417,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // spread by 1 to 2 us on either side; taking the bf16 remainders by dot products
   // as well, 16 instructions fewer per half, gave nothing: the kernel runs at the
   // power limit).
-  const int32_t pos_all = PAGED ? paged_pos(blk, min(qt * kQRows + 16 * kRG * wave_u, rows - 1) / p.G) + 1 : 0;
+  const int32_t pos_all = PAGED ? paged_pos(blk, min(qt * kQRows + wave_rows * wave_u, rows - 1) / p.G) + 1 : 0;
   auto softmax = [&](auto masked, auto rgs, float (&sc)[kRG][2][4], int64_t kh, const TileRun& u) __attribute__((always_inline)) {
     if constexpr (PAGED) {
       // slots outside the entry, or past the position of one of the wave's rows
@@ -504,7 +507,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // ((4h + kg / 2) * kRowChunks / 2 + b) * 16 + (4 (kg % 2) + r) * 2 + q / 2.
   // Two V blocks at a time: the high parts of both, then the remainders, so
   // a product never waits for the one just before it.
-  auto pv = [&](const uint16_t* vb, int h, const u32x4 (&pp)[kParts][kRG]) __attribute__((always_inline)) {
+  auto pv = [&](auto rgs, const uint16_t* vb, int h, const u32x4 (&pp)[kParts][kRG]) __attribute__((always_inline)) {
     const uint16_t* vr0 = &vb[8 * ((4 * h + (kg >> 1)) * (C::kRowChunks / 2) * 16 + (4 * (kg & 1) + (n16 >> 2)) * 2 +
                                    ((n16 >> 1) & 1)) + 4 * (n16 & 1)];
 #pragma unroll
@@ -525,7 +528,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
 #pragma unroll
         for (int bb = 0; bb < 2; ++bb)
 #pragma unroll
-          for (int q = 0; q < kRG; ++q) {
+          for (int q = 0; q < decltype(rgs)::value; ++q) {
             const int b = b0 + bb;
             f32x4 c = {o[q][b][0], o[q][b][1], o[q][b][2], o[q][b][3]};
             c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pp[part][q]),
@@ -663,7 +666,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       if (do_pv) products(rgs, kb, hk, vb, hv, true, true, pp, sc);
       else products(rgs, kb, hk, vb, hv, false, true, pp, sc);
     } else {
-      if (do_pv) pv(vb, hv, pp);
+      if (do_pv) pv(rgs, vb, hv, pp);
       __builtin_amdgcn_sched_barrier(0);
       qk(kb, hk, sc);
     }
@@ -765,12 +768,12 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     }
     if (PAGED && odd) {
       one_tile(std::true_type{}, leadc, rgs, std::integral_constant<int, 0>{});
-      if (!L) pv(vbuf[0], 1, pp);
+      if (!L) pv(rgs, vbuf[0], 1, pp);
       return;
     }
     // the follow group's P V products of the last half (tiles past k_hi hold
     // zeros and all their keys are masked, so the lead's last scores are unused)
-    if (!L && nround > 0) pv(vbuf[1], 1, pp);
+    if (!L && nround > 0) pv(rgs, vbuf[1], 1, pp);
   };
   // Paged: waves without rows (a sequence of few tokens) load and meet only;
   // the others then have the matrix units and the power to themselves.
@@ -798,8 +801,9 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     }
     if (odd) none(std::integral_constant<int, 0>{});
   };
-  if (PAGED && qt * kQRows + 16 * kRG * wave_u >= rows) attend_none();
-  else if (PAGED && qt * kQRows + 16 >= rows) walk(std::true_type{}, std::integral_constant<int, 1>{});
+  if (PAGED && qt * kQRows + wave_rows * wave_u >= rows) attend_none();
+  else if (spread && lead) walk(std::true_type{}, std::integral_constant<int, 1>{});
+  else if (spread) walk(std::false_type{}, std::integral_constant<int, 1>{});
   else if (lead) walk(std::true_type{}, std::integral_constant<int, kRG>{});
   else walk(std::false_type{}, std::integral_constant<int, kRG>{});
   // no direct load may still be writing LDS when the workgroup ends
@@ -812,11 +816,11 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     l[q] = lane_xor_sum<16>(l[q]);
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      const int rr = wave * 16 * kRG + 16 * q + 4 * kg + v;  // row within the tile
+      const int rr = wave * wave_rows + 16 * q + 4 * kg + v;  // row within the tile
       const int rq = qt * kQRows + rr;
       const float lq = __shfl(l[q], 4 * kg + v, 64);
       const float mq = __shfl(m[q], 4 * kg + v, 64);
-      if (rq < rows) {
+      if (rq < rows && 16 * q < wave_rows) {
         if (item.single) {
           const int tq = rq / p.G;
           float* orow = p.out + ((tok_row0 + tq) * p.Hq + (int64_t)g * p.G + (rq - tq * p.G)) * D;
@@ -1033,7 +1037,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
       const int s = lo * p.Hkv + g;
       const int32_t rows = unit_rows(p, blk[lo], s, qt);
       const int64_t left = (int64_t)blk[lo].n * p.G - (int64_t)qt * kQRows;
-      const int32_t cost = left <= 16 ? kThinCost : (left <= kQRows / 2 ? kHalfCost : kTileCost);
+      const int32_t cost = left <= 64 ? kThinCost : (left <= kQRows / 2 ? kHalfCost : kTileCost);
       plan.unit[u] = PagedUnit{s, qt, rows, cost, blk[lo], 0};
       mine = (unit_tiles(rows) + kUnitTiles) * cost;  // below 2^27
       most = max(most, (int32_t)mine);
