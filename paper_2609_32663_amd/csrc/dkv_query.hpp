@@ -114,19 +114,24 @@ hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, h
 // Whether the kernels for short blocks take a paged call, whose longest block has
 // `rows` query rows per segment; query tiles / short, us, attention with plan
 // and combine, 128-row pages.
-//   * Up to 64 rows: always (64 rows: 128 segments of 1,000 keys 47 / 46, of 4,000
-//     94 / 89).
-//   * Up to 128 rows: but for many segments of few keys (64 query heads on 8,
-//     128 rows: 128 segments of 1,000 keys 52 / 72, 64 of 4,000 65 / 70, 256 of
-//     4,000 167 / 150, 8 of 130,000 153 / 139; 64 dimensions, 128 of 1,000 38 / 65).
-//   * More rows: few segments and keys, where the plan and a tile's chain of
-//     phases weigh most (28 heads on 4, 252 rows: 4 of 1,000 35 / 30, of 65,000
-//     91 / 88, of 130,000 128 / 134; 64 on 8, 256 rows: 8 of 16,000 62 / 55, of 65,000
-//     119 / 141; 32 of 4,000 with 133 rows 52 / 60).
+//   * Up to 32 rows: always (32 rows: 256 segments of 1,000 keys 41 / 38, 64 of
+//     16,000 119 / 98).  The stream is the bound, and one wave's.
+//   * Up to 128 rows: few segments or keys, where the plan and a tile's chain of
+//     phases weigh most; the query tiles spread the rows over all waves (64 query
+//     heads on 8, 64 rows: 8 segments of 16,000 keys 43 / 31, of 60,000 65 / 67; 32
+//     of 1,000 33 / 25, of 4,000 37 / 35, of 16,000 72 / 78; 64 of 1,000 37 / 33, of 4,000
+//     49 / 55; 128 of 1,000 41 / 48; 128 rows: 16 of 16,000 62 / 59, of 60,000 138 /
+//     148; 32 of 1,000 37 / 35, of 4,000 43 / 47; 128 of 300 41 / 33, of 1,000 48 / 72;
+//     256 of 100 43 / 19, of 1,000 54 / 60).
+//   * More rows: fewer still (28 heads on 4, 252 rows: 4 of 1,000 35 / 31, of 65,000
+//     91 / 89; 64 on 8, 256 rows: 8 of 16,000 63 / 59, of 65,000 122 / 151; 16 of
+//     4,000 54 / 49, of 16,000 84 / 93; 32 of 1,000 49 / 53).
 inline bool paged_takes_short(int64_t nseg, int64_t rows, int64_t rows_hint) {
-  if (rows <= kShortRows / 4) return true;
-  if (rows <= kShortRows / 2) return nseg < kShortManySegments || rows_hint <= 0 || rows_hint / kShortFewKeys >= nseg;
-  return rows <= kShortRows && nseg <= 8 && rows_hint > 0 && rows_hint <= 1 << 18;
+  if (rows <= kShortRows / 8) return true;
+  if (rows <= kShortRows / 2)
+    return (nseg <= 16 && rows_hint < 1 << 18) || (nseg * rows <= 4096 && rows_hint <= 1 << 17) ||
+           (nseg <= 256 && rows_hint <= 1 << 16);
+  return rows <= kShortRows && nseg <= 16 && rows_hint > 0 && rows_hint <= 1 << 17;
 }
 
 // How a paged call is split: the most units ((segment, query tile) pairs) it
