@@ -721,7 +721,7 @@ size_t dkv_paged_query_workspace_bytes(int32_t batch, int32_t num_q_heads, int32
  *           required, or NULL when that is 0.
  * Scores, maxima and sums are fp32; a probability enters its product with V as
  * three bf16 parts (24 bits); in chunks of more query rows per KV head than the
- * short-block kernels take (64 to 256, by the segments' number and length), as
+ * short-block kernels take (32 to 256, by the segments' number and length), as
  * two (17 bits) for rows that see over 32,768 slots.
  * The call enqueues one kernel without a workspace; with one, an attention and
  * a combine kernel, and a plan kernel before them for such chunks.

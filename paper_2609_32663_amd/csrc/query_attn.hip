@@ -214,7 +214,9 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // where the block starts in the token-major arrays
   const int64_t tok_row0 = PAGED ? (int64_t)blk.tok0 : (int64_t)bseq * p.n_q;
 
-  // Paged: up to 128 rows are spread over the waves, one row group each.
+  // Paged: up to 128 rows are spread over the waves, one row group each: a wave's
+  // phases halve, and they bound a tile of few rows (32 sequences of 8,000 keys:
+  // 32 rows 264 -> 198 us, 64 278 -> 224, 128 324 -> 309).
   const bool spread = PAGED && rows - qt * kQRows <= kQRows / 2;
   const int wave_rows = spread ? 16 : 16 * kRG;
   // this lane's query rows (one per row group) in the score layout, and the keys they see
@@ -895,9 +897,10 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
 // Paged calls.  A unit is one query tile of one segment (of a sequence's own
 // number of them); its length is the cost of its key tiles (up to what its last
 // row sees) and kUnitTiles more for what it takes by itself.  A tile costs
-// kHalfCost where only the lead waves have rows (at most 128), which leaves a
-// SIMD to one wave, and else kTileCost: 32 sequences of 8,000 keys, 8 heads, walked
-// at 2.1 us a tile with 4 to 64 rows, 2.4 with 128, 3.1 with 160, 3.8 with 256.
+// kThinCost with up to 64 rows (one row group in each lead wave), kHalfCost with
+// up to 128 (one in every wave), and else kTileCost: 32 sequences of 8,000 keys, 8
+// heads, walked at 1.55 us a tile with 4 to 32 rows, 1.75 with 64, 2.2 with 96, 2.4
+// with 128, 3.1 with 160, 3.7 with 256.
 // The lengths of all units, laid end to end, are cut into P equal slices (up to
 // the next whole tile), one per workgroup: however unequal the chunks and the
 // contexts, every workgroup has the same work and all run at once.  A unit that
