@@ -188,7 +188,7 @@ def _rows(t, name, heads, dim, dtype):
 
 def _typed(t, name, dtype, count=None, shape=None):
     """_dev of a tensor of this element type (and number of elements, or shape)."""
-    if (type(t) is _Tensor and t.dtype is dtype and t.is_cuda and t.is_contiguous()
+    if ((type(t) is _Tensor or isinstance(t, _Tensor)) and t.dtype is dtype and t.is_cuda and t.is_contiguous()
             and (count is None or t.numel() == count) and (shape is None or t.shape == shape)):
         return t.data_ptr()
     _dev(t, name)
@@ -520,7 +520,7 @@ def dkv_paged_append(k_new, v_new, slots, k_pages, v_pages, stream=None):
     tokens, Hkv = slots.shape
     dtype = k_pages.dtype
     k_ptr, stride = _rows(k_new, "k_new", Hkv, dim, dtype)
-    if (type(v_new) is not _Tensor or v_new.dtype is not dtype or not v_new.is_cuda or v_new.shape != k_new.shape
+    if (not isinstance(v_new, _Tensor) or v_new.dtype is not dtype or not v_new.is_cuda or v_new.shape != k_new.shape
             or (v_new.stride() != k_new.stride() and tokens > 1) or k_new.shape[0] != tokens):
         raise ValueError("k_new and v_new must be device tensors alike, with a row per row of slots, evenly spaced alike")
     v_ptr, _ = (v_new.data_ptr(), stride) if tokens > 1 else _rows(v_new, "v_new", Hkv, dim, dtype)

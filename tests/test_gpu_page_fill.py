@@ -240,3 +240,13 @@ def test_requests_come_grow_and_go(d):
         table, stack, entries, counts = want["table"], want["stack"], want["entries"], want["n_entries"]
         length = want["new_len"].astype(np.int64)
         np.testing.assert_array_equal(x.stack.cpu().numpy()[:len(stack)], stack)
+
+
+def test_pools_that_are_parameters(d):
+    """A subclass of Tensor is a tensor."""
+    pool = torch.nn.Parameter(torch.zeros((3, 32, 64), device=DEV), requires_grad=False)
+    other = torch.nn.Parameter(torch.zeros((3, 32, 64), device=DEV), requires_grad=False)
+    x = torch.nn.Parameter(torch.ones((2, 1, 64), device=DEV), requires_grad=False)
+    d.dkv_paged_append(x, x, _dev([[5], [70]], torch.int64), pool, other)
+    for p in (pool, other):
+        assert p.view(96, 64)[[5, 70]].eq(1).all() and float(p.sum()) == 128.0
