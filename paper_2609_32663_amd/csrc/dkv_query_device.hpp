@@ -103,8 +103,10 @@ __device__ __forceinline__ int32_t paged_pos(const PagedBlock& k, int32_t t) {
 // whole runs.  It sees slots of all entries, or, when the one after that
 // position's page number starts behind it (as in an unpruned cache), of the
 // ones before that; and the last of them up to its end or that position (half a
-// page less to walk on average).
-__device__ __forceinline__ int32_t paged_rows(const QueryParams& p, int s, int32_t last) {
+// page less to walk on average).  `gaps`: whether there may be slots of no key
+// among them, as a selection's runs leave (not where the last entry seen is
+// that of its page in a cache without any).
+__device__ __forceinline__ int32_t paged_rows(const QueryParams& p, int s, int32_t last, bool* gaps) {
   const int32_t x = last >> p.page_shift;
   const i32x4* list = reinterpret_cast<const i32x4*>(p.entries) + (int64_t)s * p.max_entries;
   // an unpruned cache's last entry is x: these loads wait for nothing
@@ -113,6 +115,7 @@ __device__ __forceinline__ int32_t paged_rows(const QueryParams& p, int s, int32
   i32x4 e = list[x < p.max_entries ? x : 0];
   const int32_t all = n < 0 ? 0 : (n > p.max_entries ? p.max_entries : n);
   const int32_t held = x + 1 < all && page > x ? x + 1 : all;
+  *gaps = held != x + 1 || e[1] != x;
   if (held == 0) return 0;
   if (held != x + 1) e = list[held - 1];
   // positions from 2^31 on are beyond every token

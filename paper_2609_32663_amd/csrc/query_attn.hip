@@ -143,6 +143,7 @@ struct QueryItem {
   float* rec;
   PagedBlock blk;  // paged: the sequence's block, and the segment's rows that the tile's rows see
   int32_t seen;
+  bool gaps;  // among them may be slots of no key
 };
 
 // Paged: the next kTableRuns runs of a segment's rows, decoded side by side into
@@ -170,7 +171,7 @@ __device__ __forceinline__ u32x4 tile_run_word(const PagedRun& u, int row_bytes)
 // kParts: bf16 parts of a probability.
 template <int D, bool PAGED, int kParts>
 __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem& item, uint16_t* k0, uint16_t* k1,
-                                           uint16_t* v0, uint16_t* v1, u32x4* table) {
+                                           uint16_t* v0, uint16_t* v1, u32x4* table, int* counts) {
   using C = QCfg<D>;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -340,6 +341,32 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       }
       table[i] = w;
     }
+  };
+  // The runs with slots moved to the table's front, in order; returns their
+  // number (256 tokens over the 35% of 131,072 positions that a selection kept,
+  // in 128-row pages 283 -> 275 us, in 256-row pages 314 -> 280, in 1,024-row pages
+  // 531 -> 317; a unit of whole pages, without gaps, pays 1.5 us for the branch).  A word moves
+  // to its own index or a lower one, after the words up to it have been read.
+  auto drop_gaps = [&](int n) __attribute__((always_inline)) {
+    int at = 0;
+    for (int i0 = 0, turn = 0; i0 < n; i0 += kQThreads, turn ^= 1) {
+      const int i = i0 + tid;
+      u32x4 w = {0u, 0u, 0u, 0u};
+      if (i < n) w = table[i];
+      const uint64_t some = __builtin_amdgcn_ballot_w64(w[3] != 0u);
+      if (lane == 0) counts[8 * turn + wave] = __popcll(some);
+      __syncthreads();
+      int to = at;
+      for (int k = 0; k < kQThreads / kWave; ++k) {
+        const int c = counts[8 * turn + k];
+        to += k < wave ? c : 0;
+        at += c;
+      }
+      if (w[3] != 0u) table[to + __popcll(some & ((1ull << lane) - 1))] = w;
+    }
+    __syncthreads();
+    if (tid < kTablePad) table[at + tid] = u32x4{0u, 0u, 0u, 0u};
+    return __builtin_amdgcn_readfirstlane(at);
   };
   auto read_runs = [&](int at) __attribute__((always_inline)) {
     coming[0] = table[at];
@@ -674,9 +701,14 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     }
     __builtin_amdgcn_s_setprio(0);
   };
+  int32_t live = -1;  // paged: runs with slots, where they are known
   if constexpr (PAGED) {
     fill_table(k_lo);
     __syncthreads();
+    if (item.gaps && k_hi - k_lo <= kTableRuns * kRun) {
+      live = drop_gaps((int)((k_hi - k_lo + kRun - 1) / kRun));
+      __syncthreads();
+    }
     read_runs(0);
     take_runs(run[0]);
     read_runs(2);
@@ -691,7 +723,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
   __syncthreads();
-  const int64_t ntile = k_hi > k_lo ? (k_hi - k_lo + kQKeys - 1) / kQKeys : 0;
+  const int64_t ntile = PAGED && live >= 0 ? (live + 1) / 2 : (k_hi > k_lo ? (k_hi - k_lo + kQKeys - 1) / kQKeys : 0);
   const int64_t nround = q_uniform64((ntile + (PAGED ? 0 : 1)) / 2);
   const bool odd = PAGED && (ntile & 1) != 0;  // a last tile without a second
   int at = 4;  // paged: where the table holds the tile whose K is loaded next
@@ -890,7 +922,7 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
     t_hi = (int64_t)(r + 1) * tiles / nr;
   }
   query_item<D, false, 2>(p, QueryItem{s, qt, t_lo, t_hi, single, p.rec + (int64_t)item * kQRows * QCfg<D>::kRec,
-                                       PagedBlock{0, 0, 0}, 0}, k0, k1, v0, v1, nullptr);
+                                       PagedBlock{0, 0, 0}, 0, false}, k0, k1, v0, v1, nullptr, nullptr);
 }
 
 // ---------------------------------------------------------------------------
@@ -929,7 +961,7 @@ struct PagedUnit {
   int32_t rows;  // of the segment, up to the last that the tile sees
   int32_t cost;  // of a key tile
   PagedBlock blk;
-  int32_t pad;
+  int32_t gaps;
 };
 
 // Words of the plan: slices and units, whether units stay whole,
@@ -975,10 +1007,11 @@ __device__ __forceinline__ int64_t unit_tiles(int32_t rows) {
 }
 
 // Rows of segment s that query tile qt of a block sees.
-__device__ __forceinline__ int32_t unit_rows(const QueryParams& p, const PagedBlock& k, int s, int qt) {
+__device__ __forceinline__ int32_t unit_rows(const QueryParams& p, const PagedBlock& k, int s, int qt, bool* gaps) {
+  *gaps = false;
   if (k.pos0 < 0 || p.max_entries == 0) return 0;
   const int64_t last = (int64_t)(qt + 1) * kQRows < (int64_t)k.n * p.G ? (int64_t)(qt + 1) * kQRows : (int64_t)k.n * p.G;
-  return paged_rows(p, s, paged_pos(k, (int32_t)((last - 1) / p.G)));
+  return paged_rows(p, s, paged_pos(k, (int32_t)((last - 1) / p.G)), gaps);
 }
 
 // One workgroup; bound by the chain of its dependent reads (offsets, counts)
@@ -1038,10 +1071,11 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
       const int in = (int)(u - (int64_t)pre[lo] * p.Hkv);
       const int g = in / tiles, qt = in - g * tiles;
       const int s = lo * p.Hkv + g;
-      const int32_t rows = unit_rows(p, blk[lo], s, qt);
+      bool gaps;
+      const int32_t rows = unit_rows(p, blk[lo], s, qt, &gaps);
       const int64_t left = (int64_t)blk[lo].n * p.G - (int64_t)qt * kQRows;
       const int32_t cost = left <= 64 ? kThinCost : (left <= kQRows / 2 ? kHalfCost : kTileCost);
-      plan.unit[u] = PagedUnit{s, qt, rows, cost, blk[lo], 0};
+      plan.unit[u] = PagedUnit{s, qt, rows, cost, blk[lo], gaps};
       mine = (unit_tiles(rows) + kUnitTiles) * cost;  // below 2^27
       most = max(most, (int32_t)mine);
     }
@@ -1171,6 +1205,7 @@ template <int D>
 __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
   DKV_QUERY_TILES(D);
   __shared__ __align__(16) u32x4 table[kTableRuns + kTablePad];
+  __shared__ int counts[2 * kQThreads / kWave];  // runs with slots, per wave
   __shared__ PagedUnit own[kWholeRounds];  // whole units: this workgroup's
   // Without a plan (too few keys to split) one workgroup per (segment, query
   // tile): the loop's only unit.
@@ -1208,6 +1243,7 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.s = unit.s;
       x.qt = unit.qt;
       x.seen = unit.rows;
+      x.gaps = __builtin_amdgcn_readfirstlane(unit.gaps) != 0;
       x.blk = unit.blk;
       x.t_lo = 0;
       x.t_hi = unit_tiles(unit.rows);
@@ -1226,6 +1262,7 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.s = __builtin_amdgcn_readfirstlane(unit.s);
       x.qt = __builtin_amdgcn_readfirstlane(unit.qt);
       x.seen = __builtin_amdgcn_readfirstlane(unit.rows);
+      x.gaps = __builtin_amdgcn_readfirstlane(unit.gaps) != 0;
       x.blk = unit.blk;
       x.t_lo = (uint32_t)(a - from) / (uint32_t)cost;  // below 2^27
       x.t_hi = (uint32_t)(b - from) / (uint32_t)cost;
@@ -1237,14 +1274,16 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.qt = blockIdx.x - x.s * p.qtiles;
       x.blk = paged_block(p, x.s / p.Hkv);
       if ((int64_t)x.qt * kQRows >= (int64_t)x.blk.n * p.G) return;
-      x.seen = __builtin_amdgcn_readfirstlane(unit_rows(p, x.blk, x.s, x.qt));
+      bool gaps;
+      x.seen = __builtin_amdgcn_readfirstlane(unit_rows(p, x.blk, x.s, x.qt, &gaps));
+      x.gaps = __builtin_amdgcn_readfirstlane(gaps ? 1 : 0) != 0;
       x.t_lo = 0;
       x.t_hi = unit_tiles(x.seen);
       x.single = true;
       x.rec = nullptr;
     }
-    if (__builtin_amdgcn_readfirstlane(x.seen) <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1, table);
-    else query_item<D, true, 2>(p, x, k0, k1, v0, v1, table);
+    if (__builtin_amdgcn_readfirstlane(x.seen) <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1, table, counts);
+    else query_item<D, true, 2>(p, x, k0, k1, v0, v1, table, counts);
     __syncthreads();  // the tile buffers are free for the next unit
   }
 }

@@ -78,7 +78,8 @@ __device__ __forceinline__ int64_t short_units(const QueryParams& p, int s) {
     // tokens of 1,100 positions, pages of 1,024: 161 us whole, 124; 256: 126.5 and
     // 124.1); of small pages whole, as the look costs another round trip to memory
     // (32 of 5,000, pages of 128: 110.0 and 111.2).
-    if (p.page_shift >= 8) return paged_rows(p, s, paged_pos(k, k.n - 1)) / kRun;
+    bool gaps;
+    if (p.page_shift >= 8) return paged_rows(p, s, paged_pos(k, k.n - 1), &gaps) / kRun;
     const int32_t n = p.n_entries[s];
     return n < 0 ? 0 : (int64_t)(n > p.max_entries ? p.max_entries : n) << (p.page_shift - 5);
   }

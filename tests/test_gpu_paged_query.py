@@ -569,3 +569,15 @@ def test_a_padded_batch_replayed_with_other_lengths(d, n):
         b.max_q = n
         err = row_rel_err(got.reshape(-1, 128), b.want().reshape(-1, 128))
         assert np.isfinite(got).all() and err <= np.sqrt(3100) * 2.0 ** -17, (i, err)
+
+
+@pytest.mark.parametrize("dim,R", [(64, 256), (128, 1024), (128, 32)])
+@pytest.mark.parametrize("keep,new,held", [(0.3, [20, 17], 9000), (0.02, [150, 3], 9000), (0.5, [18], 70000),
+                                           (0.9, [40] * 12, 600)])
+def test_query_tiles_over_a_selection(d, dim, R, keep, new, held):
+    """Runs without slots between the kept ones, in ranges that fit a table of runs and in longer ones."""
+    rng = np.random.default_rng([dim, R, held, len(new)])
+    x = Batch(rng, [held] * len(new), new, 1, 16, dim, R, keep=keep, pad=1)
+    got = x.check(d)
+    whole = x.run(d, hint=1).cpu().numpy()
+    assert row_rel_err(whole.reshape(-1, dim), got.reshape(-1, dim)) <= np.sqrt(x.keys) * 2.0 ** -17
