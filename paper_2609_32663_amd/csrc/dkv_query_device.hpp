@@ -163,7 +163,8 @@ __device__ __forceinline__ PagedRun paged_run(const PagedSegment& g, const i32x4
   const int32_t slot = r & ((1 << g.shift) - 1);
   // without branches: a chain of scalar selects
   const bool ok = (r < g.end) & ((uint32_t)x.x < (uint32_t)g.pages) &
-                  ((uint32_t)x.y <= (uint32_t)(INT32_MAX - 1) >> g.shift) & (x.z >= 0) & (x.w <= (1 << g.shift));
+                  ((uint32_t)x.y <= (uint32_t)(INT32_MAX - 1) >> g.shift) & (x.z >= 0) &
+                  ((uint32_t)x.w <= 1u << g.shift);  // 0 <= x.w: no difference below wraps
   PagedRun u;
   u.row = ok ? ((int64_t)x.x << g.shift) + slot : 0;
   u.pos = ok ? (x.y << g.shift) + slot : 0;
