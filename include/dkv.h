@@ -720,11 +720,11 @@ size_t dkv_paged_query_workspace_bytes(int32_t batch, int32_t num_q_heads, int32
  * workspace dkv_paged_query_workspace_bytes(...) bytes, no initial contents
  *           required, or NULL when that is 0.
  * Scores, maxima and sums are fp32; a probability enters its product with V as
- * three bf16 parts (24 bits); in chunks of more query rows per KV head than the
- * short-block kernels take (32 to 256, by the segments' number and length), as
- * two (17 bits) for rows that see over 32,768 slots.
+ * three bf16 parts (24 bits).
  * The call enqueues one kernel without a workspace; with one, an attention and
- * a combine kernel, and a plan kernel before them for such chunks.
+ * a combine kernel, and a plan kernel before them in chunks of more query rows
+ * per KV head than the short-block kernels take (32 to 256, by the segments'
+ * number and length).
  * Only DKV_BF16 is supported (DKV_ERR_UNSUPPORTED otherwise); head_dim 64 or
  * 128; DKV_ERR_UNSUPPORTED also when max_entries * page_rows > 2^30 or a
  * dispatch would exceed 2^32 work-items.

@@ -49,11 +49,11 @@
 // for sequences whose chunks differ in length: the split into slices and the
 // kernel that plans it are described further down, tile addresses come from a
 // table of 32-row runs in LDS, the products of a phase are one pipeline of LDS
-// reads and matrix instructions, and a probability has two or three bf16 parts.
-// With three a workgroup takes 6,540 cycles for a 64-key tile, of which its
-// matrix instructions fill 4,096: 512 tokens of an 8B layer over 32K keys, two
-// parts, 349 us (794 TFLOP/s of the 4 d flops per query row and key, 1,190 with
-// the second part's), two prompts of 4K, three parts, 262 us (563 and 1,126).
+// reads and matrix instructions, and a probability has three bf16 parts.  A
+// workgroup takes 6,540 cycles for a 64-key tile, of which its matrix
+// instructions fill 4,096: 512 tokens of an 8B layer over 32K keys 423 us (655
+// TFLOP/s of the 4 d flops per query row and key, 1,310 with the further
+// parts'), two prompts of 4K 261 us (565 and 1,130).
 //
 // This file is compiled with IEEE mode off and no NaN semantics
 // (-mno-amdgpu-ieee -fno-honor-nans): the maxima then need no NaN
@@ -168,11 +168,18 @@ __device__ __forceinline__ u32x4 tile_run_word(const PagedRun& u, int row_bytes)
                (uint32_t)((u.hi() - u.lo()) * row_bytes)};
 }
 
-// kParts: bf16 parts of a probability.
-template <int D, bool PAGED, int kParts>
+template <int D, bool PAGED>
 __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem& item, uint16_t* k0, uint16_t* k1,
                                            uint16_t* v0, uint16_t* v1, u32x4* table, int* counts) {
   using C = QCfg<D>;
+  // bf16 parts of a probability.  Packed: two, 17 bits.  Paged: three, its 24
+  // bits, at any length: two err by 2.1e-6 to 2.5e-6 of the output's norm at
+  // 1,000 keys as at 131,072, three by 2.0e-7 to 5.2e-7, attention in plain fp32
+  // by 3.3e-7 to 4.0e-6 (q, K, V Gaussian; 64 dimensions at 131,072 keys 2.5e-6,
+  // 5.2e-7 and 1.8e-6).  The third product costs what it computes, as the kernel
+  // runs at the rate that the matrix units reach under the power limit (two / three
+  // parts, us, 8B layer: 512 tokens at 32K 349 / 423, 256 over 45K rows 277 / 330).
+  constexpr int kParts = PAGED ? 3 : 2;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = tid >> 6;
@@ -921,7 +928,7 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
     t_lo = (int64_t)r * tiles / nr;
     t_hi = (int64_t)(r + 1) * tiles / nr;
   }
-  query_item<D, false, 2>(p, QueryItem{s, qt, t_lo, t_hi, single, p.rec + (int64_t)item * kQRows * QCfg<D>::kRec,
+  query_item<D, false>(p, QueryItem{s, qt, t_lo, t_hi, single, p.rec + (int64_t)item * kQRows * QCfg<D>::kRec,
                                        PagedBlock{0, 0, 0}, 0, false}, k0, k1, v0, v1, nullptr, nullptr);
 }
 
@@ -1192,15 +1199,6 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
   if (tid == 0) plan.head[3] = nshared;
 }
 
-// A probability is used as three bf16 parts, its 24 bits, where the query rows
-// see at most this many rows, and as two, 17 bits, beyond.  The kernel runs at
-// the rate that the matrix units reach under the power limit, so the third
-// product costs what it computes (512 tokens at 32K 344 us with two parts, 416
-// with three; 256 tokens over 45K rows 239 and 289).  Two parts err by 2.6e-6
-// of the output's norm at any length, three by 1.7e-7 at 1K keys and 1.0e-6 at
-// 32K; attention in plain fp32 by 2.8e-7 and 2.3e-6.
-constexpr int32_t kThreePartRows = 32768;
-
 template <int D>
 __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
   DKV_QUERY_TILES(D);
@@ -1282,8 +1280,7 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.single = true;
       x.rec = nullptr;
     }
-    if (__builtin_amdgcn_readfirstlane(x.seen) <= kThreePartRows) query_item<D, true, 3>(p, x, k0, k1, v0, v1, table, counts);
-    else query_item<D, true, 2>(p, x, k0, k1, v0, v1, table, counts);
+    query_item<D, true>(p, x, k0, k1, v0, v1, table, counts);
     __syncthreads();  // the tile buffers are free for the next unit
   }
 }

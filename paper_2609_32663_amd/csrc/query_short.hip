@@ -347,7 +347,7 @@ void query_short_kernel(QueryParams p) {
 #pragma unroll
           for (int v = 0; v < 4; ++v) sc[q][j][v] = acc[q][j][v];
     };
-    // Scores of tile t to probabilities, as two bf16 parts.
+    // Scores of tile t to probabilities, as kParts bf16 parts.
     auto softmax = [&](int64_t t, const PagedRun& run) __attribute__((always_inline)) {
       const int64_t key0 = t * kSKeys;
       if constexpr (PAGED) {
