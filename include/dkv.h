@@ -614,6 +614,13 @@ size_t dkv_page_extend_workspace_bytes(int32_t num_units);
  *             of a segment is (page, p, 0, slots filled) for its page p, the
  *             format of dkv_page_select for an unpruned cache; the entries of
  *             the pages that got tokens are written, below max_entries.
+ *             This holds for every unit.  A selection's list (dkv_page_select
+ *             of a mask with pruned positions: runs, not pages) is overwritten
+ *             like the others and wrong from then on: after this call, and
+ *             before the lists are read, dkv_page_select lists the segments
+ *             of compressed units again, from the mask of their selection, with
+ *             the positions past its context (new_len - T) as append_cap;
+ *             page_table has their new pages by then.
  * n_entries   optional, int32 [N * Hkv], in and out: set to the pages of every
  *             served unit that got tokens (even above max_entries).
  * pages_needed optional out, int64 [1]: pages needed by all units that could
