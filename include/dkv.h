@@ -722,7 +722,8 @@ size_t dkv_paged_query_workspace_bytes(int32_t batch, int32_t num_q_heads, int32
  *           token of the chunk attends may hold anything.
  * max_q     (host) tokens of the longest chunk.
  * rows_hint (host) expected total rows of the call, sum over segments of
- *           entries * page_rows (0 = unknown); it sizes the split of the keys
+ *           entries * page_rows (0 = unknown, taken for a long cache); it
+ *           sizes the split of the keys
  *           and must equal the value given to dkv_paged_query_workspace_bytes.
  * workspace dkv_paged_query_workspace_bytes(...) bytes, no initial contents
  *           required, or NULL when that is 0.

@@ -73,3 +73,15 @@ def test_random_batches_do_not_depend_on_the_order():
         B = int(rng.integers(1, 9))
         cost = unit_costs(rng.integers(0, 70000, size=B).tolist(), rng.integers(200, 4097, size=B).tolist(), 8, 4)
         assert len({deal(cost, False, rng) for _ in range(4)}) == 1
+
+
+@pytest.mark.parametrize("hint", [0, -1])
+@pytest.mark.parametrize("B,Hkv", [(2, 8), (1, 16), (3, 8), (16, 8), (256, 1), (32, 8)])
+@pytest.mark.parametrize("new", [5, 8, 16])
+def test_an_unknown_hint_is_a_long_cache(B, Hkv, new, hint):
+    """33 to 128 query rows per segment and no hint: up to 16 segments the kernels for short blocks, as with long ones
+    that they take, and beyond the query tiles, as with the longest; each has a workspace of its own size."""
+    import paper_2609_32663_amd as d
+    size = lambda h: d.dkv_paged_query_workspace_bytes(B, 8 * Hkv, Hkv, 128, B * new, new, h)  # noqa: E731
+    assert size(hint) == size((1 << 18) - 1 if B * Hkv <= 16 else 1 << 40)
+    assert size((1 << 18) - 1) != size(1 << 40) or B * Hkv > 16
