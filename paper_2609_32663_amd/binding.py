@@ -213,11 +213,15 @@ def _stream(stream):
     return _raw_stream(_current_device())
 
 
-def _stream_of_device(stream):
-    """_stream where a device tensor has been seen, so that the device is initialised."""
+def _stream_of(t, stream):
+    """_stream where a device tensor has been seen, so that the device is initialised: a launch goes to the current
+    device, which has to be the tensor's and the stream's."""
+    device = torch.cuda.current_device() if _raw_stream is None else _current_device()
+    if t.get_device() != device or (stream is not None and stream.device_index != device):
+        raise ValueError("the tensors and the stream must be on the current device")
     if stream is not None:
         return stream.cuda_stream
-    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(_current_device())
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
 
 
 def _check(fn, status):
@@ -492,7 +496,7 @@ def dkv_page_extend(unit_new, unit_len, free_pages, n_free, page_table, page_row
         None if entries is None else _typed(entries, "entries", _i32, None, (nseg, most, 4)),
         None if n_entries is None else _typed(n_entries, "n_entries", _i32, nseg), most,
         None if pages_needed is None else _typed(pages_needed, "pages_needed", torch.int64, 1),
-        _dev(workspace, "workspace"), workspace.nbytes, _stream_of_device(stream)))
+        _dev(workspace, "workspace"), workspace.nbytes, _stream_of(unit_len, stream)))
 
 
 def dkv_page_release_workspace_bytes(num_segments, pages_per_seg):
@@ -510,7 +514,7 @@ def dkv_page_release(page_table, free_pages, n_free, workspace, keep=None, table
         _typed(page_table if table_out is None else table_out, "table_out", _i32, None, shape),
         _typed(free_pages, "free_pages", _i32), free_pages.numel(), _typed(n_free, "n_free", _i32, 1),
         _typed(n_free if n_free_out is None else n_free_out, "n_free_out", _i32, 1), _dev(workspace, "workspace"),
-        workspace.nbytes, _stream_of_device(stream)))
+        workspace.nbytes, _stream_of(page_table, stream)))
 
 
 def dkv_paged_append(k_new, v_new, slots, k_pages, v_pages, stream=None):
@@ -527,7 +531,7 @@ def dkv_paged_append(k_new, v_new, slots, k_pages, v_pages, stream=None):
     _check("dkv_paged_append", library().dkv_paged_append(
         dtype_code(dtype), tokens, Hkv, dim, k_ptr, v_ptr, stride, _typed(slots, "slots", torch.int64),
         _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", dtype, None, k_pages.shape), num_pages, page_rows,
-        _stream_of_device(stream)))
+        _stream_of(k_pages, stream)))
 
 
 def dkv_paged_query_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q, rows_hint=0):
@@ -554,4 +558,4 @@ def dkv_paged_query_attn(q, tok_off, first_pos, k_pages, v_pages, entries, n_ent
         _typed(first_pos, "first_pos", _i32), _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", dtype, None, pool),
         num_pages, page_rows, _typed(entries, "entries", _i32), _typed(n_entries, "n_entries", _i32, nseg), most,
         float(sm_scale), int(rows_hint), _typed(out, "out", torch.float32, None, (tokens, Hq, dim)), ws_ptr, ws_bytes,
-        _stream_of_device(stream)))
+        _stream_of(q, stream)))
