@@ -536,7 +536,7 @@ def dkv_paged_append(k_new, v_new, slots, k_pages, v_pages, stream=None):
 
 def dkv_paged_query_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q, rows_hint=0):
     return library().dkv_paged_query_workspace_bytes(int(batch), int(num_q_heads), int(num_kv_heads), int(head_dim),
-                                                     int(num_tokens), int(max_q), int(rows_hint))
+                                                     int(num_tokens), min(int(max_q), int(num_tokens)), int(rows_hint))
 
 
 def dkv_paged_query_attn(q, tok_off, first_pos, k_pages, v_pages, entries, n_entries, sm_scale, out, workspace,
@@ -554,7 +554,7 @@ def dkv_paged_query_attn(q, tok_off, first_pos, k_pages, v_pages, entries, n_ent
     q_ptr, stride = _rows(q, "q", Hq, dim, dtype)
     ws_ptr, ws_bytes = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.nbytes)
     _check("dkv_paged_query_attn", library().dkv_paged_query_attn(
-        dtype_code(dtype), B, Hq, Hkv, dim, tokens, int(max_q), q_ptr, stride, _typed(tok_off, "tok_off", _i32, B + 1),
+        dtype_code(dtype), B, Hq, Hkv, dim, tokens, min(int(max_q), tokens), q_ptr, stride, _typed(tok_off, "tok_off", _i32, B + 1),
         _typed(first_pos, "first_pos", _i32), _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", dtype, None, pool),
         num_pages, page_rows, _typed(entries, "entries", _i32), _typed(n_entries, "n_entries", _i32, nseg), most,
         float(sm_scale), int(rows_hint), _typed(out, "out", torch.float32, None, (tokens, Hq, dim)), ws_ptr, ws_bytes,

@@ -46,3 +46,10 @@ def test_another_device_is_refused(d, call, monkeypatch):
     with pytest.raises(ValueError, match="current device"):
         f(None)
     torch.cuda.synchronize()
+
+
+def test_a_longest_chunk_beyond_int32_is_all_tokens(d):
+    x = Batch(np.random.default_rng(2), [300, 90], [80, 3], 2, 4, 64, 32)
+    want = x.run(d)
+    x.max_q = 1 << 32
+    assert torch.equal(x.run(d), want)

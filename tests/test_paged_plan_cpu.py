@@ -85,3 +85,10 @@ def test_an_unknown_hint_is_a_long_cache(B, Hkv, new, hint):
     size = lambda h: d.dkv_paged_query_workspace_bytes(B, 8 * Hkv, Hkv, 128, B * new, new, h)  # noqa: E731
     assert size(hint) == size((1 << 18) - 1 if B * Hkv <= 16 else 1 << 40)
     assert size((1 << 18) - 1) != size(1 << 40) or B * Hkv > 16
+
+
+def test_a_longest_chunk_beyond_int32_is_all_tokens():
+    """The binding passes 32 bits; a bound above the number of tokens says nothing more than that number."""
+    import paper_2609_32663_amd as d
+    size = lambda most: d.dkv_paged_query_workspace_bytes(3, 32, 8, 128, 700, most, 0)  # noqa: E731
+    assert size(700) > 0 and size(1 << 32) == size(700) and size((1 << 32) + 5) == size(700) != size(5)
