@@ -118,14 +118,18 @@ hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, h
 //     16,000 119 / 98).  The stream is the bound, and one wave's.
 //   * Up to 128 rows: few segments or keys, where the plan and a tile's chain of
 //     phases weigh most; the query tiles spread the rows over all waves (64 query
-//     heads on 8, 64 rows: 8 segments of 16,000 keys 43 / 31, of 60,000 65 / 67; 32
-//     of 1,000 33 / 25, of 4,000 37 / 35, of 16,000 72 / 78; 64 of 1,000 37 / 33, of 4,000
-//     49 / 55; 128 of 1,000 41 / 48; 128 rows: 16 of 16,000 62 / 59, of 60,000 138 /
-//     148; 32 of 1,000 37 / 35, of 4,000 43 / 47; 128 of 300 41 / 33, of 1,000 48 / 72;
-//     256 of 100 43 / 19, of 1,000 54 / 60).
-//   * More rows: fewer still (28 heads on 4, 252 rows: 4 of 1,000 35 / 31, of 65,000
-//     91 / 89; 64 on 8, 256 rows: 8 of 16,000 63 / 59, of 65,000 122 / 151; 16 of
-//     4,000 54 / 49, of 16,000 84 / 93; 32 of 1,000 49 / 53).
+//     heads on 8, 64 rows: 8 segments of 16,000 keys 44 / 30, 16 of 16,000 50 / 46; 32
+//     of 1,000 35 / 25, of 4,000 38 / 34, of 16,000 70 / 74; 64 of 1,000 39 / 34, of 4,000
+//     49 / 55; 128 of 1,000 41 / 48; 128 rows: 16 of 16,000 59 / 56; 32 of 1,000 39 /
+//     35, of 4,000 44 / 46; 128 of 300 41 / 33, of 1,000 48 / 72; 256 of 100 43 / 19, of
+//     1,000 54 / 60).  Up to 16 segments longer ones would be level or ahead here
+//     too (64 rows: 8 of 65,000 79 / 71, 16 of 65,000 130 / 124), but the hint counts
+//     slots of no key, whose runs the short kernels walk and the tiles drop: of
+//     131,072 positions, the 35% that a selection kept, 8 segments, 64 rows, are 69 /
+//     57 in pages of 128 rows, 90 / 119 of 512 and 93 / 199 of 1,024.
+//   * More rows: fewer still (28 heads on 4, 252 rows: 4 of 1,000 35 / 31; 64 on 8,
+//     256 rows: 8 of 16,000 64 / 57, of 32,000 88 / 82, of 65,000 139 / 141; 16 of 4,000
+//     55 / 49, of 16,000 83 / 87; 32 of 1,000 51 / 53).
 //   * Without a hint, up to 128 rows: up to 16 segments, where they are ahead at
 //     any length (64 query heads on 8; 16 segments, 64 rows: 100 keys 21 / 17, 4,000
 //     35 / 27, 60,000 122 / 118; 128 rows: 25 / 23, 39 / 36, 157 / 142), and the
