@@ -11,17 +11,20 @@
 // starts at or past ceil(len / R) * R and stands in the table otherwise, and
 // slot page * R + pos % R.  No thread reads what another one writes, so the
 // call has two forms.  With few rows every workgroup sums all units and fills
-// 128 rows, in one launch: such calls are bound by the launch and a chain of
-// dependent reads (2,048 units, a decode step of 64 sequences on 32 layers: 9.6
-// us a call, 5 of them the kernel).  With many rows one workgroup sums the units
-// and a second kernel fills, bound by writing the slots (four prompts of up to
-// 8,192 tokens on 32 layers, 56 MB: 23.7 us, two launches included; 10.9 at the
-// rate of a copy).
+// 128 rows, in one launch: such calls are bound by the kernel's chain of reads
+// and scans, which goes over the units' lengths three times and sums rows before
+// pages (2,048 units, a decode step of 64 sequences on 32 layers: 9.7 us a call,
+// 7.9 of them the kernel; one unit 4.4; the other calls' kernels of one launch 2.6 to 2.8).
+// With many rows one workgroup sums the units and a second kernel fills, whose
+// stores each wait for a chain of reads, up to the page's word (four prompts of
+// up to 8,192 tokens on 32 layers, 56 MB: 23.7 us, of them the sums 5.5 and the
+// fill 18.2, 3 TB/s; 8.1 at the rate of stores alone).
 //
 // Release.  The pages to go, in table order, are pushed on the stack: a count
 // per chunk of table words, then every chunk sums the counts before it and
 // places its own.  One chunk needs no count.  Bound by its launches (a request
-// of 4,100 positions 6.3 us, all layers of a 128K context, 3 MB, 8.8).
+// of 4,100 positions 6.9 us, 2.8 of them the kernel; all layers of a 128K
+// context, 3 MB, 10.2, the kernels 3.4 and 4.8).
 
 #include "dkv_device.hpp"
 #include "dkv_launch.hpp"

@@ -175,8 +175,9 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // bf16 parts of a probability.  Packed: two, 17 bits.  Paged: three, its 24
   // bits, at any length: two err by 2.1e-6 to 2.5e-6 of the output's norm at
   // 1,000 keys as at 131,072, three by 2.0e-7 to 5.2e-7, attention in plain fp32
-  // by 3.3e-7 to 4.0e-6 (q, K, V Gaussian; 64 dimensions at 131,072 keys 2.5e-6,
-  // 5.2e-7 and 1.8e-6).  The third product costs what it computes, as the kernel
+  // by 3.3e-7 to 4.0e-6 (q, K, V Gaussian, one head; 64 dimensions at 131,072 keys
+  // 2.5e-6, 5.2e-7 and 1.8e-6; the more keys a workgroup adds up, the more the fp32
+  // sums err: 8 heads, 512 tokens at 32K, three parts 1.0e-6).  The third product costs what it computes, as the kernel
   // runs at the rate that the matrix units reach under the power limit (two / three
   // parts, us, 8B layer: 512 tokens at 32K 349 / 423, 256 over 45K rows 277 / 330).
   constexpr int kParts = PAGED ? 3 : 2;
@@ -351,8 +352,8 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   };
   // The runs with slots moved to the table's front, in order; returns their
   // number (256 tokens over the 35% of 131,072 positions that a selection kept,
-  // in 128-row pages 283 -> 275 us, in 256-row pages 314 -> 280, in 1,024-row pages
-  // 531 -> 317; a unit of whole pages, without gaps, pays 1.5 us for the branch).  A word moves
+  // in 128-row pages 333 -> 323 us, in 256-row pages 369 -> 324, in 1,024-row pages
+  // 613 -> 372; 512 tokens over whole pages, without gaps, 417 -> 420).  A word moves
   // to its own index or a lower one, after the words up to it have been read.
   auto drop_gaps = [&](int n) __attribute__((always_inline)) {
     int at = 0;
@@ -929,7 +930,7 @@ __global__ __launch_bounds__(kQThreads) void query_attn_kernel(QueryParams p) {
     t_hi = (int64_t)(r + 1) * tiles / nr;
   }
   query_item<D, false>(p, QueryItem{s, qt, t_lo, t_hi, single, p.rec + (int64_t)item * kQRows * QCfg<D>::kRec,
-                                       PagedBlock{0, 0, 0}, 0, false}, k0, k1, v0, v1, nullptr, nullptr);
+                                    PagedBlock{0, 0, 0}, 0, false}, k0, k1, v0, v1, nullptr, nullptr);
 }
 
 // ---------------------------------------------------------------------------
