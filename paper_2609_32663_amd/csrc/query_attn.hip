@@ -177,9 +177,10 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // 1,000 keys as at 131,072, three by 2.0e-7 to 5.2e-7, attention in plain fp32
   // by 3.3e-7 to 4.0e-6 (q, K, V Gaussian, one head; 64 dimensions at 131,072 keys
   // 2.5e-6, 5.2e-7 and 1.8e-6; the more keys a workgroup adds up, the more the fp32
-  // sums err: 8 heads, 512 tokens at 32K, three parts 1.0e-6).  The third product costs what it computes, as the kernel
-  // runs at the rate that the matrix units reach under the power limit (two / three
-  // parts, us, 8B layer: 512 tokens at 32K 349 / 423, 256 over 45K rows 277 / 330).
+  // sums err: 8 heads, 512 tokens at 32K, three parts 1.0e-6).  The third product
+  // costs what it computes, as the kernel runs at the rate that the matrix units
+  // reach under the power limit (two / three parts, us, 8B layer: 512 tokens at 32K
+  // 349 / 423, 256 over 45K rows 277 / 330).
   constexpr int kParts = PAGED ? 3 : 2;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
