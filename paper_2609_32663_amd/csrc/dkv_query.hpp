@@ -131,12 +131,13 @@ hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, h
 //     256 rows: 8 of 16,000 64 / 57, of 32,000 88 / 82, of 65,000 139 / 141; 16 of 4,000
 //     55 / 49, of 16,000 83 / 87; 32 of 1,000 51 / 53).
 //   * Without a hint, up to 128 rows: up to 16 segments, where they are ahead at
-//     any length of whole pages (behind over large pages' selections, as above; 64 query heads on 8; 16 segments, 64 rows: 100 keys 21 / 17, 4,000
-//     35 / 27, 60,000 122 / 118; 128 rows: 25 / 23, 39 / 36, 157 / 142), and the
-//     query tiles beyond, which lose with short segments only (64 rows, 32 segments: 100
-//     keys 22 / 20, 4,000 38 / 37, 60,000 202 / 222; 128 segments: 25 / 21, 74 / 90,
-//     759 / 839; 128 rows, 128 segments: 32 / 27, 1,000 keys 48 / 71, 4,000 96 / 118,
-//     16,000 303 / 314).
+//     any length of whole pages (behind over a selection in large pages, as above;
+//     64 query heads on 8; 16 segments, 64 rows: 100 keys 21 / 17, 4,000 35 / 27,
+//     60,000 122 / 118; 128 rows: 25 / 23, 39 / 36, 157 / 142), and the query tiles
+//     beyond, which lose with short segments only (64 rows, 32 segments: 100 keys 22 /
+//     20, 4,000 38 / 37, 60,000 202 / 222; 128 segments: 25 / 21, 74 / 90, 759 / 839;
+//     128 rows, 128 segments: 32 / 27, 1,000 keys 48 / 71, 4,000 96 / 118, 16,000 303 /
+//     314).
 inline bool paged_takes_short(int64_t nseg, int64_t rows, int64_t rows_hint) {
   if (rows <= kShortRows / 8) return true;
   if (rows <= kShortRows / 2 && rows_hint <= 0) return nseg <= 16;
