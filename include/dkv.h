@@ -747,6 +747,165 @@ dkv_status dkv_paged_query_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_he
                                 int64_t rows_hint, float *out, void *workspace,
                                 size_t workspace_bytes, void *stream);
 
+/*
+ * Rotary positions, a quantised cache and drafted trees
+ * -----------------------------------------------------
+ * A step of speculative decoding over a paged cache: dkv_page_extend gives the
+ * drafted tokens pages and slots, dkv_tree_plan their ancestors and positions,
+ * dkv_paged_store rotates q and K and writes K and V (in bf16, or quantised to
+ * 8 bits), dkv_paged_tree_attn lets every token attend to its request and its
+ * ancestors, and dkv_paged_accept keeps the accepted path.  Prompts in chunks
+ * and single tokens take the same calls without a tree.
+ *
+ * Cache formats.  DKV_CACHE_BF16: pools of bf16 rows, as dkv_paged_append
+ * fills them; `scales` is ignored.  DKV_CACHE_F8: a row of d values is d codes of
+ * e4m3 (sign, 4 exponent bits, 3 mantissa bits, largest value 448, no
+ * infinities) in a pool [num_pages][page_rows][d] of bytes, and an exponent
+ * byte 127 + e; code c stands for c * 2^e.  scales is uint8
+ * [num_pages][page_rows][2], the bytes of the K and the V row.  e is the smallest
+ * with the row's largest magnitude at most 448 * 2^e, within [-117, 120]; codes
+ * are rounded to nearest, ties to even.  NaN and infinities become NaN, and do
+ * not count for e.  A value is off by at most 2^-4 of itself, or 2^-10 * 2^e.
+ * Pages, tables, slots and entries are the same for both formats.
+ */
+typedef enum dkv_cache_format { DKV_CACHE_BF16 = 0, DKV_CACHE_F8 = 1 } dkv_cache_format;
+
+#define DKV_MAX_TREE 1024  /* tokens of a drafted tree (dkv_tree_plan with parents) */
+#define DKV_MAX_PATH 64    /* tokens of an accepted path */
+
+/* How rotary frequencies f_i = base^(-2i / rot_dim) are stretched by `factor`
+ * for contexts longer than trained_len (dkv_rope_freqs). */
+typedef enum dkv_rope_scaling {
+  DKV_ROPE_PLAIN = 0,  /* not */
+  DKV_ROPE_LINEAR = 1, /* all divided by factor */
+  DKV_ROPE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)): the slowest pair divided by factor */
+  DKV_ROPE_WAVE = 3,   /* pairs with up to `low` turns over trained_len divided, from `high` on kept, linear between */
+  DKV_ROPE_RAMP = 4    /* the same, linear in the pair's index between the pairs with `high` and `low` turns
+                          (rounded outwards); *mscale = 0.1 ln(factor) + 1 */
+} dkv_rope_scaling;
+
+/*
+ * dkv_rope_freqs -- rotary frequencies (host, no GPU call): inv_freq[0 ..
+ * rot_dim / 2) and the factor *mscale of the rotated elements (1 but for
+ * DKV_ROPE_RAMP), computed in double.  base > 1, factor >= 1; 0 < low < high
+ * turns and trained_len > 0 where the scaling uses them.
+ */
+dkv_status dkv_rope_freqs(dkv_rope_scaling kind, int32_t rot_dim, double base, double factor, double trained_len,
+                          double low, double high, float *inv_freq, float *mscale);
+
+/*
+ * dkv_rope -- rotary positions of token-major rows.
+ *
+ * x, out    [num_tokens][num_heads][head_dim] of `dtype`, tokens x_stride and
+ *           out_stride elements apart (multiples of 16 bytes); out == x with the
+ *           same stride rotates in place, otherwise they must not overlap.
+ * pos       int32 [num_tokens]; a token with a negative one is left out: its
+ *           rows of `out` stay as they were.
+ * inv_freq  float [rot_dim / 2] (device): pair i turns by pos * inv_freq[i],
+ *           (a, b) -> mscale * (a cos - b sin, a sin + b cos); pos * |inv_freq[i]| below
+ *           2^32.
+ * rot_dim   even, at most head_dim: the rotated part of a head; the rest is copied.
+ * interleaved  0: pair i is elements i and i + rot_dim / 2; otherwise 2i and 2i + 1.
+ * head_dim a multiple of 8, at most 256 (DKV_ERR_UNSUPPORTED otherwise, as when
+ * num_tokens * num_heads > 2^24 - 1).
+ * Angles are computed in double; the result is rounded once (bf16 rows: after
+ * fp32 products).
+ */
+dkv_status dkv_rope(dkv_dtype dtype, int32_t num_tokens, int32_t num_heads, int32_t head_dim, const void *x,
+                    int64_t x_stride, const int32_t *pos, const float *inv_freq, int32_t rot_dim, int32_t interleaved,
+                    float mscale, void *out, int64_t out_stride, void *stream);
+
+/*
+ * dkv_tree_plan -- ancestors and positions of drafted tokens.
+ *
+ * tok_off, first_pos  int32 [batch + 1] (ascending) and [batch], as from
+ *           dkv_page_extend: sequence b's new tokens are rows [tok_off[b],
+ *           tok_off[b + 1]), the first max_q of them count.
+ * parent    int32 [num_tokens] or NULL (every token follows the one before it):
+ *           index among its sequence's new tokens of the one a token
+ *           continues; one that is negative or does not come before the
+ *           token makes it continue what the sequence held.
+ * pos       out, int32 [num_tokens]: first_pos[b] + number of ancestors; -1 for
+ *           rows of no sequence, of one with a negative first_pos, and past max_q.
+ * mask      out, optional, uint64 [num_tokens][mask_words]: bit j of a row is
+ *           set when new token j of the sequence is the token itself or an
+ *           ancestor; zeros where pos is -1.  mask_words * 64 must be at least
+ *           max_q (or num_tokens, if that is less).
+ * With parents max_q is at most DKV_MAX_TREE, batch at most DKV_MAX_SEGMENTS
+ * (DKV_ERR_UNSUPPORTED otherwise).
+ */
+dkv_status dkv_tree_plan(int32_t batch, int32_t num_tokens, int32_t max_q, const int32_t *tok_off,
+                         const int32_t *first_pos, const int32_t *parent, int32_t *pos, uint64_t *mask,
+                         int32_t mask_words, void *stream);
+
+/*
+ * dkv_paged_store -- new tokens into a paged cache: q and K rotated, K and V
+ * written to their slots in the cache's format, in one launch.
+ *
+ * q, q_out  [num_tokens][Hq][d] bf16, tokens q_stride and q_out_stride elements
+ *           apart; q_out is q rotated as by dkv_rope (in place with q_out == q
+ *           and the same stride).  With num_q_heads = 0 both may be NULL.
+ * k_new, v_new  [num_tokens][Hkv][d] bf16, tokens kv_stride elements apart.
+ * pos, inv_freq, rot_dim, interleaved, mscale  as for dkv_rope; rot_dim = 0: q
+ *           and K are taken as they are and pos and inv_freq may be NULL.  With
+ *           rotation a token with a negative pos is left out altogether.
+ * slots     int64 [num_tokens][Hkv] as dkv_page_extend writes them; a row with a
+ *           slot outside [0, num_pages * page_rows) is skipped.  What rows with
+ *           the same slot leave there is unspecified.
+ * K is rotated in double where it is quantised next, in fp32 otherwise, and
+ * rounded once, to the cache's format.  head_dim 64 or 128; strides multiples
+ * of 8 elements.
+ */
+dkv_status dkv_paged_store(dkv_cache_format format, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads,
+                           int32_t head_dim, const void *q, int64_t q_stride, const void *k_new, const void *v_new,
+                           int64_t kv_stride, const int32_t *pos, const float *inv_freq, int32_t rot_dim,
+                           int32_t interleaved, float mscale, void *q_out, int64_t q_out_stride, const int64_t *slots,
+                           void *k_pages, void *v_pages, uint8_t *scales, int64_t num_pages, int32_t page_rows,
+                           void *stream);
+
+/*
+ * dkv_paged_load -- rows of a paged cache back in bf16 (exact for both formats).
+ *
+ * slots     int64 [num_tokens][Hkv]: pool rows; k_out and v_out rows of a slot
+ *           outside [0, num_pages * page_rows) stay as they were.
+ * k_out, v_out  [num_tokens][Hkv][d] bf16, tokens token_stride elements apart (a
+ *           multiple of 8).
+ */
+dkv_status dkv_paged_load(dkv_cache_format format, int32_t num_tokens, int32_t num_kv_heads, int32_t head_dim,
+                          const void *k_pages, const void *v_pages, const uint8_t *scales, int64_t num_pages,
+                          int32_t page_rows, const int64_t *slots, void *k_out, void *v_out, int64_t token_stride,
+                          void *stream);
+
+/*
+ * dkv_paged_accept -- keep an accepted path of the drafted tokens.
+ *
+ * Units are (layer, sequence) pairs, unit n = layer * batch + b, segments n *
+ * Hkv + g, as for dkv_page_extend; all layers of a step go in one call.
+ * first_pos int32 [num_units]: position of the unit's first new token; a unit
+ *           with a negative one is left as it is (nothing of it is written).
+ * path      int32 [batch][max_path]: indexes among sequence b's new tokens, from
+ *           the root on, each larger than the one before; the first n_path[b]
+ *           count, up to one that is not larger, is negative or lies past the
+ *           page table.  max_path at most DKV_MAX_PATH.
+ * The rows of token path[b][i] (position first_pos + path[b][i]) move to position
+ * first_pos + i, in every segment's K and V; a row whose page (from or to) is
+ * outside the pool does not move.
+ * new_len   out, int32 [num_units]: first_pos + accepted tokens (a buffer of
+ *           its own).
+ * keep      optional out, uint8 [num_units * Hkv][pages_per_seg]: 1 for the pages
+ *           of the first new_len positions, 0 for those behind them: the argument
+ *           of dkv_page_release that takes the others back.
+ * Entries need no change: what lies past a chunk's last position is not read,
+ * and the next dkv_page_extend (with new_len as unit_len, after the pages
+ * behind it have been released) writes those that change.
+ * num_units * Hkv at most 65,535.
+ */
+dkv_status dkv_paged_accept(dkv_cache_format format, int32_t num_units, int32_t batch, int32_t num_kv_heads,
+                            int32_t head_dim, const int32_t *first_pos, const int32_t *path, const int32_t *n_path,
+                            int32_t max_path, const int32_t *page_table, int32_t pages_per_seg, int32_t page_rows,
+                            void *k_pages, void *v_pages, uint8_t *scales, int64_t num_pages, int32_t *new_len,
+                            uint8_t *keep, void *stream);
+
 /* Static description of a status code. */
 const char *dkv_status_string(dkv_status status);
 

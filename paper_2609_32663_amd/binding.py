@@ -27,11 +27,17 @@ __all__ = [
     "dkv_topk_workspace_bytes", "dkv_topk_pattern", "dkv_map_pattern_ragged",
     "dkv_page_extend_workspace_bytes", "dkv_page_extend", "dkv_page_release_workspace_bytes", "dkv_page_release",
     "dkv_paged_append", "dkv_paged_query_workspace_bytes", "dkv_paged_query_attn",
+    "DKV_CACHE_BF16", "DKV_CACHE_F8", "DKV_ROPE_PLAIN", "DKV_ROPE_LINEAR", "DKV_ROPE_BASE", "DKV_ROPE_WAVE",
+    "DKV_ROPE_RAMP", "DKV_MAX_TREE", "DKV_MAX_PATH", "dkv_rope_freqs", "dkv_rope", "dkv_tree_plan", "dkv_paged_store",
+    "dkv_paged_load", "dkv_paged_accept",
 ]
 
 (DKV_OK, DKV_ERR_INVALID_ARG, DKV_ERR_UNSUPPORTED, DKV_ERR_MISALIGNED, DKV_ERR_CAPACITY,
  DKV_ERR_WORKSPACE, DKV_ERR_HIP) = range(7)
 DKV_BF16, DKV_F32 = 0, 1
+DKV_CACHE_BF16, DKV_CACHE_F8 = 0, 1
+DKV_ROPE_PLAIN, DKV_ROPE_LINEAR, DKV_ROPE_BASE, DKV_ROPE_WAVE, DKV_ROPE_RAMP = range(5)
+DKV_MAX_TREE, DKV_MAX_PATH = 1024, 64
 DKV_NOALLOC_SCRATCH_BYTES = 16 << 20  # include/dkv.h: scratch of dkv_append_decode_attn_noalloc
 
 library_path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdkv.so")
@@ -91,6 +97,7 @@ def library_at(path):
     lib = ctypes.CDLL(path)
     P, I32, I64, SZ, F32, VP = (ctypes.POINTER(Layout), ctypes.c_int32, ctypes.c_int64,
                                 ctypes.c_size_t, ctypes.c_float, ctypes.c_void_p)
+    F64 = ctypes.c_double
     sigs = {
         "dkv_map_pattern": (I32, [P, VP, VP, VP, VP, VP]),
         "dkv_compact_workspace_bytes": (SZ, [P]),
@@ -133,6 +140,13 @@ def library_at(path):
         "dkv_paged_query_attn": (I32, [I32, I32, I32, I32, I32, I32, I32, VP, I64, VP, VP, VP, VP, I64, I32, VP, VP, I32,
                                        F32, I64, VP, VP, SZ, VP]),
         "dkv_paged_append": (I32, [I32, I32, I32, I32, VP, VP, I64, VP, VP, VP, I64, I32, VP]),
+        "dkv_rope_freqs": (I32, [I32, I32, F64, F64, F64, F64, F64, VP, VP]),
+        "dkv_rope": (I32, [I32, I32, I32, I32, VP, I64, VP, VP, I32, I32, F32, VP, I64, VP]),
+        "dkv_tree_plan": (I32, [I32, I32, I32, VP, VP, VP, VP, VP, I32, VP]),
+        "dkv_paged_store": (I32, [I32, I32, I32, I32, I32, VP, I64, VP, VP, I64, VP, VP, I32, I32, F32, VP, I64, VP, VP,
+                                  VP, VP, I64, I32, VP]),
+        "dkv_paged_load": (I32, [I32, I32, I32, I32, VP, VP, VP, I64, I32, VP, VP, VP, I64, VP]),
+        "dkv_paged_accept": (I32, [I32, I32, I32, I32, I32, VP, VP, VP, I32, VP, I32, I32, VP, VP, VP, I64, VP, VP, VP]),
         "dkv_compact_bins_workspace_bytes": (SZ, [P]),
         "dkv_compact_bins": (I32, [P, I32, VP, VP, VP, I32, VP, VP, I64, VP, VP, VP, VP, VP, SZ, VP]),
         "dkv_compact_bins_ragged": (I32, [P, VP, I32, VP, VP, VP, I32, VP, VP, I64, VP, VP, VP, VP, VP, SZ, VP]),
@@ -559,3 +573,120 @@ def dkv_paged_query_attn(q, tok_off, first_pos, k_pages, v_pages, entries, n_ent
         num_pages, page_rows, _typed(entries, "entries", _i32), _typed(n_entries, "n_entries", _i32, nseg), most,
         float(sm_scale), int(rows_hint), _typed(out, "out", torch.float32, None, (tokens, Hq, dim)), ws_ptr, ws_bytes,
         _stream_of(q, stream)))
+
+
+# ---------------------------------------------------------------------------
+# rotary positions, a quantised cache and drafted trees
+# ---------------------------------------------------------------------------
+
+def _cache(k_pages, v_pages, scales):
+    """Format of a cache (by the pools' element type) and the addresses of its pools and exponent bytes."""
+    dtype, shape = k_pages.dtype, k_pages.shape
+    if dtype is _bf16:
+        return DKV_CACHE_BF16, _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", _bf16, None, shape), None
+    if dtype is not _f8:
+        raise TypeError(f"unsupported cache element type {dtype}: bfloat16 or float8_e4m3fn")
+    return (DKV_CACHE_F8, _dev(k_pages, "k_pages"), _typed(v_pages, "v_pages", _f8, None, shape),
+            _typed(scales, "scales", torch.uint8, None, (shape[0], shape[1], 2)))
+
+
+_bf16, _f8 = torch.bfloat16, torch.float8_e4m3fn
+
+
+def dkv_rope_freqs(kind, rot_dim, base, factor=1.0, trained_len=0.0, low=0.0, high=0.0):
+    """Frequencies of rot_dim / 2 pairs as a float32 host tensor, and mscale."""
+    if int(rot_dim) <= 0:
+        raise DkvError("dkv_rope_freqs", DKV_ERR_INVALID_ARG)
+    freq, mscale = torch.empty(int(rot_dim) // 2, dtype=torch.float32), ctypes.c_float()
+    _check("dkv_rope_freqs", library().dkv_rope_freqs(
+        int(kind), int(rot_dim), float(base), float(factor), float(trained_len), float(low), float(high), freq.data_ptr(),
+        ctypes.byref(mscale)))
+    return freq, mscale.value
+
+
+def dkv_rope(x, pos, inv_freq, rot_dim, out, interleaved=False, mscale=1.0, stream=None):
+    """x, out: [tokens][heads][dim] bf16 or fp32, tokens evenly spaced (views of a fused projection included), out may
+    be x; pos: int32 [tokens]; inv_freq: float32 [rot_dim / 2]."""
+    tokens, heads, dim = x.shape
+    dtype = x.dtype
+    x_ptr, x_stride = _rows(x, "x", heads, dim, dtype)
+    out_ptr, out_stride = _rows(out, "out", heads, dim, dtype)
+    if out.shape[0] != tokens:
+        raise ValueError("out must have a row per row of x")
+    _check("dkv_rope", library().dkv_rope(
+        dtype_code(dtype), tokens, heads, dim, x_ptr, x_stride, _typed(pos, "pos", _i32, tokens),
+        _typed(inv_freq, "inv_freq", torch.float32, int(rot_dim) // 2), int(rot_dim), 1 if interleaved else 0,
+        float(mscale), out_ptr, out_stride, _stream_of(x, stream)))
+
+
+def dkv_tree_plan(tok_off, first_pos, max_q, pos, parent=None, mask=None, stream=None):
+    """tok_off: int32 [B+1]; first_pos: int32 [B]; parent: optional int32 [tokens]; pos: int32 [tokens] (out); mask:
+    optional int64 [tokens][words] (out)."""
+    B, tokens = first_pos.shape[0], pos.shape[0]
+    words = 0 if mask is None else mask.shape[1]
+    _check("dkv_tree_plan", library().dkv_tree_plan(
+        B, tokens, min(int(max_q), tokens), _typed(tok_off, "tok_off", _i32, B + 1), _typed(first_pos, "first_pos", _i32),
+        None if parent is None else _typed(parent, "parent", _i32, tokens), _typed(pos, "pos", _i32),
+        None if mask is None else _typed(mask, "mask", torch.int64, None, (tokens, words)), words,
+        _stream_of(pos, stream)))
+
+
+def dkv_paged_store(k_new, v_new, slots, k_pages, v_pages, scales=None, q=None, q_out=None, pos=None, inv_freq=None,
+                    rot_dim=0, interleaved=False, mscale=1.0, stream=None):
+    """k_new, v_new: bf16 [tokens][Hkv][d], q, q_out: bf16 [tokens][Hq][d], tokens evenly spaced (views of a fused
+    projection included); slots: int64 [tokens][Hkv]; k_pages, v_pages: [num_pages][page_rows][d] bf16, or
+    float8_e4m3fn with scales uint8 [num_pages][page_rows][2]; pos, inv_freq: as dkv_rope's, with rot_dim > 0."""
+    num_pages, page_rows, dim = k_pages.shape
+    tokens, Hkv = slots.shape
+    fmt, k_pool, v_pool, ex = _cache(k_pages, v_pages, scales)
+    k_ptr, stride = _rows(k_new, "k_new", Hkv, dim, _bf16)
+    v_ptr, v_stride = _rows(v_new, "v_new", Hkv, dim, _bf16)
+    if v_stride != stride or k_new.shape[0] != tokens or v_new.shape[0] != tokens:
+        raise ValueError("k_new and v_new must have a row per row of slots, evenly spaced alike")
+    Hq, q_ptr, q_stride, o_ptr, o_stride = 0, None, 0, None, 0
+    if q is not None:
+        Hq = q.shape[1]
+        q_ptr, q_stride = _rows(q, "q", Hq, dim, _bf16)
+        o_ptr, o_stride = _rows(q_out, "q_out", Hq, dim, _bf16)
+        if q.shape[0] != tokens or q_out.shape[0] != tokens:
+            raise ValueError("q and q_out must have a row per row of slots")
+    rot_dim = int(rot_dim)
+    _check("dkv_paged_store", library().dkv_paged_store(
+        fmt, tokens, Hq, Hkv, dim, q_ptr, q_stride, k_ptr, v_ptr, stride,
+        _typed(pos, "pos", _i32, tokens) if rot_dim else None,
+        _typed(inv_freq, "inv_freq", torch.float32, rot_dim // 2) if rot_dim else None, rot_dim, 1 if interleaved else 0,
+        float(mscale), o_ptr, o_stride, _typed(slots, "slots", torch.int64), k_pool, v_pool, ex, num_pages, page_rows,
+        _stream_of(k_pages, stream)))
+
+
+def dkv_paged_load(slots, k_pages, v_pages, k_out, v_out, scales=None, stream=None):
+    """slots: int64 [tokens][Hkv]; pools as dkv_paged_store's; k_out, v_out: bf16 [tokens][Hkv][d], tokens evenly
+    spaced."""
+    num_pages, page_rows, dim = k_pages.shape
+    tokens, Hkv = slots.shape
+    fmt, k_pool, v_pool, ex = _cache(k_pages, v_pages, scales)
+    k_ptr, stride = _rows(k_out, "k_out", Hkv, dim, _bf16)
+    v_ptr, v_stride = _rows(v_out, "v_out", Hkv, dim, _bf16)
+    if v_stride != stride or k_out.shape[0] != tokens or v_out.shape[0] != tokens:
+        raise ValueError("k_out and v_out must have a row per row of slots, evenly spaced alike")
+    _check("dkv_paged_load", library().dkv_paged_load(
+        fmt, tokens, Hkv, dim, k_pool, v_pool, ex, num_pages, page_rows, _typed(slots, "slots", torch.int64), k_ptr, v_ptr,
+        stride, _stream_of(k_pages, stream)))
+
+
+def dkv_paged_accept(first_pos, path, n_path, page_table, num_kv_heads, k_pages, v_pages, new_len, scales=None, keep=None,
+                     stream=None):
+    """first_pos, new_len (out): int32 [N]; path: int32 [B][max_path], n_path: int32 [B], N a multiple of B; page_table:
+    int32 [N*Hkv][pages_per_seg]; pools as dkv_paged_store's; keep: optional uint8 of page_table's shape (out)."""
+    N, Hkv = first_pos.shape[0], int(num_kv_heads)
+    B, most = path.shape
+    shape = page_table.shape
+    num_pages, page_rows, dim = k_pages.shape
+    if shape[0] != N * Hkv:
+        raise ValueError("page_table must have N * Hkv rows")
+    fmt, k_pool, v_pool, ex = _cache(k_pages, v_pages, scales)
+    _check("dkv_paged_accept", library().dkv_paged_accept(
+        fmt, N, B, Hkv, dim, _typed(first_pos, "first_pos", _i32), _typed(path, "path", _i32),
+        _typed(n_path, "n_path", _i32, B), most, _typed(page_table, "page_table", _i32), shape[1], page_rows, k_pool,
+        v_pool, ex, num_pages, _typed(new_len, "new_len", _i32, N),
+        None if keep is None else _typed(keep, "keep", torch.uint8, None, shape), _stream_of(first_pos, stream)))

@@ -40,7 +40,7 @@ COMMON_FLAGS = [
 FILE_FLAGS = {f: ["-mno-amdgpu-ieee", "-fno-honor-nans"] for f in ("query_attn.hip", "query_short.hip")}
 SOURCES = ["map_pattern.hip", "compact.hip", "compact_bins.hip", "decode_attn.hip", "dkv_api.cpp", "bw_probe.hip",
            "query_attn.hip", "query_short.hip", "dkv_query_api.cpp", "page_select.hip", "page_fill.hip", "dkv_paged_api.cpp",
-           "topk_pattern.hip", "dkv_pattern_api.cpp"]
+           "topk_pattern.hip", "dkv_pattern_api.cpp", "rotate_store.hip", "tree_plan.hip", "dkv_tree_api.cpp"]
 
 
 def _hipcc():

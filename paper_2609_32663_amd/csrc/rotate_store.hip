@@ -1,0 +1,356 @@
+// Rotary positions, and rows of K and V written into a paged cache and read
+// back, in bf16 or quantised (dkv_f8.hpp).
+//
+// Rotation.  Pair i of a head, at position t, turns by t f_i:
+//   (a, b) -> m (a cos - b sin, a sin + b cos),
+// with a, b elements i and i + n of the head (half layout, n pairs) or 2i and
+// 2i + 1 (interleaved); the rest of the head stays.  Angles are taken in 64
+// bits: at t = 10^6 an fp32 product is off by 0.06.  bf16 rows are turned in
+// fp32 (the result is rounded to 8 bits), fp32 rows and rows that are quantised
+// next in 64 bits: an error in the last of fp32's bits would put values next to
+// a border of the four-bit codes on its other side.
+//
+// One wave per token (or `parts` waves where tokens are few, to fill the card):
+// its lanes take the sine and cosine of a pair each and exchange them through
+// LDS, then walk the token's rows, eight elements per lane; an element's
+// partner comes from the lane that holds it, or from memory where the pairs do
+// not line up with the lanes' eight.  A row's largest magnitude is a reduction
+// over its 8 or 16 lanes.  Nothing meets beyond a wave.  Moving the rows bounds
+// all of it.
+
+#include <hip/hip_runtime.h>
+
+#include "dkv_f8.hpp"
+#include "dkv_tree.hpp"
+
+namespace dkv {
+
+namespace {
+
+constexpr int kRotThreads = 256;
+constexpr int kRotWaves = kRotThreads / kWave;
+constexpr int kMaxPairs = 128;  // heads of up to 256 elements
+constexpr int kGroups = 4;      // row groups of a wave whose loads are in flight together
+
+// Sine and cosine in 64 bits of x >= 0 below 2^32 (about 2 ulp): x - k pi/2 by two
+// fused steps, the first of them exact as x and k (pi/2 rounded to 53 bits) are
+// multiples of 2^-52 that nearly cancel, then the Taylor series up to pi/4.
+__device__ __forceinline__ void sincos64(double x, double* s, double* c) {
+  const double k = __builtin_rint(x * 0.63661977236758134308);
+  double r = __builtin_fma(-k, 1.57079632679489655800, x);
+  r = __builtin_fma(-k, 6.12323399573676603587e-17, r);
+  const double z = r * r;
+  double ps = 1.0 / 355687428096000.0;  // 17!
+  ps = __builtin_fma(ps, z, -1.0 / 1307674368000.0);
+  ps = __builtin_fma(ps, z, 1.0 / 6227020800.0);
+  ps = __builtin_fma(ps, z, -1.0 / 39916800.0);
+  ps = __builtin_fma(ps, z, 1.0 / 362880.0);
+  ps = __builtin_fma(ps, z, -1.0 / 5040.0);
+  ps = __builtin_fma(ps, z, 1.0 / 120.0);
+  ps = __builtin_fma(ps, z, -1.0 / 6.0);
+  const double sn = __builtin_fma(r * z, ps, r);
+  double pc = 1.0 / 20922789888000.0;  // 16!
+  pc = __builtin_fma(pc, z, -1.0 / 87178291200.0);
+  pc = __builtin_fma(pc, z, 1.0 / 479001600.0);
+  pc = __builtin_fma(pc, z, -1.0 / 3628800.0);
+  pc = __builtin_fma(pc, z, 1.0 / 40320.0);
+  pc = __builtin_fma(pc, z, -1.0 / 720.0);
+  pc = __builtin_fma(pc, z, 1.0 / 24.0);
+  pc = __builtin_fma(pc, z, -0.5);
+  const double cs = __builtin_fma(z, pc, 1.0);
+  const int64_t q = (int64_t)k;
+  const double u = (q & 1) ? cs : sn, w = (q & 1) ? sn : cs;
+  *s = (q & 2) ? -u : u;
+  *c = ((q + 1) & 2) ? -w : w;
+}
+
+// Eight elements of a row as they lie in memory.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<uint16_t> {
+  u32x4 w;
+  __device__ __forceinline__ void zero() { w = u32x4{0u, 0u, 0u, 0u}; }
+  __device__ __forceinline__ float at(int e) const { return (e & 1) ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]); }
+  __device__ __forceinline__ void put(int e, const uint16_t* x) {
+    const uint32_t b = *x;
+    w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xFFFFu) | b << 16 : (w[e >> 1] & 0xFFFF0000u) | b;
+  }
+  __device__ __forceinline__ void shuffle(const Raw& from, int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)__shfl((int)from.w[i], lane, kWave);
+  }
+};
+template <>
+struct Raw<float> {
+  f32x4 w[2];
+  __device__ __forceinline__ void zero() { w[0] = w[1] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ float at(int e) const { return w[e >> 2][e & 3]; }
+  __device__ __forceinline__ void put(int e, const float* x) { w[e >> 2][e & 3] = *x; }
+  __device__ __forceinline__ void shuffle(const Raw& from, int lane) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i >> 2][i & 3] = __shfl(from.w[i >> 2][i & 3], lane, kWave);
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(Raw<T>& r, const T* at) {  // at any element
+  __builtin_memcpy(&r, at, sizeof(r));
+}
+
+__device__ __forceinline__ u32x4 pack_bf16(const float (&y)[8]) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    bf16x2_t b;
+    b[0] = (__bf16)y[2 * i];
+    b[1] = (__bf16)y[2 * i + 1];
+    w[i] = __builtin_bit_cast(uint32_t, b);
+  }
+  return w;
+}
+
+enum RowKind { kRowX, kRowK, kRowV };
+enum StoreMode { kRopeOnly, kStoreBf16, kStoreF8 };
+
+// LPR: lanes per row, 0 for any (dim / 8, at most 32).
+template <typename T, int MODE, int LPR>
+__global__ __launch_bounds__(kRotThreads) void rotate_store_kernel(RotateParams p) {
+  __shared__ double2 trig[kRotWaves][kMaxPairs];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const int64_t id = (int64_t)blockIdx.x * kRotWaves + wave;
+  const int64_t t = id / p.parts;
+  const int part = (int)(id - t * p.parts);
+  if (t >= p.tokens) return;
+  const int lpr = LPR > 0 ? LPR : p.dim / 8;
+  const int per = kWave / lpr;  // rows of a group
+  const int row_in = lane / lpr, c = lane - row_in * lpr;
+  const int rows = p.heads + (MODE == kRopeOnly ? 0 : 2 * p.Hkv);
+  const int groups = (rows + per - 1) / per;
+  const int n = p.pairs, i0 = 8 * c;
+  const bool turns = p.pos != nullptr;
+  const int32_t at = turns ? p.pos[t] : 0;
+
+  // which of the lane's elements turn, and where their partners are
+  uint32_t moved = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) moved |= (i0 + e < 2 * n ? 1u : 0u) << e;
+  const bool lined = (n & 7) == 0;
+  const int mate = lane + (i0 < n ? n / 8 : -(n / 8));
+  const bool pairs_apart = turns && !p.interleaved;
+
+  float cf[8], sf[8];
+  bool ready = false;
+  // cosine and signed sine of the lane's element e
+  auto turn_of = [&](int e) __attribute__((always_inline)) {
+    const int i = i0 + e;
+    const int pair = p.interleaved ? i >> 1 : (i < n ? i : i - n);
+    double2 w = trig[wave][i < 2 * n ? pair : 0];
+    if (p.interleaved ? (i & 1) == 0 : i < n) w.y = -w.y;
+    return w;
+  };
+
+  for (int g0 = part; g0 < groups; g0 += kGroups * p.parts) {
+    Raw<T> x[kGroups], y[kGroups];
+    const T* from[kGroups];
+    int row[kGroups];
+    int64_t slot[kGroups];
+#pragma unroll
+    for (int b = 0; b < kGroups; ++b) {
+      const int g = g0 + b * p.parts;
+      row[b] = g * per + row_in;
+      if (g >= groups || row[b] >= rows || row_in >= per) row[b] = -1;
+      x[b].zero();
+      y[b].zero();
+      slot[b] = -1;
+      from[b] = nullptr;
+      if (row[b] < 0) continue;
+      const int h = row[b] - p.heads;
+      const char* base;
+      if (MODE == kRopeOnly || h < 0) {
+        base = static_cast<const char*>(p.x) + t * p.x_stride + (int64_t)row[b] * p.dim * sizeof(T);
+      } else {
+        const int kv = h < p.Hkv ? h : h - p.Hkv;
+        base = static_cast<const char*>(h < p.Hkv ? p.k : p.v) + t * p.kv_stride + (int64_t)kv * p.dim * sizeof(T);
+        slot[b] = p.slots[t * p.Hkv + kv];
+      }
+      from[b] = reinterpret_cast<const T*>(base);
+      load8(x[b], from[b] + i0);
+      if (pairs_apart && !lined && h < p.Hkv) {
+        if (i0 + 8 <= n) {
+          load8(y[b], from[b] + i0 + n);
+        } else if (i0 >= n && i0 + 8 <= 2 * n) {
+          load8(y[b], from[b] + i0 - n);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int i = i0 + e;
+            if (i < 2 * n) y[b].put(e, from[b] + (i < n ? i + n : i - n));
+          }
+        }
+      }
+    }
+    if (turns && !ready) {
+      ready = true;
+      for (int i = lane; i < n; i += kWave) {
+        double s, co;
+        sincos64((double)(at < 0 ? 0 : at) * __builtin_fabs((double)p.freq[i]), &s, &co);
+        if (p.freq[i] < 0.f) s = -s;
+        trig[wave][i] = double2{co * p.mscale, s * p.mscale};
+      }
+      wave_lds_fence();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double2 w = turn_of(e);
+        cf[e] = (float)w.x;
+        sf[e] = (float)w.y;
+      }
+    }
+    if (at < 0) return;  // a row of no sequence
+    // no lane writes before the wave's loads of these rows (rotation in place)
+    wave_lds_fence();
+#pragma unroll
+    for (int b = 0; b < kGroups; ++b) {
+      if (g0 + b * p.parts >= groups) break;
+      const int h = row[b] - p.heads;
+      const RowKind kind = MODE == kRopeOnly || h < 0 ? kRowX : (h < p.Hkv ? kRowK : kRowV);
+      float out[8];
+      if (turns) {
+        if (!p.interleaved && lined) y[b].shuffle(x[b], mate);
+        const bool turn = kind != kRowV;
+        // one branch for the wave: 64 bits where one of its rows needs them
+        const bool wide = sizeof(T) == 4 || (MODE == kStoreF8 && __builtin_amdgcn_ballot_w64(row[b] >= 0 && kind == kRowK));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float u = x[b].at(e), w = p.interleaved ? x[b].at(e ^ 1) : y[b].at(e);
+          float r = __builtin_fmaf(u, cf[e], w * sf[e]);
+          if (wide) {
+            const double2 cs = turn_of(e);
+            const float r64 = (float)__builtin_fma((double)u, cs.x, (double)w * cs.y);
+            if (sizeof(T) == 4 || kind == kRowK) r = r64;  // q as dkv_rope leaves it
+          }
+          out[e] = turn && (moved >> e & 1) ? r : u;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = x[b].at(e);
+      }
+      if (MODE == kRopeOnly || kind == kRowX) {
+        if (row[b] >= 0) {
+          T* to = reinterpret_cast<T*>(static_cast<char*>(p.out) + t * p.out_stride) + (int64_t)row[b] * p.dim + i0;
+          if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<f32x4*>(to) = f32x4{out[0], out[1], out[2], out[3]};
+            *reinterpret_cast<f32x4*>(to + 4) = f32x4{out[4], out[5], out[6], out[7]};
+          } else {
+            *reinterpret_cast<u32x4*>(to) = pack_bf16(out);
+          }
+        }
+      }
+      if constexpr (MODE == kStoreBf16) {
+        if (kind != kRowX && slot[b] >= 0 && slot[b] < p.pool_rows) {
+          char* pool = static_cast<char*>(kind == kRowK ? p.k_pages : p.v_pages);
+          *reinterpret_cast<u32x4*>(pool + (slot[b] * p.dim + i0) * 2) = pack_bf16(out);
+        }
+      }
+      if constexpr (MODE == kStoreF8) {
+        if (__builtin_amdgcn_ballot_w64(row[b] >= 0 && kind != kRowX)) {
+          float most = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) most = fmaxf(most, __builtin_isfinite(out[e]) ? __builtin_fabsf(out[e]) : 0.f);
+          // the largest of the row's 8 or 16 lanes
+          most = fmaxf(most, dpp_mov<0xB1>(most));
+          most = fmaxf(most, dpp_mov<0x4E>(most));
+          most = fmaxf(most, dpp_mov<0x141>(most));
+          if (LPR == 16) most = fmaxf(most, dpp_mov<0x140>(most));
+          const int ex = f8_exponent(__float_as_uint(most));
+          const float inv = __uint_as_float((uint32_t)(127 - ex) << 23), lim = ex == kF8MaxExp ? 240.f : 448.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) out[e] = f8_scaled(out[e], inv, lim);
+          const uint2 codes = {f8_pack4(out[0], out[1], out[2], out[3]), f8_pack4(out[4], out[5], out[6], out[7])};
+          if (kind != kRowX && slot[b] >= 0 && slot[b] < p.pool_rows) {
+            char* pool = static_cast<char*>(kind == kRowK ? p.k_pages : p.v_pages);
+            *reinterpret_cast<uint2*>(pool + slot[b] * p.dim + i0) = codes;
+            if (c == 0) p.scales[2 * slot[b] + (kind == kRowV ? 1 : 0)] = (uint8_t)(ex + 127);
+          }
+        }
+      }
+    }
+  }
+}
+
+// Waves per token: a whole token to a wave where tokens fill the card (16
+// waves a compute unit), else its row groups over several.
+constexpr int64_t kRotFill = 4096;
+
+template <typename T, int MODE>
+hipError_t launch_rotate(RotateParams p, hipStream_t stream) {
+  const int rows = p.heads + (MODE == kRopeOnly ? 0 : 2 * p.Hkv);
+  const int per = kWave / (p.dim / 8);
+  const int groups = (rows + per - 1) / per;
+  const int64_t want = (kRotFill + p.tokens - 1) / p.tokens;
+  p.parts = (int32_t)(want < groups ? (want > 1 ? want : 1) : groups);
+  const unsigned blocks = (unsigned)(((int64_t)p.tokens * p.parts + kRotWaves - 1) / kRotWaves);
+  if (p.dim == 128) hipLaunchKernelGGL((rotate_store_kernel<T, MODE, 16>), dim3(blocks), dim3(kRotThreads), 0, stream, p);
+  else if (p.dim == 64) hipLaunchKernelGGL((rotate_store_kernel<T, MODE, 8>), dim3(blocks), dim3(kRotThreads), 0, stream, p);
+  else if constexpr (MODE == kRopeOnly)
+    hipLaunchKernelGGL((rotate_store_kernel<T, MODE, 0>), dim3(blocks), dim3(kRotThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- read back
+// 16 bytes of a K and of a V row per thread, rows of one token side by side.
+// Bound by moving the rows.
+template <bool F8>
+__global__ __launch_bounds__(kRotThreads) void paged_load_kernel(LoadParams p) {
+  constexpr int kElems = F8 ? 16 : 8;
+  const int per_row = p.dim / kElems;  // a power of two
+  const int shift = 31 - __builtin_clz(per_row);
+  const int64_t i = (int64_t)blockIdx.x * kRotThreads + threadIdx.x;
+  const int64_t r = i >> shift;  // token * Hkv + head
+  if (r >= (int64_t)p.tokens * p.Hkv) return;
+  const int64_t slot = p.slots[r];
+  if (slot < 0 || slot >= p.pool_rows) return;
+  const int c = (int)(i & (per_row - 1));
+  const uint32_t t = (uint32_t)r / (uint32_t)p.Hkv;
+  const int64_t to = t * p.stride + ((r - (int64_t)t * p.Hkv) * p.dim + c * kElems) * 2;
+  const int64_t from = slot * p.dim * (F8 ? 1 : 2) + c * 16;
+  const u32x4 k = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.k_pages) + from);
+  const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.v_pages) + from);
+  u32x4* ko = reinterpret_cast<u32x4*>(static_cast<char*>(p.k_out) + to);
+  u32x4* vo = reinterpret_cast<u32x4*>(static_cast<char*>(p.v_out) + to);
+  if constexpr (F8) {
+    const uint32_t ex = *reinterpret_cast<const uint16_t*>(p.scales + 2 * slot);
+    const float kp = f8_power(ex & 0xFF), vp = f8_power(ex >> 8);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      ko[j] = u32x4{f8_pair<false>(k[2 * j], kp), f8_pair<true>(k[2 * j], kp), f8_pair<false>(k[2 * j + 1], kp),
+                    f8_pair<true>(k[2 * j + 1], kp)};
+      vo[j] = u32x4{f8_pair<false>(v[2 * j], vp), f8_pair<true>(v[2 * j], vp), f8_pair<false>(v[2 * j + 1], vp),
+                    f8_pair<true>(v[2 * j + 1], vp)};
+    }
+  } else {
+    ko[0] = k;
+    vo[0] = v;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RotateParams& p, bool f32, hipStream_t stream) {
+  return f32 ? launch_rotate<float, kRopeOnly>(p, stream) : launch_rotate<uint16_t, kRopeOnly>(p, stream);
+}
+
+hipError_t launch_paged_store(const RotateParams& p, bool f8, hipStream_t stream) {
+  return f8 ? launch_rotate<uint16_t, kStoreF8>(p, stream) : launch_rotate<uint16_t, kStoreBf16>(p, stream);
+}
+
+hipError_t launch_paged_load(const LoadParams& p, bool f8, hipStream_t stream) {
+  const int64_t n = (int64_t)p.tokens * p.Hkv * (p.dim / (f8 ? 16 : 8));
+  const dim3 grid((unsigned)((n + kRotThreads - 1) / kRotThreads)), block(kRotThreads);
+  if (f8) hipLaunchKernelGGL(paged_load_kernel<true>, grid, block, 0, stream, p);
+  else hipLaunchKernelGGL(paged_load_kernel<false>, grid, block, 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace dkv

@@ -1,0 +1,338 @@
+"""GPU parity of rotary positions, quantised writes, reading back, tree plans
+and accepted paths with the oracle.
+
+Tolerances.  dkv_rope: a bf16 result is a rounding (2^-8 of the value at most)
+after fp32 products: sine and cosine off by 2^-25 each, two products, a sum and
+mscale folded in, together below 2^-22 (|a| + |b|) mscale.  An fp32 result is a
+rounding (2^-24) of a sum in double, whose own error, and that of the angle's
+sine, stay below 2^-48 (|a| + |b|) mscale up to positions of 2^20.  Everything
+that is quantised, copied or counted is exact."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import tree_cache as tc
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+KEEP = 77.0  # what the outputs hold before a call
+
+
+@pytest.fixture(scope="module")
+def d():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2609_32663_amd as lib
+    return lib
+
+
+def _dev(x, dtype=torch.int32):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(device=DEV, dtype=dtype)
+
+
+def _rows(rng, shape, dtype=torch.bfloat16):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(dtype)
+
+
+def _freq(rng, pairs):
+    f = 10000.0 ** (-np.arange(pairs) / max(pairs, 1)) * rng.uniform(0.9, 1.1, pairs)
+    return f.astype(np.float32)
+
+
+def _check_rotated(got, x, pos, f, rot, inter, ms, dtype):
+    x64 = x.double().numpy()
+    want = tc.rope(x64, pos, f, rot, inter, ms)
+    n = rot // 2
+    pair = np.abs(x64)
+    both = pair.copy()
+    if inter:
+        both[..., 0:2 * n:2] = both[..., 1:2 * n:2] = pair[..., 0:2 * n:2] + pair[..., 1:2 * n:2]
+    else:
+        both[..., :n] = both[..., n:2 * n] = pair[..., :n] + pair[..., n:2 * n]
+    half, inner = (2.0 ** -8, 2.0 ** -22) if dtype == torch.bfloat16 else (2.0 ** -24, 2.0 ** -48)
+    tol = half * np.abs(want) + inner * ms * both * (1 + half)
+    for t in range(x.shape[0]):
+        if pos[t] < 0:
+            assert (got[t] == KEEP).all()
+        else:
+            assert (np.abs(got[t] - want[t]) <= tol[t]).all(), (t, np.abs(got[t] - want[t]).max())
+            np.testing.assert_array_equal(got[t][:, 2 * n:], x64[t][:, 2 * n:])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim, rots", [(64, [64, 32, 2, 50]), (128, [128, 64, 96, 6, 126]), (80, [80, 20]), (8, [8, 2]),
+                                       (256, [256, 200, 64])])
+@pytest.mark.parametrize("inter", [False, True])
+def test_rope(d, dtype, dim, rots, inter):
+    for rot in rots:
+        for tokens, heads, fused in ((1, 1, False), (3, 6, True), (67, 5, False), (130, 3, True)):
+            rng = np.random.default_rng([dim, rot, tokens, inter])
+            x = _rows(rng, (tokens, heads + (2 if fused else 0), dim), dtype)
+            part = x.to(DEV)[:, 1 if fused else 0:][:, :heads]
+            host = x[:, 1 if fused else 0:][:, :heads]
+            pos = rng.choice([0, 1, 17, 4095, 131071, 1 << 20], size=tokens)
+            pos[rng.integers(tokens)] = -1 if tokens > 1 else 5
+            f, ms = _freq(rng, rot // 2), float(rng.choice([1.0, 1.2]))
+            out = torch.full((tokens, heads, dim), KEEP, dtype=dtype, device=DEV)
+            d.dkv_rope(part, _dev(pos), _dev(f, torch.float32), rot, out, interleaved=inter, mscale=ms)
+            got = out.double().cpu().numpy()
+            _check_rotated(got, host, pos, f, rot, inter, np.float32(ms), dtype)
+            # in place, in the fused buffer: the same bits, the other rows as they were
+            whole = x.to(DEV)
+            view = whole[:, 1 if fused else 0:][:, :heads]
+            d.dkv_rope(view, _dev(pos), _dev(f, torch.float32), rot, view, interleaved=inter, mscale=ms)
+            want = torch.where(_dev(pos)[:, None, None] < 0, part, out)
+            assert torch.equal(view, want)
+            if fused:
+                assert torch.equal(whole[:, 0], x.to(DEV)[:, 0]) and torch.equal(whole[:, -1], x.to(DEV)[:, -1])
+
+
+def test_rope_far_positions(d):
+    """Angles of positions up to 2^31 - 1 keep their fraction of a turn."""
+    pos = np.array([2 ** 31 - 1, 2 ** 30 + 1, 123456789, 2 ** 24 + 1])
+    f = np.array([1.0, 0.77, 1e-3, 1.9], dtype=np.float32)
+    x = torch.ones(4, 1, 8)
+    out = torch.empty(4, 1, 8, device=DEV)
+    d.dkv_rope(x.to(DEV), _dev(pos), _dev(f, torch.float32), 8, out)
+    # the angle (up to 4.1e9) is rounded to 53 bits by either side: 2^-22 at most
+    want = tc.rope(x.double().numpy(), pos, f, 8)
+    assert np.abs(out.cpu().double().numpy() - want).max() <= 2.0 ** -20
+
+
+class Pools:
+    def __init__(self, fmt, pages, R, dim):
+        self.fmt, self.R, self.dim = fmt, R, dim
+        if fmt == "f8":
+            self.k = torch.full((pages, R, dim), 0xA5, dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
+            self.v = self.k.view(torch.uint8).clone().view(torch.float8_e4m3fn)
+            self.ex = torch.full((pages, R, 2), 0x77, dtype=torch.uint8, device=DEV)
+        else:
+            self.k = torch.full((pages, R, dim), KEEP, dtype=torch.bfloat16, device=DEV)
+            self.v, self.ex = self.k.clone(), None
+
+    def host(self):
+        raw = [x.view(torch.uint8).cpu().numpy() for x in (self.k, self.v)]
+        return raw + ([] if self.ex is None else [self.ex.cpu().numpy()])
+
+
+def _bf16_bytes(x):
+    return torch.from_numpy(x).float().bfloat16().contiguous().view(torch.uint8).numpy()
+
+
+@pytest.mark.parametrize("fmt", ["f8", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("Hq, Hkv", [(4, 2), (28, 4), (3, 1), (8, 8), (0, 3)])
+def test_store_and_load(d, fmt, dim, inter, Hq, Hkv):
+    for rot in (dim, dim // 2, 22, 0):
+        for tokens in (1, 5, 150):
+            rng = np.random.default_rng([dim, Hq, Hkv, rot, tokens, inter])
+            R, pages = 64, 3 * Hkv + 4
+            P = Pools(fmt, pages, R, dim)
+            before = P.host()
+            x = _rows(rng, (tokens, Hq + 2 * Hkv, dim)) * torch.from_numpy(rng.choice([1e-4, 1.0, 300.0], size=(tokens, 1, 1)))
+            x = x.to(torch.bfloat16)
+            x[rng.integers(tokens), -1] = 0.0  # a row of zeros
+            xd = x.to(DEV)
+            slots = rng.permutation(pages * R)[:tokens * Hkv].reshape(tokens, Hkv)
+            slots[rng.uniform(size=slots.shape) < 0.1] = -1
+            slots[rng.uniform(size=slots.shape) < 0.05] = pages * R
+            pos = rng.integers(0, 9000, size=tokens)
+            if tokens > 1:
+                pos[rng.integers(tokens)] = -1
+            f = _freq(rng, rot // 2)
+            q_out = torch.full((tokens, Hq, dim), KEEP, dtype=torch.bfloat16, device=DEV)
+            kw = dict(pos=_dev(pos), inv_freq=_dev(f, torch.float32), rot_dim=rot, interleaved=inter, mscale=1.25) if rot else {}
+            d.dkv_paged_store(xd[:, Hq:Hq + Hkv], xd[:, Hq + Hkv:], _dev(slots, torch.int64), P.k, P.v, scales=P.ex,
+                              q=xd[:, :Hq] if Hq else None, q_out=q_out if Hq else None, **kw)
+            # q as dkv_rope leaves it
+            if Hq:
+                want = torch.full_like(q_out, KEEP)
+                if rot:
+                    d.dkv_rope(xd[:, :Hq], kw["pos"], kw["inv_freq"], rot, want, interleaved=inter, mscale=1.25)
+                else:
+                    want = xd[:, :Hq].contiguous()
+                assert torch.equal(q_out, want)
+            # the pools: rows of the batch, and nothing else
+            k, v = (x[:, a:a + Hkv].double().numpy() for a in (Hq, Hq + Hkv))
+            skip = np.zeros(tokens, dtype=bool)
+            if rot:
+                k = tc.rope(k, pos, f, rot, inter, np.float32(1.25)).astype(np.float32).astype(np.float64)
+                skip = pos < 0
+            after, want = P.host(), [y.copy() for y in before]
+            for i, rows in enumerate((k, v)):
+                flat = want[i].reshape(pages * R, -1)
+                if fmt == "f8":
+                    codes, ex = tc.quantise(rows)
+                for t in range(tokens):
+                    for g in range(Hkv):
+                        if skip[t] or not 0 <= slots[t, g] < pages * R:
+                            continue
+                        if fmt == "f8":
+                            flat[slots[t, g]] = codes[t, g]
+                            want[2].reshape(-1, 2)[slots[t, g], i] = ex[t, g]
+                        elif i == 1 or not rot:
+                            flat[slots[t, g]] = _bf16_bytes(rows[t, g])
+                        else:  # K in bf16 comes from fp32 products
+                            got = after[0].reshape(pages * R, -1)[slots[t, g]]
+                            val = torch.from_numpy(got.copy()).view(torch.bfloat16).double().numpy()
+                            size = np.abs(x[t, Hq + g].double().numpy()).max() * 2 * 1.25
+                            assert (np.abs(val - rows[t, g]) <= 2.0 ** -8 * np.abs(rows[t, g]) + 2.0 ** -22 * size).all()
+                            flat[slots[t, g]] = got
+            for got, y in zip(after, want):
+                np.testing.assert_array_equal(got, y)
+            # and read back: the values that the codes stand for, rows without a slot as they were
+            back = torch.full((tokens, 2 * Hkv, dim), KEEP, dtype=torch.bfloat16, device=DEV)
+            d.dkv_paged_load(_dev(slots, torch.int64), P.k, P.v, back[:, :Hkv], back[:, Hkv:], scales=P.ex)
+            got = back.double().cpu().numpy()
+            for t in range(tokens):
+                for g in range(Hkv):
+                    for i in range(2):
+                        row = got[t, g + i * Hkv]
+                        if not 0 <= slots[t, g] < pages * R:
+                            assert (row == KEEP).all()
+                            continue
+                        raw = after[i].reshape(pages * R, -1)[slots[t, g]]
+                        if fmt == "f8":
+                            val = tc.row_values(raw, after[2].reshape(-1, 2)[slots[t, g], i])
+                        else:
+                            val = torch.from_numpy(raw.copy()).view(torch.bfloat16).double().numpy()
+                        np.testing.assert_array_equal(row, val)
+
+
+def test_every_code_and_exponent_reads_back(d):
+    """All 256 codes at exponents over the whole range; borders between codes, and the extremes, are stored right."""
+    R, dim = 64, 64
+    ex = np.arange(10, 248)
+    P = Pools("f8", 16, R, dim)
+    codes = np.arange(16 * R * dim, dtype=np.int64).reshape(16, R, dim) * 7 % 256
+    P.k = torch.from_numpy(codes.astype(np.uint8)).to(DEV).view(torch.float8_e4m3fn)
+    P.ex[..., 0] = torch.from_numpy(np.resize(ex, 16 * R).reshape(16, R).astype(np.uint8)).to(DEV)
+    slots = torch.arange(16 * R, device=DEV)[:, None]
+    out = torch.zeros(16 * R, 2, dim, dtype=torch.bfloat16, device=DEV)
+    d.dkv_paged_load(slots, P.k, P.v, out[:, :1], out[:, 1:], scales=P.ex)
+    want = tc.row_values(codes.reshape(-1, dim), np.resize(ex, 16 * R))
+    got = out[:, 0].double().cpu().numpy()
+    big = np.abs(want) > float(torch.finfo(torch.bfloat16).max)  # 448 * 2^120: no row that was stored holds it
+    np.testing.assert_array_equal(got[~big], want[~big])
+
+    x = np.concatenate([tc._BORDERS, tc._LADDER, -tc._BORDERS, tc._LADDER[::-1]])
+    x = np.resize(x, (40, 63)) * 2.0 ** np.arange(-20, 20)[:, None]
+    x = np.concatenate([x, 448.0 * 2.0 ** np.arange(-20.0, 20)[:, None]], axis=1)
+    rows = torch.from_numpy(x).float().bfloat16()  # borders have five significant bits: exact
+    assert (rows.double().numpy() == x).all()
+    special = torch.zeros(4, 64, dtype=torch.bfloat16)
+    special[0, :5] = torch.tensor([float("nan"), float("inf"), -float("inf"), 2.5, -1e-3])
+    special[1, :2] = torch.tensor([torch.finfo(torch.bfloat16).max, -3.2e38])
+    special[2, :3] = torch.tensor([1e-38, 2.0 ** -133, -2.0 ** -126])
+    special[3, 0] = -0.0
+    rows = torch.cat([rows, special])[:, None]
+    P = Pools("f8", 1, R, dim)
+    at = torch.arange(rows.shape[0], device=DEV)[:, None]
+    d.dkv_paged_store(rows.to(DEV), rows.to(DEV), at, P.k, P.v, scales=P.ex)
+    codes, ex = tc.quantise(rows[:, 0].double().numpy())
+    n = rows.shape[0]
+    for pool, col in ((P.k, 0), (P.v, 1)):
+        got = pool.view(torch.uint8)[0, :n].cpu().numpy()
+        nan = codes == 0x7F
+        assert ((got & 0x7F) == 0x7F)[nan].all()
+        np.testing.assert_array_equal(got[~nan], codes[~nan])
+        np.testing.assert_array_equal(P.ex[0, :n, col].cpu().numpy(), ex)
+
+
+def test_store_beyond_2_31(d):
+    """Pool offsets and slots beyond 2^31."""
+    dim, R = 128, 1024
+    pages = (1 << 31) // (R * dim) + 5
+    k = torch.zeros((pages, R, dim), dtype=torch.float8_e4m3fn, device=DEV)
+    v, ex = torch.zeros_like(k), torch.zeros((pages, R, 2), dtype=torch.uint8, device=DEV)
+    x = _rows(np.random.default_rng(0), (3, 1, dim)).to(DEV)
+    slots = torch.tensor([[pages * R - 1], [0], [pages * R - 1000]], device=DEV)
+    d.dkv_paged_store(x, x, slots, k, v, scales=ex)
+    back = torch.zeros(3, 2, dim, dtype=torch.bfloat16, device=DEV)
+    d.dkv_paged_load(slots, k, v, back[:, :1], back[:, 1:], scales=ex)
+    codes, e = tc.quantise(x[:, 0].double().cpu().numpy())
+    np.testing.assert_array_equal(back[:, 0].double().cpu().numpy(), tc.row_values(codes, e))
+    assert torch.equal(back[:, 0], back[:, 1])
+
+
+@pytest.mark.parametrize("with_parent", [True, False])
+@pytest.mark.parametrize("sizes, pad", [([1], 0), ([5, 0, 64, 65], 3), ([200, 1, 333], 0), ([1000], 7), ([2] * 300, 1)])
+def test_tree_plan(d, with_parent, sizes, pad):
+    rng = np.random.default_rng([len(sizes), pad])
+    off = np.concatenate([[0], np.cumsum(sizes)])
+    n, B = int(off[-1]) + pad, len(sizes)
+    first = rng.integers(0, 100000, size=B)
+    first[rng.integers(B)] = 2 ** 31 - 4
+    if B > 2:
+        first[B // 2] = -1
+    parent = None
+    if with_parent:
+        parent = np.concatenate([rng.integers(np.maximum(-2, np.arange(s) - 6), np.arange(s) + 1) for s in sizes]
+                                + [np.zeros(pad, dtype=np.int64)])  # some name themselves: roots
+    for most, words in ((max(sizes), -(-max(sizes) // 64)), (max(1, max(sizes) - 2), -(-max(sizes) // 64) + 1), (max(sizes), 0)):
+        pos = torch.full((n,), 55, dtype=torch.int32, device=DEV)
+        mask = torch.full((n, words), 55, dtype=torch.int64, device=DEV) if words else None
+        d.dkv_tree_plan(_dev(off), _dev(first), most, pos, parent=None if parent is None else _dev(parent), mask=mask)
+        wp, wm = tc.tree_plan(off, first, most, n, parent, words)
+        np.testing.assert_array_equal(pos.cpu().numpy(), wp)
+        if words:
+            np.testing.assert_array_equal(mask.cpu().numpy().view(np.uint64), wm)
+
+
+@pytest.mark.parametrize("fmt", ["f8", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("R", [32, 128])
+def test_accept(d, fmt, dim, R):
+    for trial in range(6):
+        rng = np.random.default_rng([dim, R, trial])
+        L, B, Hkv, most = int(rng.integers(1, 4)), int(rng.integers(1, 6)), int(rng.integers(1, 4)), int(rng.choice([1, 5, 16, 64]))
+        N = L * B
+        pps = 200 // R + 4
+        S = N * Hkv
+        table = rng.permutation(S * pps + 2)[:S * pps].reshape(S, pps)
+        table[rng.uniform(size=table.shape) < 0.03] = -1
+        table[rng.uniform(size=table.shape) < 0.02] = S * pps + 2
+        first = rng.integers(0, 100, size=N)
+        first[rng.uniform(size=N) < 0.2] = -1
+        path = np.sort(np.stack([rng.permutation(max(90, most))[:most] for _ in range(B)]), axis=1)
+        path[:, :most // 2] = np.arange(most // 2)  # a head that stays in place
+        n_path = rng.integers(-1, most + 3, size=B)
+        if most > 4:
+            path[0, 4] = path[0, 3]   # not ascending: ends there
+            path[-1, -1] = 100000     # past the table
+        pages = S * pps + 2
+        P = Pools(fmt, pages, R, dim)
+        for x in (P.k, P.v) + ((P.ex,) if P.ex is not None else ()):
+            y = x.view(torch.uint8)
+            y.copy_(torch.from_numpy(rng.integers(0, 256, size=y.shape).astype(np.uint8)))
+        before = P.host()
+        new_len = torch.full((N,), 55, dtype=torch.int32, device=DEV)
+        keep = torch.full((S, pps), 55, dtype=torch.uint8, device=DEV) if trial % 2 else None
+        d.dkv_paged_accept(_dev(first), _dev(path), _dev(n_path), _dev(table), Hkv, P.k, P.v, new_len, scales=P.ex, keep=keep)
+        want, wl, wk = tc.accept(first, path, n_path, table, R, Hkv, [x.reshape(pages, R, -1) for x in before])
+        for got, y in zip(P.host(), want):
+            np.testing.assert_array_equal(got.reshape(pages, R, -1), y)
+        assert new_len.cpu().tolist() == [55 if x is None else x for x in wl]
+        if keep is not None:
+            np.testing.assert_array_equal(keep.cpu().numpy(), np.where(wk < 0, 55, wk))
+
+
+def test_other_streams_and_empty_calls(d):
+    x = torch.ones(3, 2, 64, dtype=torch.bfloat16, device=DEV)
+    pos, f = _dev([0, 1, 2]), torch.ones(32, device=DEV)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out = torch.zeros_like(x)
+    d.dkv_rope(x, pos, f, 64, out, stream=s)
+    s.synchronize()
+    want = torch.zeros_like(x)
+    d.dkv_rope(x, pos, f, 64, want)
+    assert torch.equal(out, want)
+    none = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device=DEV)
+    d.dkv_rope(none, _dev(np.zeros(0)), f, 64, none.clone())
+    pool = torch.zeros(2, 32, 64, dtype=torch.bfloat16, device=DEV)
+    d.dkv_paged_store(none, none, torch.zeros(0, 2, dtype=torch.int64, device=DEV), pool, pool.clone())
+    d.dkv_paged_load(torch.zeros(0, 2, dtype=torch.int64, device=DEV), pool, pool, none, none)
+    torch.cuda.synchronize()
