@@ -762,7 +762,7 @@ dkv_status dkv_paged_query_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_he
  * e4m3 (sign, 4 exponent bits, 3 mantissa bits, largest value 448, no
  * infinities) in a pool [num_pages][page_rows][d] of bytes, and an exponent
  * byte 127 + e; code c stands for c * 2^e.  scales is uint8
- * [num_pages][page_rows][2], the bytes of the K and the V row.  e is the smallest
+ * [num_pages][page_rows][2], 16-byte aligned, the bytes of the K and the V row.  e is the smallest
  * with the row's largest magnitude at most 448 * 2^e, within [-117, 120]; codes
  * are rounded to nearest, ties to even.  NaN and infinities become NaN, and do
  * not count for e.  A value is off by at most 2^-4 of itself, or 2^-10 * 2^e.
@@ -875,6 +875,43 @@ dkv_status dkv_paged_load(dkv_cache_format format, int32_t num_tokens, int32_t n
                           const void *k_pages, const void *v_pages, const uint8_t *scales, int64_t num_pages,
                           int32_t page_rows, const int64_t *slots, void *k_out, void *v_out, int64_t token_stride,
                           void *stream);
+
+/* Workspace bytes for dkv_paged_tree_attn with the same shapes and rows_hint
+ * (host, no GPU call); 0 when the call needs none (workspace may be NULL). */
+size_t dkv_paged_tree_workspace_bytes(dkv_cache_format format, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                      int32_t head_dim, int32_t num_tokens, int32_t max_q, int64_t rows_hint);
+
+/*
+ * dkv_paged_tree_attn -- attention of every sequence's new tokens over a paged
+ * cache, in bf16 or quantised, with a mask over the new tokens: trees of drafted
+ * tokens, and without a mask chunks and single tokens (dkv_paged_query_attn).
+ *
+ * mask      uint64 [num_tokens][mask_words], 8-byte aligned (dkv_tree_plan writes
+ *           it), or NULL.  A token of sequence b sees the slots of its segment's
+ *           entries at positions below first_pos[b], and at first_pos[b] + j
+ *           where bit j of its row is set, j within the sequence's new tokens
+ *           (those that count: max_q).  Bits beyond mask_words * 64 count as 0.
+ *           NULL: j up to the token itself.
+ * k_pages, v_pages, scales  the pools in the cache's format; scales only for
+ *           DKV_CACHE_F8, 16-byte aligned.
+ * out       [num_tokens][Hq][d] fp32; zeros for a token that sees nothing.  Rows
+ *           of no sequence are left as they were.
+ * q, sm_scale, and the K and V of all positions below first_pos[b] + (new tokens)
+ * that entries name must be finite, also those of new tokens that a mask
+ * hides; other slots may hold anything.
+ * Every other argument as dkv_paged_query_attn's, with the workspace of
+ * dkv_paged_tree_workspace_bytes and the same rules for the launches.
+ * mask_words at most 2^20.
+ * Quantised values enter the products exactly; scores, maxima and sums are
+ * fp32; a probability enters its product with V as three bf16 parts (24 bits).
+ */
+dkv_status dkv_paged_tree_attn(dkv_cache_format format, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                               int32_t head_dim, int32_t num_tokens, int32_t max_q, const void *q, int64_t q_stride,
+                               const int32_t *tok_off, const int32_t *first_pos, const uint64_t *mask, int32_t mask_words,
+                               const void *k_pages, const void *v_pages, const uint8_t *scales, int64_t num_pages,
+                               int32_t page_rows, const int32_t *entries, const int32_t *n_entries, int32_t max_entries,
+                               float sm_scale, int64_t rows_hint, float *out, void *workspace, size_t workspace_bytes,
+                               void *stream);
 
 /*
  * dkv_paged_accept -- keep an accepted path of the drafted tokens.

@@ -29,7 +29,7 @@ __all__ = [
     "dkv_paged_append", "dkv_paged_query_workspace_bytes", "dkv_paged_query_attn",
     "DKV_CACHE_BF16", "DKV_CACHE_F8", "DKV_ROPE_PLAIN", "DKV_ROPE_LINEAR", "DKV_ROPE_BASE", "DKV_ROPE_WAVE",
     "DKV_ROPE_RAMP", "DKV_MAX_TREE", "DKV_MAX_PATH", "dkv_rope_freqs", "dkv_rope", "dkv_tree_plan", "dkv_paged_store",
-    "dkv_paged_load", "dkv_paged_accept",
+    "dkv_paged_load", "dkv_paged_tree_workspace_bytes", "dkv_paged_tree_attn", "dkv_paged_accept",
 ]
 
 (DKV_OK, DKV_ERR_INVALID_ARG, DKV_ERR_UNSUPPORTED, DKV_ERR_MISALIGNED, DKV_ERR_CAPACITY,
@@ -146,6 +146,9 @@ def library_at(path):
         "dkv_paged_store": (I32, [I32, I32, I32, I32, I32, VP, I64, VP, VP, I64, VP, VP, I32, I32, F32, VP, I64, VP, VP,
                                   VP, VP, I64, I32, VP]),
         "dkv_paged_load": (I32, [I32, I32, I32, I32, VP, VP, VP, I64, I32, VP, VP, VP, I64, VP]),
+        "dkv_paged_tree_workspace_bytes": (SZ, [I32, I32, I32, I32, I32, I32, I32, I64]),
+        "dkv_paged_tree_attn": (I32, [I32, I32, I32, I32, I32, I32, I32, VP, I64, VP, VP, VP, I32, VP, VP, VP, I64, I32, VP,
+                                      VP, I32, F32, I64, VP, VP, SZ, VP]),
         "dkv_paged_accept": (I32, [I32, I32, I32, I32, I32, VP, VP, VP, I32, VP, I32, I32, VP, VP, VP, I64, VP, VP, VP]),
         "dkv_compact_bins_workspace_bytes": (SZ, [P]),
         "dkv_compact_bins": (I32, [P, I32, VP, VP, VP, I32, VP, VP, I64, VP, VP, VP, VP, VP, SZ, VP]),
@@ -672,6 +675,38 @@ def dkv_paged_load(slots, k_pages, v_pages, k_out, v_out, scales=None, stream=No
     _check("dkv_paged_load", library().dkv_paged_load(
         fmt, tokens, Hkv, dim, k_pool, v_pool, ex, num_pages, page_rows, _typed(slots, "slots", torch.int64), k_ptr, v_ptr,
         stride, _stream_of(k_pages, stream)))
+
+
+def dkv_paged_tree_workspace_bytes(cache_format, batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q,
+                                   rows_hint=0):
+    return library().dkv_paged_tree_workspace_bytes(int(cache_format), int(batch), int(num_q_heads), int(num_kv_heads),
+                                                    int(head_dim), int(num_tokens), min(int(max_q), int(num_tokens)),
+                                                    int(rows_hint))
+
+
+def dkv_paged_tree_attn(q, tok_off, first_pos, k_pages, v_pages, entries, n_entries, sm_scale, out, workspace,
+                        num_kv_heads, max_q, mask=None, scales=None, rows_hint=0, stream=None):
+    """q: bf16 [tokens][Hq][d], tokens evenly spaced (a view of a fused projection included); tok_off: int32 [B+1];
+    first_pos: int32 [B]; k_pages, v_pages: [num_pages][page_rows][d] bf16, or float8_e4m3fn with scales uint8
+    [num_pages][page_rows][2]; entries: int32 [B*Hkv][max_entries][4]; n_entries: int32 [B*Hkv]; out: fp32
+    [tokens][Hq][d]; max_q: the most new tokens of a sequence; mask: optional int64 [tokens][words] (dkv_tree_plan's);
+    workspace: device tensor of dkv_paged_tree_workspace_bytes(...) bytes, or None when that is 0."""
+    tokens, Hq, dim = q.shape
+    B, Hkv = first_pos.shape[0], int(num_kv_heads)
+    num_pages, page_rows, depth = k_pages.shape
+    nseg, most, four = entries.shape
+    if depth != dim or nseg != B * Hkv or four != 4:
+        raise ValueError("k_pages must hold rows of q's size and entries B * Hkv lists of four int32 each")
+    fmt, k_pool, v_pool, ex = _cache(k_pages, v_pages, scales)
+    q_ptr, stride = _rows(q, "q", Hq, dim, _bf16)
+    words = 0 if mask is None else mask.shape[1]
+    ws_ptr, ws_bytes = (None, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.nbytes)
+    _check("dkv_paged_tree_attn", library().dkv_paged_tree_attn(
+        fmt, B, Hq, Hkv, dim, tokens, min(int(max_q), tokens), q_ptr, stride, _typed(tok_off, "tok_off", _i32, B + 1),
+        _typed(first_pos, "first_pos", _i32), None if mask is None else _typed(mask, "mask", torch.int64, None, (tokens, words)),
+        words, k_pool, v_pool, ex, num_pages, page_rows, _typed(entries, "entries", _i32),
+        _typed(n_entries, "n_entries", _i32, nseg), most, float(sm_scale), int(rows_hint),
+        _typed(out, "out", torch.float32, None, (tokens, Hq, dim)), ws_ptr, ws_bytes, _stream_of(q, stream)))
 
 
 def dkv_paged_accept(first_pos, path, n_path, page_table, num_kv_heads, k_pages, v_pages, new_len, scales=None, keep=None,

@@ -27,14 +27,6 @@ __device__ __forceinline__ int f8_exponent(uint32_t amax) {
   return e < kF8MinExp ? kF8MinExp : (e > kF8MaxExp ? kF8MaxExp : e);
 }
 
-// x 2^-e for the conversion: within the largest code, and NaN for what has no
-// finite value.  With the largest exponent 448 2^e lies beyond bf16; what
-// passes 240 2^e rounds to that.
-__device__ __forceinline__ float f8_scaled(float x, float inv, float most) {
-  const float y = __builtin_amdgcn_fmed3f(x * inv, -most, most);
-  return __builtin_isfinite(x) ? y : __builtin_nanf("");
-}
-
 __device__ __forceinline__ uint32_t f8_pack4(float a, float b, float c, float d) {
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);

@@ -54,6 +54,13 @@ struct QueryParams {
   const int32_t* n_entries;  // [nseg]
   int64_t num_pages, q_stride;
   int32_t max_entries, page_shift, num_tokens, max_q;
+  // Tree calls only.  mask: [num_tokens][mask_words], bit j of a token's row
+  // says whether it sees its sequence's new token j (null: those up to itself);
+  // everything before the new tokens is seen.  scales: quantised pools (rows of
+  // d codes), the exponent bytes of the K and the V row [pool rows][2].
+  const uint64_t* mask;
+  const uint8_t* scales;
+  int32_t mask_words;
 };
 
 // How a call is split, from the shapes and the caller's hint of the total
@@ -161,5 +168,7 @@ PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t h
                                 int32_t max_q, int64_t rows_hint);
 hipError_t launch_paged_query_attn(const QueryParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_paged_query_short(const QueryParams& p, int head_dim, hipStream_t stream);
+hipError_t launch_paged_tree_attn(const QueryParams& p, int head_dim, hipStream_t stream);
+hipError_t launch_paged_tree_short(const QueryParams& p, int head_dim, hipStream_t stream);
 
 }  // namespace dkv

@@ -16,6 +16,8 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t q_rsrc(const char* base, uint32_t bytes) {
   const uint64_t a = reinterpret_cast<uint64_t>(base);
@@ -174,6 +176,27 @@ __device__ __forceinline__ PagedRun paged_run(const PagedSegment& g, const i32x4
   hi = hi > kRun ? kRun : hi;
   u.lohi = ok & (lo < hi) ? lo | hi << 8 : 0;
   return u;
+}
+
+// Which of the 32 slots of a run at position `pos` a token sees, as bits: those
+// of [lo, hi) below its position (no mask), or before the new tokens and where
+// its mask row has their bit.  `cut` is the position past the token's own, `first`
+// that of its sequence's first new token.
+__device__ __forceinline__ uint32_t tree_sees(const QueryParams& p, int64_t token, int32_t cut, int32_t first, int32_t pos,
+                                              int32_t lo, int32_t hi) {
+  uint32_t sees;
+  if (p.mask != nullptr) {
+    const uint32_t* row = reinterpret_cast<const uint32_t*>(p.mask) + token * 2 * p.mask_words;
+    const int32_t rel = pos - first, w = rel >> 5, words = 2 * p.mask_words;
+    const uint32_t a = w < 0 ? ~0u : (w < words ? row[w] : 0u);
+    const uint32_t b = w + 1 < 0 ? ~0u : (w + 1 < words ? row[w + 1] : 0u);
+    sees = __builtin_amdgcn_alignbit(b, a, (uint32_t)rel & 31u);
+  } else {
+    const int32_t n = cut - pos;
+    sees = n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u);
+  }
+  const uint32_t below = hi >= 32 ? ~0u : (1u << hi) - 1u;
+  return sees & below & (lo >= 32 ? 0u : ~0u << lo);
 }
 
 }  // namespace dkv

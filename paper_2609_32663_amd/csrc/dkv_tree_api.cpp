@@ -28,6 +28,18 @@ bool format_ok(dkv_cache_format f) { return f == DKV_CACHE_BF16 || f == DKV_CACH
 // Rows of `heads` x dim elements, tokens `stride` elements apart.
 bool stride_ok(int64_t stride, int64_t heads, int32_t dim) { return stride >= heads * dim && stride <= INT32_MAX; }
 
+dkv_status check_tree(int32_t batch, int32_t hq, int32_t hkv, int32_t d, int32_t num_tokens, int32_t max_q) {
+  if (batch < 0 || hq <= 0 || hkv <= 0 || hq % hkv != 0 || num_tokens < 0 || max_q < 0) return DKV_ERR_INVALID_ARG;
+  if (hq / hkv > DKV_MAX_GROUP || (d != 64 && d != 128)) return DKV_ERR_UNSUPPORTED;
+  if ((int64_t)batch * hkv > DKV_MAX_SEGMENTS) return DKV_ERR_UNSUPPORTED;
+  // query rows per segment must fit 31 bits, workgroups of 512 threads 32 bits of work-items
+  const int64_t rows = (int64_t)(max_q < num_tokens ? max_q : num_tokens) * (hq / hkv);
+  if (rows > INT32_MAX / 2) return DKV_ERR_UNSUPPORTED;
+  if ((rows + dkv::kQueryRowsPerWG - 1) / dkv::kQueryRowsPerWG * batch * hkv > 0xFFFFFFFFLL / 512)
+    return DKV_ERR_UNSUPPORTED;
+  return DKV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -131,7 +143,7 @@ dkv_status dkv_paged_store(dkv_cache_format format, int32_t num_tokens, int32_t 
   if (num_q_heads > 0 && (q == nullptr || q_out == nullptr)) return DKV_ERR_INVALID_ARG;
   if (rot_dim > 0 && (pos == nullptr || inv_freq == nullptr)) return DKV_ERR_INVALID_ARG;
   if (!aligned16(k_new) || !aligned16(v_new) || kv_stride % 8 != 0 || !aligned16(k_pages) || !aligned16(v_pages) ||
-      !aligned(slots, 8) || !aligned(scales, 2))
+      !aligned(slots, 8) || (format == DKV_CACHE_F8 && !aligned16(scales)))
     return DKV_ERR_MISALIGNED;
   if (num_q_heads > 0 && (!aligned16(q) || !aligned16(q_out) || q_stride % 8 != 0 || q_out_stride % 8 != 0))
     return DKV_ERR_MISALIGNED;
@@ -177,7 +189,7 @@ dkv_status dkv_paged_load(dkv_cache_format format, int32_t num_tokens, int32_t n
       (format == DKV_CACHE_F8 && scales == nullptr))
     return DKV_ERR_INVALID_ARG;
   if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_out) || !aligned16(v_out) || token_stride % 8 != 0 ||
-      !aligned(slots, 8) || !aligned(scales, 2))
+      !aligned(slots, 8) || (format == DKV_CACHE_F8 && !aligned16(scales)))
     return DKV_ERR_MISALIGNED;
   dkv::LoadParams p;
   std::memset(&p, 0, sizeof(p));
@@ -220,6 +232,90 @@ dkv_status dkv_tree_plan(int32_t batch, int32_t num_tokens, int32_t max_q, const
   return hip_status(dkv::launch_tree_plan(p, (hipStream_t)stream));
 }
 
+size_t dkv_paged_tree_workspace_bytes(dkv_cache_format format, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                      int32_t head_dim, int32_t num_tokens, int32_t max_q, int64_t rows_hint) {
+  if (!format_ok(format) || check_tree(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q) != DKV_OK) return 0;
+  if (batch == 0 || num_tokens == 0 || max_q == 0) return 0;
+  const dkv::PagedPlanShape sh =
+      dkv::paged_plan_shape(batch, num_kv_heads, num_q_heads / num_kv_heads, head_dim, num_tokens,
+                            max_q < num_tokens ? max_q : num_tokens, rows_hint);
+  return sh.plan_bytes + sh.rec_bytes;
+}
+
+dkv_status dkv_paged_tree_attn(dkv_cache_format format, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                               int32_t head_dim, int32_t num_tokens, int32_t max_q, const void* q, int64_t q_stride,
+                               const int32_t* tok_off, const int32_t* first_pos, const uint64_t* mask, int32_t mask_words,
+                               const void* k_pages, const void* v_pages, const uint8_t* scales, int64_t num_pages,
+                               int32_t page_rows, const int32_t* entries, const int32_t* n_entries, int32_t max_entries,
+                               float sm_scale, int64_t rows_hint, float* out, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  if (!format_ok(format)) return DKV_ERR_INVALID_ARG;
+  const dkv_status st = check_tree(batch, num_q_heads, num_kv_heads, head_dim, num_tokens, max_q);
+  if (st != DKV_OK) return st;
+  if (!dkv::scale_in_range(sm_scale) || num_pages < 0 || max_entries < 0 || mask_words < 0) return DKV_ERR_INVALID_ARG;
+  if (!page_rows_ok(page_rows)) return DKV_ERR_UNSUPPORTED;
+  // the row space of a segment is walked with 32-bit rows, a mask row with 32-bit words
+  if (num_pages > INT32_MAX || (int64_t)max_entries * page_rows > (int64_t)1 << 30 || mask_words > 1 << 20)
+    return DKV_ERR_UNSUPPORTED;
+  if (q_stride < (int64_t)num_q_heads * head_dim || q_stride > INT32_MAX) return DKV_ERR_INVALID_ARG;
+  if (batch == 0 || num_tokens == 0 || max_q == 0) return DKV_OK;
+  if (q == nullptr || tok_off == nullptr || first_pos == nullptr || n_entries == nullptr || out == nullptr ||
+      (num_pages > 0 && (k_pages == nullptr || v_pages == nullptr)) || (max_entries > 0 && entries == nullptr) ||
+      (format == DKV_CACHE_F8 && scales == nullptr))
+    return DKV_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(entries) ||
+      q_stride % 8 != 0 || !aligned(mask, 8) || (format == DKV_CACHE_F8 && !aligned16(scales)))
+    return DKV_ERR_MISALIGNED;
+  const dkv::PagedPlanShape sh =
+      dkv::paged_plan_shape(batch, num_kv_heads, num_q_heads / num_kv_heads, head_dim, num_tokens,
+                            max_q < num_tokens ? max_q : num_tokens, rows_hint);
+  const size_t need = sh.plan_bytes + sh.rec_bytes;
+  if (need > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need)) return DKV_ERR_WORKSPACE;
+
+  dkv::QueryParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.q = q;
+  p.k = k_pages;
+  p.v = v_pages;
+  p.nseg = batch * num_kv_heads;
+  p.Hkv = num_kv_heads;
+  p.Hq = num_q_heads;
+  p.G = num_q_heads / num_kv_heads;
+  p.max_q = max_q < num_tokens ? max_q : num_tokens;
+  p.rows = p.max_q * p.G;
+  p.qtiles = (p.rows + dkv::kQueryRowsPerWG - 1) / dkv::kQueryRowsPerWG;
+  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  p.out = out;
+  p.tok_off = tok_off;
+  p.first_pos = first_pos;
+  p.entries = entries;
+  p.n_entries = n_entries;
+  p.num_pages = num_pages;
+  p.q_stride = q_stride * 2;
+  p.max_entries = max_entries;
+  p.page_shift = __builtin_ctz((unsigned)page_rows);
+  p.num_tokens = num_tokens;
+  p.mask = mask;
+  p.mask_words = mask_words;
+  p.scales = format == DKV_CACHE_F8 ? scales : nullptr;
+  if (sh.shorts) {
+    const int64_t row_bytes = (int64_t)head_dim * (format == DKV_CACHE_F8 ? 2 : 4);  // of K and V
+    p.stream_once = rows_hint <= 0 || rows_hint > dkv::kShortCachedBytes / row_bytes;
+    p.P = sh.slices;
+    p.rec_rows = sh.rec_rows;
+    p.seg_meta = static_cast<int32_t*>(workspace);
+    p.rec = reinterpret_cast<float*>(static_cast<char*>(workspace) + sh.plan_bytes);
+    return hip_status(dkv::launch_paged_tree_short(p, head_dim, (hipStream_t)stream));
+  }
+  if (sh.slices > 0) {
+    p.P = sh.slices;
+    p.max_items = (int32_t)sh.units;
+    p.plan = static_cast<int32_t*>(workspace);
+    p.rec = reinterpret_cast<float*>(static_cast<char*>(workspace) + sh.plan_bytes);
+  }
+  return hip_status(dkv::launch_paged_tree_attn(p, head_dim, (hipStream_t)stream));
+}
+
 dkv_status dkv_paged_accept(dkv_cache_format format, int32_t num_units, int32_t batch, int32_t num_kv_heads,
                             int32_t head_dim, const int32_t* first_pos, const int32_t* path, const int32_t* n_path,
                             int32_t max_path, const int32_t* page_table, int32_t pages_per_seg, int32_t page_rows,
@@ -238,7 +334,8 @@ dkv_status dkv_paged_accept(dkv_cache_format format, int32_t num_units, int32_t 
     return DKV_ERR_INVALID_ARG;
   if (num_pages > 0 && (k_pages == nullptr || v_pages == nullptr || (format == DKV_CACHE_F8 && scales == nullptr)))
     return DKV_ERR_INVALID_ARG;
-  if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned(scales, 2)) return DKV_ERR_MISALIGNED;
+  if (!aligned16(k_pages) || !aligned16(v_pages) || (format == DKV_CACHE_F8 && !aligned16(scales)))
+    return DKV_ERR_MISALIGNED;
   dkv::AcceptParams p;
   std::memset(&p, 0, sizeof(p));
   p.first_pos = first_pos;

@@ -67,6 +67,7 @@
 
 #include "dkv_device.hpp"
 #include "../../include/dkv.h"
+#include "dkv_f8.hpp"
 #include "dkv_query_device.hpp"
 
 namespace dkv {
@@ -168,10 +169,18 @@ __device__ __forceinline__ u32x4 tile_run_word(const PagedRun& u, int row_bytes)
                (uint32_t)((u.hi() - u.lo()) * row_bytes)};
 }
 
-template <int D, bool PAGED>
+// Quantised pools: where a tile's codes and exponent bytes wait for their
+// conversion, each wave's eight rows apart (nothing meets there).
+struct RawTiles {
+  uint8_t *k, *v, *kx, *vx;
+};
+
+template <int D, bool PAGED, bool F8 = false, bool TREE = false>
 __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem& item, uint16_t* k0, uint16_t* k1,
-                                           uint16_t* v0, uint16_t* v1, u32x4* table, int* counts) {
+                                           uint16_t* v0, uint16_t* v1, u32x4* table, int* counts,
+                                           const RawTiles raw = RawTiles{}) {
   using C = QCfg<D>;
+  constexpr int kPoolRow = F8 ? D : C::kRowBytes;  // bytes of a pool's row
   // bf16 parts of a probability.  Packed: two, 17 bits.  Paged: three, its 24
   // bits, at any length: two err by 2.1e-6 to 2.5e-6 of the output's norm at
   // 1,000 keys as at 131,072, three by 2.0e-7 to 5.2e-7, attention in plain fp32
@@ -346,7 +355,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       u32x4 w = {0u, 0u, 0u, 0u};
       if (i < n) {
         const int32_t r = (int32_t)from + i * kRun;
-        w = tile_run_word(paged_run(seg, entries[r >> seg.shift], r), C::kRowBytes);
+        w = tile_run_word(paged_run(seg, entries[r >> seg.shift], r), kPoolRow);
       }
       table[i] = w;
     }
@@ -402,6 +411,42 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
                                                off - x.lo() * C::kRowBytes, 0, 0, 0);
     }
   };
+  // Quantised: wave w brings rows 8w .. 8w + 7 of a tile (lane l: row l % 8, 16
+  // bytes l / 8 of it; with 64 dims the first 32 lanes), and their exponent
+  // bytes, to LDS of its own; raw_runs two phases' pairs ahead of convert, which
+  // reads them back (row l % 8, D / 8 codes l / 8), and writes the values, exact
+  // in bf16, to the tile buffers: the products then run as for bf16 pools.
+  const int crow = lane & 7, ccol = lane >> 3;
+  auto raw_runs = [&](const void* pool, const TileRun (&u)[2], uint8_t* codes, uint8_t* exps) __attribute__((always_inline)) {
+    const TileRun& x = wave_u >= 4 ? u[1] : u[0];
+    const uint64_t at = (uint64_t)(x.off_hi & 0xFFFF) << 32 | x.off;  // of the run's first slot that counts
+    const __amdgpu_buffer_rsrc_t rs = q_rsrc(static_cast<const char*>(pool) + at, x.bytes);
+    const uint32_t row = (uint32_t)(8 * (wave_u & 3));
+    if (D == 128 || lane < 32)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(codes + 8 * D * wave_u), 16,
+                                               (row + crow - x.lo()) * D + 16 * ccol, 0, 0, 0);
+    if (lane == 0)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          q_rsrc(reinterpret_cast<const char*>(p.scales) + 2 * (at / D - x.lo()), x.bytes > 0 ? 2 * kRun : 0),
+          (__attribute__((address_space(3))) void*)(exps + 16 * wave_u), 16, 2 * row, 0, 0, 0);
+  };
+  auto convert = [&](const uint8_t* codes, const uint8_t* exps, int which, uint16_t* buf, bool is_k) __attribute__((always_inline)) {
+    // a byte that belongs to no slot of the entry may be that of an infinity
+    const uint32_t e = exps[16 * wave_u + 2 * crow + which];
+    const float power = f8_power(e < 254u ? e : 254u);
+    const int R = 8 * wave + crow;
+    const uint8_t* from = codes + 8 * D * wave_u + (D == 128 ? 16 * lane : 16 * (crow + 8 * (ccol >> 1)) + 8 * (ccol & 1));
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) {
+      const uint2 c = *reinterpret_cast<const uint2*>(from + 8 * h);
+      const u32x4 w = {f8_pair<false>(c.x, power), f8_pair<true>(c.x, power), f8_pair<false>(c.y, power),
+                       f8_pair<true>(c.y, power)};
+      const int col = D / 64 * ccol + h;  // eight columns
+      const int chunk = is_k ? ((R / 16) * C::kRowChunks + col) * 16 + R % 16
+                             : ((R / 8) * (C::kRowChunks / 2) + col / 2) * 16 + (R % 8) * 2 + col % 2;
+      *reinterpret_cast<u32x4*>(buf + 8 * chunk) = w;
+    }
+  };
   auto issue = [&](const char* base, uint32_t off, int64_t kt, uint16_t* buf) __attribute__((always_inline)) {
     const int64_t left = k_hi - kt;
     const uint32_t nk = (uint32_t)(left <= 0 ? 0 : (left < kQKeys ? left : kQKeys));
@@ -455,9 +500,25 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // spread by 1 to 2 us on either side; taking the bf16 remainders by dot products
   // as well, 16 instructions fewer per half, gave nothing: the kernel runs at the
   // power limit).
-  const int32_t pos_all = PAGED ? paged_pos(blk, min(qt * kQRows + wave_rows * wave_u, rows - 1) / p.G) + 1 : 0;
+  int32_t pos_all = PAGED ? paged_pos(blk, min(qt * kQRows + wave_rows * wave_u, rows - 1) / p.G) + 1 : 0;
+  if (TREE && p.mask != nullptr) pos_all = blk.pos0;  // new tokens are seen by their bits
   auto softmax = [&](auto masked, auto rgs, float (&sc)[kRG][2][4], int64_t kh, const TileRun& u) __attribute__((always_inline)) {
-    if constexpr (PAGED) {
+    if constexpr (TREE) {
+      // slots outside the entry, or that one of the wave's rows does not see
+      if (!u.whole() || (int32_t)u.pos + kRun > pos_all) {
+        asm volatile("");
+#pragma unroll
+        for (int q = 0; q < decltype(rgs)::value; ++q) {
+          const uint32_t sees = tree_sees(p, tok_row0 + tok[q], cut[q], blk.pos0, (int32_t)u.pos, (int32_t)u.lo(),
+                                          (int32_t)u.hi()) >> 4 * kg;
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+              if (!(sees >> (16 * jj + v) & 1)) sc[q][jj][v] = -INFINITY;
+        }
+      }
+    } else if constexpr (PAGED) {
       // slots outside the entry, or past the position of one of the wave's rows
       if (!u.whole() || (int32_t)u.pos + kRun > pos_all) {
         asm volatile("");  // keeps this a branch: the selects would run for every half
@@ -685,7 +746,22 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   const bool lead = __builtin_amdgcn_readfirstlane(wave < 4 ? 1 : 0) != 0;
   float sc[kRG][2][4];
   u32x4 pp[kParts][kRG];
-  constexpr int kWaitOne = 0x0F70 | C::kDma;  // vmcnt(kDma): the younger of two tiles may still be in flight
+  // vmcnt: the younger of two tiles may still be in flight (quantised: codes and exponents)
+  constexpr int kWaitOne = 0x0F70 | (F8 ? 2 : C::kDma);
+  // quantised: the wave's rows of V of tile t, or K of the tile after it, have
+  // arrived; they become values, and those of the next tile set out
+  auto next_v = [&](uint16_t* buf, const TileRun (&u)[2]) __attribute__((always_inline)) {
+    convert(raw.v, raw.vx, 1, buf, false);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): read before they are overwritten, written before the meeting
+    __builtin_amdgcn_sched_barrier(0);
+    raw_runs(p.v, u, raw.v, raw.vx);
+  };
+  auto next_k = [&](uint16_t* buf, const TileRun (&u)[2]) __attribute__((always_inline)) {
+    convert(raw.k, raw.kx, 0, buf, true);
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_sched_barrier(0);
+    raw_runs(p.k, u, raw.k, raw.kx);
+  };
   auto vphase = [&](auto masked, auto rgs, int64_t kh, const TileRun& u) __attribute__((always_inline)) {
     softmax(masked, rgs, sc, kh, u);
     split(rgs, sc, pp);
@@ -722,9 +798,17 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     take_runs(run[0]);
     read_runs(2);
     take_runs(run[1]);
-    issue_runs(p.k, koff, run[0], kbuf[0]);
-    issue_runs(p.v, voff, run[0], vbuf[0]);
-    issue_runs(p.k, koff, run[1], kbuf[1]);
+    if constexpr (F8) {
+      raw_runs(p.k, run[0], raw.k, raw.kx);
+      raw_runs(p.v, run[0], raw.v, raw.vx);
+      __builtin_amdgcn_s_waitcnt(kWaitOne);
+      __builtin_amdgcn_sched_barrier(0);
+      next_k(kbuf[0], run[1]);
+    } else {
+      issue_runs(p.k, koff, run[0], kbuf[0]);
+      issue_runs(p.v, voff, run[0], vbuf[0]);
+      issue_runs(p.k, koff, run[1], kbuf[1]);
+    }
   } else {
     issue(kbase, koff, k_lo, kbuf[0]);
     issue(vbase, voff, k_lo, vbuf[0]);
@@ -758,9 +842,14 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     else mphase(rgs, kbuf[i], 0, vbuf[1 - i], 1, i == 1 || kt != k_lo);
     if (PAGED && L) take_runs(ahead);
     __builtin_amdgcn_s_waitcnt(kWaitOne);  // V of tile t
+    if constexpr (F8) {
+      __builtin_amdgcn_sched_barrier(0);
+      next_v(vbuf[i], run[1 - i]);
+    }
     meet();
     // 4t + 2: lead: P V of 2t, scores of 2t + 1; follow: vector phase of 2t
-    if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
+    if constexpr (F8) ;
+    else if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
     else issue(vbase, voff, kt + kQKeys, vbuf[1 - i]);
     if (PAGED && !L) read_runs(at);
     if (L) mphase(rgs, kbuf[i], 1, vbuf[i], 0, true);
@@ -772,12 +861,16 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     if (L) vphase(masked, rgs, kt + 32, second);
     else mphase(rgs, kbuf[i], 1, vbuf[i], 0, true);
     __builtin_amdgcn_s_waitcnt(kWaitOne);  // K of tile t + 1
+    if constexpr (F8) {
+      __builtin_amdgcn_sched_barrier(0);
+      next_k(kbuf[1 - i], ahead);
+    }
     meet();
     // 4t + 4: lead: P V of 2t + 1, scores of 2t + 2; follow: vector phase of 2t + 1
     if constexpr (PAGED) {
       run[i][0] = ahead[0];
       run[i][1] = ahead[1];
-      issue_runs(p.k, koff, run[i], kbuf[i]);
+      if constexpr (!F8) issue_runs(p.k, koff, run[i], kbuf[i]);
       at += 2;
     } else {
       issue(kbase, koff, kt + 2 * kQKeys, kbuf[i]);
@@ -825,15 +918,23 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     auto none = [&](auto par) __attribute__((always_inline)) {
       constexpr int i = decltype(par)::value;
       __builtin_amdgcn_s_waitcnt(kWaitOne);
+      if constexpr (F8) {
+        __builtin_amdgcn_sched_barrier(0);
+        next_v(vbuf[i], run[1 - i]);
+      }
       meet();
-      issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
+      if constexpr (!F8) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
       read_runs(at);
       take_runs(run[i]);
       at += 2;
       meet();
       __builtin_amdgcn_s_waitcnt(kWaitOne);
+      if constexpr (F8) {
+        __builtin_amdgcn_sched_barrier(0);
+        next_k(kbuf[1 - i], run[i]);
+      }
       meet();
-      issue_runs(p.k, koff, run[i], kbuf[i]);
+      if constexpr (!F8) issue_runs(p.k, koff, run[i], kbuf[i]);
       meet();
       kt += kQKeys;
     };
@@ -1019,7 +1120,8 @@ __device__ __forceinline__ int64_t unit_tiles(int32_t rows) {
 __device__ __forceinline__ int32_t unit_rows(const QueryParams& p, const PagedBlock& k, int s, int qt, bool* gaps) {
   *gaps = false;
   if (k.pos0 < 0 || p.max_entries == 0) return 0;
-  const int64_t last = (int64_t)(qt + 1) * kQRows < (int64_t)k.n * p.G ? (int64_t)(qt + 1) * kQRows : (int64_t)k.n * p.G;
+  int64_t last = (int64_t)(qt + 1) * kQRows < (int64_t)k.n * p.G ? (int64_t)(qt + 1) * kQRows : (int64_t)k.n * p.G;
+  if (p.mask != nullptr) last = (int64_t)k.n * p.G;  // a token may see any of the new ones
   return paged_rows(p, s, paged_pos(k, (int32_t)((last - 1) / p.G)), gaps);
 }
 
@@ -1211,9 +1313,12 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
   if (tid == 0) plan.head[3] = nshared;
 }
 
-template <int D>
+template <int D, bool F8 = false, bool TREE = false>
 __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
   DKV_QUERY_TILES(D);
+  constexpr int kRaw = F8 ? kQKeys * D : 16, kRawExps = F8 ? 2 * kQKeys : 16;
+  __shared__ __align__(1024) uint8_t rk[kRaw], rv[kRaw];
+  __shared__ __align__(16) uint8_t rkx[kRawExps], rvx[kRawExps];
   __shared__ __align__(16) u32x4 table[kTableRuns + kTablePad];
   __shared__ int counts[2 * kQThreads / kWave];  // runs with slots, per wave
   __shared__ PagedUnit own[kWholeRounds];  // whole units: this workgroup's
@@ -1292,7 +1397,9 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.single = true;
       x.rec = nullptr;
     }
-    query_item<D, true>(p, x, k0, k1, v0, v1, table, counts);
+    if constexpr (F8 || TREE)
+      query_item<D, true, F8, TREE>(p, x, k0, k1, v0, v1, table, counts, RawTiles{rk, rv, rkx, rvx});
+    else query_item<D, true>(p, x, k0, k1, v0, v1, table, counts);
     __syncthreads();  // the tile buffers are free for the next unit
   }
 }
@@ -1425,15 +1532,15 @@ __global__ __launch_bounds__(kMergeThreads, 5) void paged_merge_kernel(QueryPara
   *reinterpret_cast<f32x4*>(orow + 4 * c4) = A * inv;
 }
 
-template <int D>
+template <int D, bool F8 = false, bool TREE = false>
 hipError_t launch_paged_d(const QueryParams& p, hipStream_t stream) {
   if (p.plan == nullptr) {
-    hipLaunchKernelGGL((paged_query_kernel<D>), dim3((unsigned)((int64_t)p.nseg * p.qtiles)), dim3(kQThreads), 0, stream,
-                       p);
+    hipLaunchKernelGGL((paged_query_kernel<D, F8, TREE>), dim3((unsigned)((int64_t)p.nseg * p.qtiles)), dim3(kQThreads), 0,
+                       stream, p);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p);
-  hipLaunchKernelGGL((paged_query_kernel<D>), dim3((unsigned)p.P), dim3(kQThreads), 0, stream, p);
+  hipLaunchKernelGGL((paged_query_kernel<D, F8, TREE>), dim3((unsigned)p.P), dim3(kQThreads), 0, stream, p);
   if (p.P > 1)
     hipLaunchKernelGGL((paged_merge_kernel<D>), dim3((unsigned)((p.P - 1) * (kQRows * (D / 4) / kMergeThreads))),
                        dim3(kMergeThreads), 0, stream, p);
@@ -1527,6 +1634,12 @@ PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t h
 
 hipError_t launch_paged_query_attn(const QueryParams& p, int head_dim, hipStream_t stream) {
   return head_dim == 64 ? launch_paged_d<64>(p, stream) : launch_paged_d<128>(p, stream);
+}
+
+hipError_t launch_paged_tree_attn(const QueryParams& p, int head_dim, hipStream_t stream) {
+  if (p.scales != nullptr)
+    return head_dim == 64 ? launch_paged_d<64, true, true>(p, stream) : launch_paged_d<128, true, true>(p, stream);
+  return head_dim == 64 ? launch_paged_d<64, false, true>(p, stream) : launch_paged_d<128, false, true>(p, stream);
 }
 
 }  // namespace dkv

@@ -46,6 +46,7 @@
 
 #include <type_traits>
 
+#include "dkv_f8.hpp"
 #include "dkv_query_device.hpp"
 
 namespace dkv {
@@ -57,12 +58,13 @@ constexpr int kSRG = 2;     // 16-row groups per wave
 constexpr int kSMergeThreads = 256;
 constexpr int kStreamOnce = 2;  // non-temporal: every K and V byte is read once
 
-template <int D>
+template <int D, bool F8 = false>
 struct SCfg {
-  static constexpr int kRowBytes = D * 2;
+  static constexpr int kRowBytes = F8 ? D : D * 2;
+  static constexpr int kQBytes = D * 2;                  // of a query row
   static constexpr int kChunks = D / 32;                 // 16-byte chunks of a row per lane (QK)
   static constexpr int kBlocks = D / 16;                 // 16-column output blocks per lane
-  static constexpr int kRowChunks = D / 8;               // 16-byte chunks per row
+  static constexpr int kRowChunks = kRowBytes / 16;      // 16-byte chunks per row
   static constexpr int kPairs = D / 16;                  // 32-byte column pairs per row
   static constexpr int kDma = kSKeys * kRowChunks / 64;  // direct loads per tile and matrix
 };
@@ -91,15 +93,16 @@ __device__ __forceinline__ int64_t short_units(const QueryParams& p, int s) {
 // many keys (one key wave) or the stream is long enough to pay for a third
 // tile's longer start (23 tokens, 8B layer: 128K 56.7 us with two, 52.9 with
 // three; 32K 27.7 and 29.5; four are slower on both).
-template <int RW, int KW, bool NT>
+template <int RW, int KW, bool NT, bool F8>
 constexpr int short_stages() {
-  return KW == 1 || (RW > 1 && NT) ? 3 : 2;
+  return F8 || KW == 1 || (RW > 1 && NT) ? 3 : 2;
 }
 
-template <int D, int RW, int KW, bool NT, bool PAGED>
+template <int D, int RW, int KW, bool NT, bool PAGED, bool F8, bool TREE>
 __global__ __launch_bounds__(512)
 void query_short_kernel(QueryParams p) {
-  using C = SCfg<D>;
+  using C = SCfg<D, F8>;
+  static_assert(PAGED || !(F8 || TREE), "tree calls are paged");
   constexpr int RG = kSRG;
   constexpr int kThreads = RW * KW * kWave;
   constexpr int64_t kUnit = PAGED ? kRun : 1;                        // rows per unit of the split
@@ -109,14 +112,17 @@ void query_short_kernel(QueryParams p) {
   // S tiles per key wave and matrix (separate arrays: the compiler then tells
   // the direct loads into one apart from the reads of the others), and what
   // the key waves hand each other at the fold
-  constexpr int S = short_stages<RW, KW, NT>();
-  constexpr int kTile = KW * kSKeys * D;
+  constexpr int S = short_stages<RW, KW, NT, F8>();
+  constexpr int kTile = KW * kSKeys * C::kRowBytes / 2;  // in 16-bit words
   // Packed: two parts, 16 to 17 bits.  Paged: three, the probabilities' 24
   // bits; the third product hides behind the loads of these kernels.
   constexpr int kParts = PAGED ? 3 : 2;
   static_assert(S == 2 || S == 3, "the ring's arrays");
   __shared__ __align__(1024) uint16_t k0[kTile], k1[kTile], k2[S > 2 ? kTile : 8];
   __shared__ __align__(1024) uint16_t v0[kTile], v1[kTile], v2[S > 2 ? kTile : 8];
+  // quantised: the tiles' exponent bytes (64 bytes of each key wave's 256)
+  constexpr int kExps = F8 ? KW * kWave : 1;
+  __shared__ __align__(16) uint32_t x0[kExps], x1[kExps], x2[kExps];
   constexpr int OB = C::kBlocks / KW;  // 16-column output blocks that a key wave finishes
   constexpr int HB = KW == 1 ? 1 : (KW > 2 ? (OB + 1) / 2 : OB);  // handed over at a time
   __shared__ __align__(16) f32x4 fo[KW][RW][KW > 1 ? KW - 1 : 1][HB][kWave];
@@ -201,8 +207,13 @@ void query_short_kernel(QueryParams p) {
   // bytes 16c .. 16c + 15), as in query_attn.hip:
   //   K: ((R / 16) * kRowChunks + c) * 16 + R % 16
   //   V: ((R / 8) * kPairs + c / 2) * 16 + (R % 8) * 2 + c % 2
+  // Quantised rows, K and V alike: chunk c of key row R is chunk
+  //   ((R / 8) * kRowChunks + (c ^ (R / 16))) * 8 + R % 8,
+  // so an instruction reads whole rows, and the rows 16 apart that a transpose
+  // read takes together lie in other banks.
   const uint32_t koff = (uint32_t)(n16 * C::kRowBytes + 16 * kg);
   const uint32_t voff = (uint32_t)(((lane >> 1) & 7) * C::kRowBytes + 16 * (2 * kg + (lane & 1)));
+  const int frow = D == 64 ? 8 * (lane >> 5) + (lane & 7) : lane & 7, fcol = D == 64 ? (lane >> 3) & 3 : lane >> 3;
 
   for (; s < nseg; ++s) {
     int64_t seg_lo = 0, seg_hi = 0, a = 0, bnd;
@@ -239,6 +250,7 @@ void query_short_kernel(QueryParams p) {
       seg = paged_segment(p, s, (int32_t)q_uniform64((((split ? seg_hi - seg_lo : bnd) - 1) >> (p.page_shift - 5)) + 1),
                           (int32_t)q_uniform64(bnd * kUnit), paged_pos(blk, blk.n - 1) + 1);
       pos_all = paged_pos(blk, min(16 * RG * rw, rows - 1) / p.G) + 1;  // the wave's first row's position, past it
+      if (TREE && p.mask != nullptr) pos_all = blk.pos0;  // new tokens are seen by their bits
     }
     PagedRun ring[S] = {};
     const int64_t tok_row0 = PAGED ? (int64_t)blk.tok0 : (int64_t)bseq * p.n_q;
@@ -252,7 +264,7 @@ void query_short_kernel(QueryParams p) {
     // us either way).
     // Paged: a tile is one run; its descriptor covers the run's slots [lo, hi),
     // so the slots before them get wrapped offsets and read zeros too.
-    auto load = [&](uint16_t* kt, uint16_t* vt, int64_t t, PagedRun& run) __attribute__((always_inline)) {
+    auto load = [&](uint16_t* kt, uint16_t* vt, uint32_t* xt, int64_t t, PagedRun& run) __attribute__((always_inline)) {
       const int64_t left = nkeys - t * kSKeys;
       uint32_t nk = (uint32_t)(left <= 0 ? 0 : (left < kSKeys ? left : kSKeys));
       int64_t from = nk > 0 ? t * kSKeys * C::kRowBytes : 0;
@@ -266,6 +278,30 @@ void query_short_kernel(QueryParams p) {
       }
       const __amdgpu_buffer_rsrc_t ks = q_rsrc(kbase + from, nk * C::kRowBytes);
       const __amdgpu_buffer_rsrc_t vs = q_rsrc(vbase + from, nk * C::kRowBytes);
+      if constexpr (F8) {
+#pragma unroll
+        for (int i0 = 0; i0 < 2 * C::kDma; i0 += RW < C::kDma ? RW : C::kDma) {
+          if (RW > C::kDma && rw >= C::kDma) break;
+          const int i = (i0 + rw) % C::kDma;  // K's instructions, then V's
+          const int far = (D == 64 ? i : i >> 1) & 1;  // rows from 16 on
+          const uint32_t at = (uint32_t)((1024 / C::kRowBytes * i + frow) * C::kRowBytes + 16 * (fcol ^ far)) - skip;
+          if (i0 < C::kDma)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (__attribute__((address_space(3))) void*)(kt + 512 * i), 16, at, 0,
+                                                     0, NT ? kStreamOnce : 0);
+          else
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (__attribute__((address_space(3))) void*)(vt + 512 * i), 16, at, 0,
+                                                     0, NT ? kStreamOnce : 0);
+        }
+        if (rw == 0) {
+          // from the run's first slot on, so that a word's pair of rows is aligned
+          const uint32_t most = (uint32_t)((run.hi() + 1) & ~1);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(
+              q_rsrc(reinterpret_cast<const char*>(p.scales) + 2 * run.row, 2 * most),
+              (__attribute__((address_space(3))) void*)xt, 4, 4 * lane, 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        return;
+      }
 #pragma unroll
       for (int i0 = 0; i0 < C::kDma; i0 += RW) {
         const int i = i0 + rw;
@@ -285,31 +321,37 @@ void query_short_kernel(QueryParams p) {
       __builtin_amdgcn_sched_barrier(0);
     };
 
-    uint16_t* const kb[3] = {k0 + kw * kSKeys * D, k1 + kw * kSKeys * D, S > 2 ? k2 + kw * kSKeys * D : k2};
-    uint16_t* const vb[3] = {v0 + kw * kSKeys * D, v1 + kw * kSKeys * D, S > 2 ? v2 + kw * kSKeys * D : v2};
+    constexpr int kOwn = kTile / KW;  // of a key wave
+    uint16_t* const kb[3] = {k0 + kw * kOwn, k1 + kw * kOwn, S > 2 ? k2 + kw * kOwn : k2};
+    uint16_t* const vb[3] = {v0 + kw * kOwn, v1 + kw * kOwn, S > 2 ? v2 + kw * kOwn : v2};
+    uint32_t* const xb[3] = {x0 + (F8 ? kw * kWave : 0), x1 + (F8 ? kw * kWave : 0), x2 + (F8 ? kw * kWave : 0)};
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i) load(kb[i], vb[i], kw + i * KW, ring[i]);
+    for (int i = 0; i < S - 1; ++i) load(kb[i], vb[i], xb[i], kw + i * KW, ring[i]);
 
     // B operand of QK: query row 16 (RG rw + q) + n16, dims 32u + 8kg .. +7;
     // cut: the keys of the piece that the row sees; paged: the positions below which it sees
     u32x4 qb[RG][C::kChunks];
     int64_t cut[RG];
+    int mine[RG];  // the row's token of the block
 #pragma unroll
     for (int q = 0; q < RG; ++q) {
       const int r = 16 * (RG * rw + q) + n16;
       const bool ok = r < rows;
       const int tok = ok ? r / p.G : 0;
+      mine[q] = tok;
       const int64_t see = base_len + tok + 1 - a;
       cut[q] = PAGED ? paged_pos(blk, tok) + 1 : (see < nkeys ? see : nkeys);
       const char* qrow = reinterpret_cast<const char*>(p.q);
       if constexpr (PAGED)
-        qrow += (tok_row0 + tok) * p.q_stride + ((int64_t)g * p.G + (ok ? r - tok * p.G : 0)) * C::kRowBytes;
+        qrow += (tok_row0 + tok) * p.q_stride + ((int64_t)g * p.G + (ok ? r - tok * p.G : 0)) * C::kQBytes;
       else
-        qrow += ((tok_row0 + tok) * p.Hq + (int64_t)g * p.G + (ok ? r - tok * p.G : 0)) * C::kRowBytes;
+        qrow += ((tok_row0 + tok) * p.Hq + (int64_t)g * p.G + (ok ? r - tok * p.G : 0)) * C::kQBytes;
 #pragma unroll
       for (int u = 0; u < C::kChunks; ++u) {
         const u32x4 z = {0u, 0u, 0u, 0u};
-        qb[q][u] = ok ? *reinterpret_cast<const u32x4*>(qrow + 64 * u + 16 * kg) : z;
+        // quantised: a lane's 16 codes of a chunk are the dims of two products
+        const int at = F8 ? 32 * (4 * (u >> 1) + kg) + 16 * (u & 1) : 64 * u + 16 * kg;
+        qb[q][u] = ok ? *reinterpret_cast<const u32x4*>(qrow + at) : z;
         if (qneg) qb[q][u] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
       }
     }
@@ -326,10 +368,32 @@ void query_short_kernel(QueryParams p) {
     float sc[RG][2][4];
     u32x4 pp[kParts][RG];  // the probabilities' bf16 parts
     // S^T = K Q^T: lane (n16, kg) receives the scores of keys 16j + 4kg + v
-    auto qk = [&](const uint16_t* kt) __attribute__((always_inline)) {
+    auto qk = [&](const uint16_t* kt, const uint32_t* xt) __attribute__((always_inline)) {
       f32x4 acc[RG][2];
 #pragma unroll
       for (int q = 0; q < RG; ++q) acc[q][0] = acc[q][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (F8) {
+        // A lane's codes are all of one key: its power of two goes into their
+        // conversion to bf16, which is exact.
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float power = f8_power(reinterpret_cast<const uint8_t*>(xt)[2 * (16 * j + n16)]);
+          const uint16_t* kr = kt + 8 * (((2 * j + (n16 >> 3)) * C::kRowChunks + (kg ^ j)) * 8 + (n16 & 7));
+#pragma unroll
+          for (int u = 0; u < C::kChunks; u += 2) {
+            const u32x4 c = *reinterpret_cast<const u32x4*>(kr + 8 * 32 * (u >> 1));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const u32x4 ka = {f8_pair<false>(c[2 * h], power), f8_pair<true>(c[2 * h], power),
+                                f8_pair<false>(c[2 * h + 1], power), f8_pair<true>(c[2 * h + 1], power)};
+#pragma unroll
+              for (int q = 0; q < RG; ++q)
+                acc[q][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    __builtin_bit_cast(bf16x8, ka), __builtin_bit_cast(bf16x8, qb[q][u + h]), acc[q][j], 0, 0, 0);
+            }
+          }
+        }
+      } else
 #pragma unroll
       for (int u = 0; u < C::kChunks; ++u)
 #pragma unroll
@@ -348,9 +412,43 @@ void query_short_kernel(QueryParams p) {
           for (int v = 0; v < 4; ++v) sc[q][j][v] = acc[q][j][v];
     };
     // Scores of tile t to probabilities, as kParts bf16 parts.
-    auto softmax = [&](int64_t t, const PagedRun& run) __attribute__((always_inline)) {
+    auto softmax = [&](int64_t t, const PagedRun& run, const uint32_t* xt) __attribute__((always_inline)) {
       const int64_t key0 = t * kSKeys;
-      if constexpr (PAGED) {
+      // quantised: the words that hold the V exponents of this lane's keys
+      uint2 vx[2];
+      if constexpr (F8) {
+        vx[0] = *reinterpret_cast<const uint2*>(xt + 2 * kg);
+        vx[1] = *reinterpret_cast<const uint2*>(xt + 8 + 2 * kg);
+      }
+      if constexpr (TREE) {
+        // slots outside the entry, or that one of the wave's rows does not see
+        if (run.lohi != kRun << 8 || run.pos + kRun > pos_all) {
+          asm volatile("");
+#pragma unroll
+          for (int q = 0; q < RG; ++q) {
+            const uint32_t sees =
+                tree_sees(p, tok_row0 + mine[q], (int32_t)cut[q], blk.pos0, run.pos, run.lo(), run.hi()) >> 4 * kg;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int v = 0; v < 4; ++v)
+                if (!(sees >> (16 * j + v) & 1)) sc[q][j][v] = -INFINITY;
+          }
+          if constexpr (F8) {
+            // bytes that belong to no slot of the entry may hold anything
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              uint32_t w[2] = {vx[j].x, vx[j].y};
+#pragma unroll
+              for (int v = 0; v < 4; ++v) {
+                const int key = 16 * j + 4 * kg + v;
+                if (key >= run.hi() || key < run.lo()) w[v >> 1] &= ~(0xFF00u << 16 * (v & 1));
+              }
+              vx[j] = uint2{w[0], w[1]};
+            }
+          }
+        }
+      } else if constexpr (PAGED) {
         // slots outside the entry, or past the position of one of the wave's rows
         if (run.lohi != kRun << 8 || run.pos + kRun > pos_all) {
           asm volatile("");
@@ -423,6 +521,17 @@ void query_short_kernel(QueryParams p) {
           }
         l[q] += ps;
         asm volatile("" : "+v"(l[q]));  // the sum is formed here, not sunk into a later phase
+        if constexpr (F8) {
+          // V's codes enter the product as they are, their powers of two with
+          // the probabilities: a lane's codes of V are of eight keys.
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const uint32_t w = v < 2 ? vx[j].x : vx[j].y;
+              sc[q][j][v] *= __uint_as_float(((v & 1) ? w >> 1 : w << 15) & 0x7F800000u);
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           uint32_t x[kParts];
@@ -438,12 +547,24 @@ void query_short_kernel(QueryParams p) {
     auto pv = [&](const uint16_t* vt) __attribute__((always_inline)) {
       const uint16_t* vr0 = &vt[8 * ((kg >> 1) * C::kPairs * 16 + (4 * (kg & 1) + (n16 >> 2)) * 2 + ((n16 >> 1) & 1)) +
                                 4 * (n16 & 1)];
+      // Quantised: lanes 2r and 2r + 1 of group kg address the two halves of row
+      // 4kg + r (r < 4) or 16 + 4kg + r - 4 of a 16-column chunk, and lane i
+      // receives its column i of the eight rows.
+      const int far = n16 >> 3;  // rows from 16 on
+      const int row = 16 * far + 4 * kg + ((n16 >> 1) & 3);
+      const uint16_t* vq = vt + 8 * ((row >> 3) * C::kRowChunks * 8 + (row & 7)) + 4 * (n16 & 1);
 #pragma unroll
       for (int b0 = 0; b0 < C::kBlocks; b0 += 2) {
         u32x4 vf[2];
 #pragma unroll
         for (int bb = 0; bb < 2; ++bb) {
           const int b = b0 + bb;
+          if constexpr (F8) {
+            const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vq + 64 * (b0 + (bb ^ far))));
+            vf[bb] = u32x4{f8_pair<false>((uint32_t)c[0], 1.f), f8_pair<true>((uint32_t)c[0], 1.f),
+                           f8_pair<false>((uint32_t)c[1], 1.f), f8_pair<true>((uint32_t)c[1], 1.f)};
+            continue;
+          }
           const uint2 w0 = __builtin_bit_cast(
               uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vr0 + 8 * 16 * b)));
           const uint2 w1 = __builtin_bit_cast(
@@ -475,7 +596,16 @@ void query_short_kernel(QueryParams p) {
       constexpr int kOut = decltype(out)::value;
       constexpr int kWait = 0x0F70 | (kOut & 15) | ((kOut >> 4) << 14);
       __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_waitcnt(kWait);
+      if constexpr (F8) {
+        // tiles that may be out, times a wave's loads per tile: its share of
+        // the rows (none in the row waves past the instructions), and in the first
+        // row wave the exponents
+        constexpr int kRows = kOut * 2 * (RW < C::kDma ? C::kDma / RW : 1), kAll = kRows + kOut;
+        if (rw == 0) __builtin_amdgcn_s_waitcnt(0x0F70 | (kAll & 15) | ((kAll >> 4) << 14));
+        else if (rw < C::kDma) __builtin_amdgcn_s_waitcnt(0x0F70 | (kRows & 15) | ((kRows >> 4) << 14));
+      } else {
+        __builtin_amdgcn_s_waitcnt(kWait);
+      }
       if (RW > 1) {
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
         __builtin_amdgcn_s_barrier();
@@ -492,11 +622,12 @@ void query_short_kernel(QueryParams p) {
       for (int i = 0; i < S; ++i) {
         const int64_t r = r0 + i;
         if (r < nround) {
-          if (RW == 1) load(kb[(i + S - 1) % S], vb[(i + S - 1) % S], kw + (r + S - 1) * KW, ring[(i + S - 1) % S]);
-          arrive(std::integral_constant<int, (RW == 1 ? S - 1 : S - 2) * 2 * C::kDma / RW>{});
-          if (RW > 1) load(kb[(i + S - 1) % S], vb[(i + S - 1) % S], kw + (r + S - 1) * KW, ring[(i + S - 1) % S]);
-          qk(kb[i]);
-          softmax(kw + r * KW, ring[i]);
+          if (RW == 1) load(kb[(i + S - 1) % S], vb[(i + S - 1) % S], xb[(i + S - 1) % S], kw + (r + S - 1) * KW, ring[(i + S - 1) % S]);
+          constexpr int kTilesOut = RW == 1 ? S - 1 : S - 2;
+          arrive(std::integral_constant<int, F8 ? kTilesOut : kTilesOut * 2 * C::kDma / RW>{});
+          if (RW > 1) load(kb[(i + S - 1) % S], vb[(i + S - 1) % S], xb[(i + S - 1) % S], kw + (r + S - 1) * KW, ring[(i + S - 1) % S]);
+          qk(kb[i], xb[i]);
+          softmax(kw + r * KW, ring[i], xb[i]);
           pv(vb[i]);
         }
       }
@@ -683,24 +814,25 @@ __global__ __launch_bounds__(kSMergeThreads) void query_short_merge_kernel(Query
   }
 }
 
-template <int D, int RW, int KW, bool PAGED>
+template <int D, int RW, int KW, bool PAGED, bool F8, bool TREE>
 hipError_t launch_short_r(const QueryParams& p, hipStream_t stream) {
   const size_t lds = p.P > 0 ? ((PAGED ? 1 : 2) * (size_t)p.nseg + 1) * sizeof(int64_t) : 0;
   const dim3 grid((unsigned)(p.P > 0 ? p.P : p.nseg)), block(RW * KW * kWave);
-  if (p.stream_once) hipLaunchKernelGGL((query_short_kernel<D, RW, KW, true, PAGED>), grid, block, lds, stream, p);
-  else hipLaunchKernelGGL((query_short_kernel<D, RW, KW, false, PAGED>), grid, block, lds, stream, p);
+  if (p.stream_once)
+    hipLaunchKernelGGL((query_short_kernel<D, RW, KW, true, PAGED, F8, TREE>), grid, block, lds, stream, p);
+  else hipLaunchKernelGGL((query_short_kernel<D, RW, KW, false, PAGED, F8, TREE>), grid, block, lds, stream, p);
   if (p.P > 1)
     hipLaunchKernelGGL((query_short_merge_kernel<D, PAGED>), dim3((unsigned)(p.nseg * p.rows)), dim3(kSMergeThreads), 0,
                        stream, p);
   return hipGetLastError();
 }
 
-template <int D, bool PAGED>
+template <int D, bool PAGED, bool F8 = false, bool TREE = false>
 hipError_t launch_short_d(const QueryParams& p, hipStream_t stream) {
-  if (p.rows <= 32) return launch_short_r<D, 1, 4, PAGED>(p, stream);
-  if (p.rows <= 64) return launch_short_r<D, 2, 2, PAGED>(p, stream);
-  if (p.rows <= 128) return launch_short_r<D, 4, 2, PAGED>(p, stream);
-  return launch_short_r<D, 8, 1, PAGED>(p, stream);
+  if (p.rows <= 32) return launch_short_r<D, 1, 4, PAGED, F8, TREE>(p, stream);
+  if (p.rows <= 64) return launch_short_r<D, 2, 2, PAGED, F8, TREE>(p, stream);
+  if (p.rows <= 128) return launch_short_r<D, 4, 2, PAGED, F8, TREE>(p, stream);
+  return launch_short_r<D, 8, 1, PAGED, F8, TREE>(p, stream);
 }
 
 }  // namespace
@@ -711,6 +843,12 @@ hipError_t launch_query_short(const QueryParams& p, int head_dim, hipStream_t st
 
 hipError_t launch_paged_query_short(const QueryParams& p, int head_dim, hipStream_t stream) {
   return head_dim == 64 ? launch_short_d<64, true>(p, stream) : launch_short_d<128, true>(p, stream);
+}
+
+hipError_t launch_paged_tree_short(const QueryParams& p, int head_dim, hipStream_t stream) {
+  if (p.scales != nullptr)
+    return head_dim == 64 ? launch_short_d<64, true, true, true>(p, stream) : launch_short_d<128, true, true, true>(p, stream);
+  return head_dim == 64 ? launch_short_d<64, true, false, true>(p, stream) : launch_short_d<128, true, false, true>(p, stream);
 }
 
 }  // namespace dkv

@@ -110,6 +110,14 @@ __device__ __forceinline__ u32x4 pack_bf16(const float (&y)[8]) {
   return w;
 }
 
+// x 2^-e for the conversion: within the largest code, and NaN for what has no
+// finite value.  With the largest exponent 448 2^e lies beyond bf16; what
+// passes 240 2^e rounds to that.
+__device__ __forceinline__ float f8_scaled(float x, float inv, float most) {
+  const float y = __builtin_amdgcn_fmed3f(x * inv, -most, most);
+  return __builtin_isfinite(x) ? y : __builtin_nanf("");
+}
+
 enum RowKind { kRowX, kRowK, kRowV };
 enum StoreMode { kRopeOnly, kStoreBf16, kStoreF8 };
 

@@ -15,7 +15,7 @@ from oracle import tree_cache as tc
 
 A = ctypes.c_void_p(0x10000)    # fake 16-byte-aligned device address
 MIS = ctypes.c_void_p(0x10008)  # 8-byte-aligned only
-ODD = ctypes.c_void_p(0x10001)
+ODD = ctypes.c_void_p(0x10002)
 NUL = None
 
 
