@@ -808,8 +808,8 @@ dkv_status dkv_rope_freqs(dkv_rope_scaling kind, int32_t rot_dim, double base, d
  * interleaved  0: pair i is elements i and i + rot_dim / 2; otherwise 2i and 2i + 1.
  * head_dim a multiple of 8, at most 256 (DKV_ERR_UNSUPPORTED otherwise, as when
  * num_tokens * num_heads > 2^24 - 1).
- * Angles are computed in double; the result is rounded once (bf16 rows: after
- * fp32 products).
+ * Angles and products are computed in double; a result is rounded to fp32, and
+ * from there to `dtype`.
  */
 dkv_status dkv_rope(dkv_dtype dtype, int32_t num_tokens, int32_t num_heads, int32_t head_dim, const void *x,
                     int64_t x_stride, const int32_t *pos, const float *inv_freq, int32_t rot_dim, int32_t interleaved,
@@ -852,8 +852,8 @@ dkv_status dkv_tree_plan(int32_t batch, int32_t num_tokens, int32_t max_q, const
  * slots     int64 [num_tokens][Hkv] as dkv_page_extend writes them; a row with a
  *           slot outside [0, num_pages * page_rows) is skipped.  What rows with
  *           the same slot leave there is unspecified.
- * K is rotated in double where it is quantised next, in fp32 otherwise, and
- * rounded once, to the cache's format.  head_dim 64 or 128; strides multiples
+ * K is rotated as by dkv_rope, but rounded from fp32 to the cache's format at
+ * once.  head_dim 64 or 128; strides multiples
  * of 8 elements.
  */
 dkv_status dkv_paged_store(dkv_cache_format format, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads,

@@ -5,10 +5,11 @@
 //   (a, b) -> m (a cos - b sin, a sin + b cos),
 // with a, b elements i and i + n of the head (half layout, n pairs) or 2i and
 // 2i + 1 (interleaved); the rest of the head stays.  Angles are taken in 64
-// bits: at t = 10^6 an fp32 product is off by 0.06.  bf16 rows are turned in
-// fp32 (the result is rounded to 8 bits), fp32 rows and rows that are quantised
-// next in 64 bits: an error in the last of fp32's bits would put values next to
-// a border of the four-bit codes on its other side.
+// bits: at t = 10^6 an fp32 product is off by 0.06.  The products are in 64 bits
+// too, so that a result is rounded once, to fp32 (and from there to the rows'
+// type): fp32 products put one bf16 result of 10^5 on the other side of a
+// border, which attention then shows (outputs off by 2.3e-5 of their norm).  They
+// cost nothing beside the rows' way through memory.
 //
 // One wave per token (or `parts` waves where tokens are few, to fill the card):
 // its lanes take the sine and cosine of a pair each and exchange them through
@@ -19,6 +20,8 @@
 // all of it.
 
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "dkv_f8.hpp"
 #include "dkv_tree.hpp"
@@ -121,15 +124,16 @@ __device__ __forceinline__ float f8_scaled(float x, float inv, float most) {
 enum RowKind { kRowX, kRowK, kRowV };
 enum StoreMode { kRopeOnly, kStoreBf16, kStoreF8 };
 
-// LPR: lanes per row, 0 for any (dim / 8, at most 32).
-template <typename T, int MODE, int LPR>
+// LPR: lanes per row, 0 for any (dim / 8, at most 32).  FAR: an element's partner
+// is read from memory (half layout, pairs that do not line up with lanes).
+template <typename T, int MODE, int LPR, bool FAR>
 __global__ __launch_bounds__(kRotThreads) void rotate_store_kernel(RotateParams p) {
   __shared__ double2 trig[kRotWaves][kMaxPairs];
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const int64_t id = (int64_t)blockIdx.x * kRotWaves + wave;
-  const int64_t t = id / p.parts;
-  const int part = (int)(id - t * p.parts);
+  const int32_t t = p.parts == 1 ? (int32_t)id : (int32_t)((uint32_t)id / (uint32_t)p.parts);
+  const int part = (int)(id - (int64_t)t * p.parts);
   if (t >= p.tokens) return;
   const int lpr = LPR > 0 ? LPR : p.dim / 8;
   const int per = kWave / lpr;  // rows of a group
@@ -139,29 +143,16 @@ __global__ __launch_bounds__(kRotThreads) void rotate_store_kernel(RotateParams 
   const int n = p.pairs, i0 = 8 * c;
   const bool turns = p.pos != nullptr;
   const int32_t at = turns ? p.pos[t] : 0;
-
-  // which of the lane's elements turn, and where their partners are
-  uint32_t moved = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) moved |= (i0 + e < 2 * n ? 1u : 0u) << e;
-  const bool lined = (n & 7) == 0;
+  const char* const xt = static_cast<const char*>(p.x) + t * p.x_stride;
+  const char* const kt = static_cast<const char*>(p.k) + t * p.kv_stride;
+  const char* const vt = static_cast<const char*>(p.v) + t * p.kv_stride;
+  // the lane that holds the partners
   const int mate = lane + (i0 < n ? n / 8 : -(n / 8));
-  const bool pairs_apart = turns && !p.interleaved;
-
-  float cf[8], sf[8];
+  double cs[8], sn[8];
   bool ready = false;
-  // cosine and signed sine of the lane's element e
-  auto turn_of = [&](int e) __attribute__((always_inline)) {
-    const int i = i0 + e;
-    const int pair = p.interleaved ? i >> 1 : (i < n ? i : i - n);
-    double2 w = trig[wave][i < 2 * n ? pair : 0];
-    if (p.interleaved ? (i & 1) == 0 : i < n) w.y = -w.y;
-    return w;
-  };
 
   for (int g0 = part; g0 < groups; g0 += kGroups * p.parts) {
-    Raw<T> x[kGroups], y[kGroups];
-    const T* from[kGroups];
+    Raw<T> x[kGroups], y[FAR ? kGroups : 1];
     int row[kGroups];
     int64_t slot[kGroups];
 #pragma unroll
@@ -170,31 +161,31 @@ __global__ __launch_bounds__(kRotThreads) void rotate_store_kernel(RotateParams 
       row[b] = g * per + row_in;
       if (g >= groups || row[b] >= rows || row_in >= per) row[b] = -1;
       x[b].zero();
-      y[b].zero();
+      if constexpr (FAR) y[b].zero();
       slot[b] = -1;
-      from[b] = nullptr;
       if (row[b] < 0) continue;
       const int h = row[b] - p.heads;
       const char* base;
       if (MODE == kRopeOnly || h < 0) {
-        base = static_cast<const char*>(p.x) + t * p.x_stride + (int64_t)row[b] * p.dim * sizeof(T);
+        base = xt + (int64_t)row[b] * p.dim * sizeof(T);
       } else {
         const int kv = h < p.Hkv ? h : h - p.Hkv;
-        base = static_cast<const char*>(h < p.Hkv ? p.k : p.v) + t * p.kv_stride + (int64_t)kv * p.dim * sizeof(T);
-        slot[b] = p.slots[t * p.Hkv + kv];
+        base = (h < p.Hkv ? kt : vt) + (int64_t)kv * p.dim * sizeof(T);
+        slot[b] = p.slots[(int64_t)t * p.Hkv + kv];
       }
-      from[b] = reinterpret_cast<const T*>(base);
-      load8(x[b], from[b] + i0);
-      if (pairs_apart && !lined && h < p.Hkv) {
+      const T* from = reinterpret_cast<const T*>(base);
+      load8(x[b], from + i0);
+      if constexpr (FAR) {
+        if (h >= p.Hkv) continue;
         if (i0 + 8 <= n) {
-          load8(y[b], from[b] + i0 + n);
+          load8(y[b], from + i0 + n);
         } else if (i0 >= n && i0 + 8 <= 2 * n) {
-          load8(y[b], from[b] + i0 - n);
+          load8(y[b], from + i0 - n);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const int i = i0 + e;
-            if (i < 2 * n) y[b].put(e, from[b] + (i < n ? i + n : i - n));
+            if (i < 2 * n) y[b].put(e, from + (i < n ? i + n : i - n));
           }
         }
       }
@@ -203,16 +194,21 @@ __global__ __launch_bounds__(kRotThreads) void rotate_store_kernel(RotateParams 
       ready = true;
       for (int i = lane; i < n; i += kWave) {
         double s, co;
-        sincos64((double)(at < 0 ? 0 : at) * __builtin_fabs((double)p.freq[i]), &s, &co);
-        if (p.freq[i] < 0.f) s = -s;
+        const float f = p.freq[i];
+        sincos64((double)(at < 0 ? 0 : at) * __builtin_fabs((double)f), &s, &co);
+        if (f < 0.f) s = -s;
         trig[wave][i] = double2{co * p.mscale, s * p.mscale};
       }
       wave_lds_fence();
+      // cosine and signed sine of the lane's elements; 1 and 0 for those that stay
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const double2 w = turn_of(e);
-        cf[e] = (float)w.x;
-        sf[e] = (float)w.y;
+        const int i = i0 + e;
+        const int pair = p.interleaved ? i >> 1 : (i < n ? i : i - n);
+        const bool stays = i >= 2 * n;
+        const double2 w = trig[wave][stays ? 0 : pair];
+        cs[e] = stays ? 1.0 : w.x;
+        sn[e] = stays ? 0.0 : ((p.interleaved ? (i & 1) != 0 : i >= n) ? w.y : -w.y);
       }
     }
     if (at < 0) return;  // a row of no sequence
@@ -224,25 +220,22 @@ __global__ __launch_bounds__(kRotThreads) void rotate_store_kernel(RotateParams 
       const int h = row[b] - p.heads;
       const RowKind kind = MODE == kRopeOnly || h < 0 ? kRowX : (h < p.Hkv ? kRowK : kRowV);
       float out[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e] = x[b].at(e);
       if (turns) {
-        if (!p.interleaved && lined) y[b].shuffle(x[b], mate);
-        const bool turn = kind != kRowV;
-        // one branch for the wave: 64 bits where one of its rows needs them
-        const bool wide = sizeof(T) == 4 || (MODE == kStoreF8 && __builtin_amdgcn_ballot_w64(row[b] >= 0 && kind == kRowK));
+        Raw<T> m;
+        if constexpr (FAR) m = y[b];
+        else if (!p.interleaved) m.shuffle(x[b], mate);
+        else m = x[b];
+        if (__builtin_amdgcn_ballot_w64(row[b] >= 0 && kind != kRowV)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float u = x[b].at(e), w = p.interleaved ? x[b].at(e ^ 1) : y[b].at(e);
-          float r = __builtin_fmaf(u, cf[e], w * sf[e]);
-          if (wide) {
-            const double2 cs = turn_of(e);
-            const float r64 = (float)__builtin_fma((double)u, cs.x, (double)w * cs.y);
-            if (sizeof(T) == 4 || kind == kRowK) r = r64;  // q as dkv_rope leaves it
+          for (int e = 0; e < 8; ++e) {
+            const float w = !FAR && p.interleaved ? m.at(e ^ 1) : m.at(e);
+            const float r = (float)__builtin_fma((double)out[e], cs[e], (double)w * sn[e]);
+            // what stays keeps its bits
+            if (kind != kRowV && i0 + e < 2 * n) out[e] = r;
           }
-          out[e] = turn && (moved >> e & 1) ? r : u;
         }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = x[b].at(e);
       }
       if (MODE == kRopeOnly || kind == kRowX) {
         if (row[b] >= 0) {
@@ -299,10 +292,15 @@ hipError_t launch_rotate(RotateParams p, hipStream_t stream) {
   const int64_t want = (kRotFill + p.tokens - 1) / p.tokens;
   p.parts = (int32_t)(want < groups ? (want > 1 ? want : 1) : groups);
   const unsigned blocks = (unsigned)(((int64_t)p.tokens * p.parts + kRotWaves - 1) / kRotWaves);
-  if (p.dim == 128) hipLaunchKernelGGL((rotate_store_kernel<T, MODE, 16>), dim3(blocks), dim3(kRotThreads), 0, stream, p);
-  else if (p.dim == 64) hipLaunchKernelGGL((rotate_store_kernel<T, MODE, 8>), dim3(blocks), dim3(kRotThreads), 0, stream, p);
-  else if constexpr (MODE == kRopeOnly)
-    hipLaunchKernelGGL((rotate_store_kernel<T, MODE, 0>), dim3(blocks), dim3(kRotThreads), 0, stream, p);
+  const bool far = p.pos != nullptr && !p.interleaved && p.pairs % 8 != 0;
+  const auto launch = [&](auto lpr) {
+    constexpr int L = decltype(lpr)::value;
+    if (far) hipLaunchKernelGGL((rotate_store_kernel<T, MODE, L, true>), dim3(blocks), dim3(kRotThreads), 0, stream, p);
+    else hipLaunchKernelGGL((rotate_store_kernel<T, MODE, L, false>), dim3(blocks), dim3(kRotThreads), 0, stream, p);
+  };
+  if (p.dim == 128) launch(std::integral_constant<int, 16>{});
+  else if (p.dim == 64) launch(std::integral_constant<int, 8>{});
+  else if constexpr (MODE == kRopeOnly) launch(std::integral_constant<int, 0>{});
   return hipGetLastError();
 }
 
