@@ -41,4 +41,68 @@ __device__ __forceinline__ uint32_t f8_pair(uint32_t codes, float power) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, power, HALF));
 }
 
+// The same codes without a power, exact in fp16.
+typedef __fp16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
+template <bool HALF>
+__device__ __forceinline__ uint32_t f8_pair_f16(uint32_t codes) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, 1.f, HALF));
+}
+
+// Attention over quantised V.  The weight of key j's codes is 2^(s_j + e_j), s_j
+// its score in log2 units: the running maximum M is that of s_j + e_j in place of
+// the scores', and whole (rounded up), so that the exponent byte less M is exact
+// and a weight's exponent is rounded once, where it is small (a sum with the byte
+// first would be rounded near 2^7: outputs off by 2.4e-6 of their norm).  The
+// largest weights of a row are then near one whatever the rows of V measure, and
+// two fp16 parts, cut to 11 bits each, hold 22 bits of a weight (kF8Up raises
+// them by 2^7: the smaller ones then stay clear of fp16's subnormals, and 2^(7 + 8)
+// of a lazy maximum below its largest), for which codes, exact in fp16, need one
+// product less than bf16 parts do.  The sum of the probabilities takes 2^-e_j back, in
+// fp32.  It could only overflow where thousands of keys with |V| below 2^-100
+// outweigh all others: kept below 2^126 it is then still no infinity, and the
+// output zero.  A row that has seen no key has M = kF8None.
+constexpr float kF8Up = 7.f;
+constexpr float kF8SumMax = 0x1p126f;
+constexpr float kF8None = -0x1p127f;
+
+struct F8Keys {
+  float byte[8], back[8];  // exponent byte of the lane's key, and 2^(127 - byte)
+};
+
+// From the words of the lane's keys 4kg .. 4kg + 3 of two 16-key blocks
+// (exponent bytes K V K V).
+__device__ __forceinline__ F8Keys f8_keys(const uint2 (&w)[2]) {
+  F8Keys k;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t x = (j & 2) ? w[j >> 2].y : w[j >> 2].x;
+    const uint32_t b = (x >> ((j & 1) ? 24 : 8)) & 0xFFu;
+    k.byte[j] = (float)b;
+    k.back[j] = __builtin_amdgcn_ldexpf(1.f, 127 - (int)b);
+  }
+  return k;
+}
+
+// The same from words of V's bytes alone.
+__device__ __forceinline__ F8Keys f8_keys_v(const uint32_t (&w)[2]) {
+  F8Keys k;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t b = (w[j >> 2] >> (8 * (j & 3))) & 0xFFu;
+    k.byte[j] = (float)b;
+    k.back[j] = __builtin_amdgcn_ldexpf(1.f, 127 - (int)b);
+  }
+  return k;
+}
+
+// Two weights as two fp16 pairs.
+__device__ __forceinline__ void f16_parts(float x0, float x1, uint32_t& a, uint32_t& b) {
+  const auto h = __builtin_amdgcn_cvt_pkrtz(x0, x1);
+  const float r0 = __builtin_fmaf((float)h[0], -1.f, x0), r1 = __builtin_fmaf((float)h[1], -1.f, x1);
+  a = __builtin_bit_cast(uint32_t, h);
+  b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(r0, r1));
+}
+
 }  // namespace dkv

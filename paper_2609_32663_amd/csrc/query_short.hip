@@ -54,7 +54,7 @@ namespace dkv {
 namespace {
 
 constexpr int kSKeys = 32;  // keys per tile
-constexpr int kSRG = 2;     // 16-row groups per wave
+constexpr int kSRG = 2;     // 16-row groups per wave (quantised: one for up to 16 rows)
 constexpr int kSMergeThreads = 256;
 constexpr int kStreamOnce = 2;  // non-temporal: every K and V byte is read once
 
@@ -95,15 +95,15 @@ __device__ __forceinline__ int64_t short_units(const QueryParams& p, int s) {
 // three; 32K 27.7 and 29.5; four are slower on both).
 template <int RW, int KW, bool NT, bool F8>
 constexpr int short_stages() {
-  return F8 || KW == 1 || (RW > 1 && NT) ? 3 : 2;
+  if (F8) return KW == 8 ? 2 : 3;
+  return KW == 1 || (RW > 1 && NT) ? 3 : 2;
 }
 
-template <int D, int RW, int KW, bool NT, bool PAGED, bool F8, bool TREE>
+template <int D, int RW, int KW, bool NT, bool PAGED, bool F8, bool TREE, int RG>
 __global__ __launch_bounds__(512)
 void query_short_kernel(QueryParams p) {
   using C = SCfg<D, F8>;
   static_assert(PAGED || !(F8 || TREE), "tree calls are paged");
-  constexpr int RG = kSRG;
   constexpr int kThreads = RW * KW * kWave;
   constexpr int64_t kUnit = PAGED ? kRun : 1;                        // rows per unit of the split
   constexpr int64_t kSegCost = 196608 / (2 * C::kRowBytes) / kUnit;  // as the decode step's
@@ -116,16 +116,23 @@ void query_short_kernel(QueryParams p) {
   constexpr int kTile = KW * kSKeys * C::kRowBytes / 2;  // in 16-bit words
   // Packed: two parts, 16 to 17 bits.  Paged: three, the probabilities' 24
   // bits; the third product hides behind the loads of these kernels.
-  constexpr int kParts = PAGED ? 3 : 2;
+  // Quantised: two of fp16 (dkv_f8.hpp).
+  constexpr int kParts = PAGED && !F8 ? 3 : 2;
   static_assert(S == 2 || S == 3, "the ring's arrays");
   __shared__ __align__(1024) uint16_t k0[kTile], k1[kTile], k2[S > 2 ? kTile : 8];
   __shared__ __align__(1024) uint16_t v0[kTile], v1[kTile], v2[S > 2 ? kTile : 8];
   // quantised: the tiles' exponent bytes (64 bytes of each key wave's 256)
   constexpr int kExps = F8 ? KW * kWave : 1;
   __shared__ __align__(16) uint32_t x0[kExps], x1[kExps], x2[kExps];
-  constexpr int OB = C::kBlocks / KW;  // 16-column output blocks that a key wave finishes
+  constexpr int FW = KW < C::kBlocks ? KW : C::kBlocks;  // key waves that finish 16-column output blocks
+  constexpr int OB = C::kBlocks / FW;                    // and how many each
   constexpr int HB = KW == 1 ? 1 : (KW > 2 ? (OB + 1) / 2 : OB);  // handed over at a time
-  __shared__ __align__(16) f32x4 fo[KW][RW][KW > 1 ? KW - 1 : 1][HB][kWave];
+  typedef f32x4 Hand[RW][KW > 1 ? KW - 1 : 1][HB][kWave];
+  constexpr bool kOver = KW == 8 && D == 128;  // no room of its own: over the tiles, which are done with by then
+  constexpr int FK = kOver ? FW / 2 : FW;  // waves that finish at a time
+  static_assert(!kOver || sizeof(Hand) * FK <= sizeof(k0), "the hand-over's room");
+  __shared__ __align__(16) f32x4 fo_own[kOver ? 1 : FK * RW * (KW > 1 ? KW - 1 : 1) * HB * kWave];
+  Hand* const fo = reinterpret_cast<Hand*>(kOver ? reinterpret_cast<f32x4*>(k0) : fo_own);
   __shared__ __align__(16) float fm[KW][RW][RG][16], fl[KW][RW][RG][16];
   __shared__ int64_t red[RW * KW + 1];
 
@@ -361,7 +368,7 @@ void query_short_kernel(QueryParams p) {
     for (int q = 0; q < RG; ++q) {
 #pragma unroll
       for (int b = 0; b < C::kBlocks; ++b) o[q][b][0] = o[q][b][1] = o[q][b][2] = o[q][b][3] = 0.f;
-      m[q] = -INFINITY;
+      m[q] = F8 ? kF8None : -INFINITY;
       l[q] = 0.f;
     }
 
@@ -375,24 +382,28 @@ void query_short_kernel(QueryParams p) {
       if constexpr (F8) {
         // A lane's codes are all of one key: its power of two goes into their
         // conversion to bf16, which is exact.
+        float power[2];
+        u32x4 c[C::kChunks / 2][2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float power = f8_power(reinterpret_cast<const uint8_t*>(xt)[2 * (16 * j + n16)]);
-          const uint16_t* kr = kt + 8 * (((2 * j + (n16 >> 3)) * C::kRowChunks + (kg ^ j)) * 8 + (n16 & 7));
+        for (int j = 0; j < 2; ++j) power[j] = f8_power(reinterpret_cast<const uint8_t*>(xt)[2 * (16 * j + n16)]);
 #pragma unroll
-          for (int u = 0; u < C::kChunks; u += 2) {
-            const u32x4 c = *reinterpret_cast<const u32x4*>(kr + 8 * 32 * (u >> 1));
+        for (int u = 0; u < C::kChunks / 2; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const u32x4 ka = {f8_pair<false>(c[2 * h], power), f8_pair<true>(c[2 * h], power),
-                                f8_pair<false>(c[2 * h + 1], power), f8_pair<true>(c[2 * h + 1], power)};
+          for (int j = 0; j < 2; ++j)
+            c[u][j] = *reinterpret_cast<const u32x4*>(
+                kt + 8 * (((2 * j + (n16 >> 3)) * C::kRowChunks + (kg ^ j)) * 8 + (n16 & 7)) + 8 * 32 * u);
 #pragma unroll
-              for (int q = 0; q < RG; ++q)
-                acc[q][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    __builtin_bit_cast(bf16x8, ka), __builtin_bit_cast(bf16x8, qb[q][u + h]), acc[q][j], 0, 0, 0);
-            }
+        for (int u = 0; u < C::kChunks; ++u)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t lo = c[u >> 1][j][2 * (u & 1)], hi = c[u >> 1][j][2 * (u & 1) + 1];
+            const u32x4 ka = {f8_pair<false>(lo, power[j]), f8_pair<true>(lo, power[j]), f8_pair<false>(hi, power[j]),
+                              f8_pair<true>(hi, power[j])};
+#pragma unroll
+            for (int q = 0; q < RG; ++q)
+              acc[q][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka),
+                                                                  __builtin_bit_cast(bf16x8, qb[q][u]), acc[q][j], 0, 0, 0);
           }
-        }
       } else
 #pragma unroll
       for (int u = 0; u < C::kChunks; ++u)
@@ -434,19 +445,6 @@ void query_short_kernel(QueryParams p) {
               for (int v = 0; v < 4; ++v)
                 if (!(sees >> (16 * j + v) & 1)) sc[q][j][v] = -INFINITY;
           }
-          if constexpr (F8) {
-            // bytes that belong to no slot of the entry may hold anything
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              uint32_t w[2] = {vx[j].x, vx[j].y};
-#pragma unroll
-              for (int v = 0; v < 4; ++v) {
-                const int key = 16 * j + 4 * kg + v;
-                if (key >= run.hi() || key < run.lo()) w[v >> 1] &= ~(0xFF00u << 16 * (v & 1));
-              }
-              vx[j] = uint2{w[0], w[1]};
-            }
-          }
         }
       } else if constexpr (PAGED) {
         // slots outside the entry, or past the position of one of the wave's rows
@@ -477,6 +475,61 @@ void query_short_kernel(QueryParams p) {
             for (int v = 0; v < 4; ++v)
               if (16 * j + 4 * kg + v >= lim) sc[q][j][v] = -INFINITY;
         }
+      }
+      if constexpr (F8) {
+        const F8Keys key = f8_keys(vx);
+#pragma unroll
+        for (int q = 0; q < RG; ++q) {
+          float x[2][4], mx = kF8None;
+          auto exponents = [&]() __attribute__((always_inline)) {
+            const float base = m[q] - kF8Up;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) {
+                x[j][v] = __builtin_fmaf(sc[q][j][v], cpos, key.byte[4 * j + v] - base);
+                mx = fmaxf(mx, x[j][v]);
+              }
+          };
+          exponents();
+          if (__builtin_amdgcn_ballot_w64(mx > kF8Up + kLazy)) {
+            float mt = kF8None;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) mt = fmaxf(mt, __builtin_fmaf(sc[q][j][v], cpos, key.byte[4 * j + v]));
+            mt = __builtin_ceilf(row4_max(mt));
+            const bool grow = mt > m[q] + kLazy;
+            const float alpha = fast_exp2(grow ? m[q] - mt : 0.f);
+            m[q] = grow ? mt : m[q];
+            l[q] *= alpha;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const float av = __shfl(alpha, 4 * kg + v, 64);
+#pragma unroll
+              for (int b = 0; b < C::kBlocks; ++b) o[q][b][v] *= av;
+            }
+            exponents();
+          }
+          float ps = l[q];
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              sc[q][j][v] = fast_exp2(x[j][v]);
+              ps = __builtin_fmaf(sc[q][j][v], key.back[4 * j + v], ps);
+            }
+          l[q] = fminf(ps, kF8SumMax);
+          asm volatile("" : "+v"(l[q]));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t x[2];
+            f16_parts(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x[0], x[1]);
+            pp[0][q][e] = x[0];
+            pp[1][q][e] = x[1];
+          }
+        }
+        return;
       }
       // The reference max moves only when a tile's max passes it by more than
       // kLazy; the wave leaves it and the accumulators alone unless a row's
@@ -521,17 +574,6 @@ void query_short_kernel(QueryParams p) {
           }
         l[q] += ps;
         asm volatile("" : "+v"(l[q]));  // the sum is formed here, not sunk into a later phase
-        if constexpr (F8) {
-          // V's codes enter the product as they are, their powers of two with
-          // the probabilities: a lane's codes of V are of eight keys.
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const uint32_t w = v < 2 ? vx[j].x : vx[j].y;
-              sc[q][j][v] *= __uint_as_float(((v & 1) ? w >> 1 : w << 15) & 0x7F800000u);
-            }
-        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           uint32_t x[kParts];
@@ -561,8 +603,8 @@ void query_short_kernel(QueryParams p) {
           const int b = b0 + bb;
           if constexpr (F8) {
             const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vq + 64 * (b0 + (bb ^ far))));
-            vf[bb] = u32x4{f8_pair<false>((uint32_t)c[0], 1.f), f8_pair<true>((uint32_t)c[0], 1.f),
-                           f8_pair<false>((uint32_t)c[1], 1.f), f8_pair<true>((uint32_t)c[1], 1.f)};
+            vf[bb] = u32x4{f8_pair_f16<false>((uint32_t)c[0]), f8_pair_f16<true>((uint32_t)c[0]),
+                           f8_pair_f16<false>((uint32_t)c[1]), f8_pair_f16<true>((uint32_t)c[1])};
             continue;
           }
           const uint2 w0 = __builtin_bit_cast(
@@ -579,8 +621,12 @@ void query_short_kernel(QueryParams p) {
             for (int q = 0; q < RG; ++q) {
               const int b = b0 + bb;
               f32x4 c = {o[q][b][0], o[q][b][1], o[q][b][2], o[q][b][3]};
-              c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pp[part][q]),
-                                                          __builtin_bit_cast(bf16x8, vf[bb]), c, 0, 0, 0);
+              if constexpr (F8)
+                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, pp[part][q]),
+                                                           __builtin_bit_cast(f16x8_t, vf[bb]), c, 0, 0, 0);
+              else
+                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pp[part][q]),
+                                                            __builtin_bit_cast(bf16x8, vf[bb]), c, 0, 0, 0);
               o[q][b][0] = c[0];
               o[q][b][1] = c[1];
               o[q][b][2] = c[2];
@@ -635,6 +681,7 @@ void query_short_kernel(QueryParams p) {
     // no direct load may still be writing LDS when the next piece begins or
     // the workgroup ends
     __builtin_amdgcn_s_waitcnt(0x0F70);
+    if constexpr (kOver) __syncthreads();  // nor a wave be reading tiles
 
     // ---- fold the key waves and write the output or this piece's record --------
     // Key wave k finishes output blocks k OB .. k OB + OB - 1: the others hand
@@ -661,19 +708,21 @@ void query_short_kernel(QueryParams p) {
       }
     }
 #pragma unroll
-    for (int z = 0; z < RG * OB / HB; ++z) {
-      const int q = z / (OB / HB), h0 = z % (OB / HB) * HB;  // row group, first of the HB blocks
+    for (int z = 0; z < RG * OB / HB * (FW / FK); ++z) {
+      const int y = z / (FW / FK), f0 = z % (FW / FK) * FK;  // first of the waves that finish now
+      const int q = y / (OB / HB), h0 = y % (OB / HB) * HB;  // row group, first of the HB blocks
       if (z > 0) __syncthreads();
 #pragma unroll
-      for (int k = 0; k < KW; ++k)
+      for (int k = f0; k < f0 + FK; ++k)
         if (kw != k) {
 #pragma unroll
           for (int b = 0; b < HB; ++b) {
             const int x = k * OB + h0 + b;
-            fo[k][rw][kw < k ? kw : kw - 1][b][lane] = f32x4{o[q][x][0], o[q][x][1], o[q][x][2], o[q][x][3]};
+            fo[k - f0][rw][kw < k ? kw : kw - 1][b][lane] = f32x4{o[q][x][0], o[q][x][1], o[q][x][2], o[q][x][3]};
           }
         }
       __syncthreads();
+      if (FK < KW && (kw < f0 || kw >= f0 + FK)) continue;
       f32x4 M = *reinterpret_cast<const f32x4*>(&fm[0][rw][q][4 * kg]);
 #pragma unroll
       for (int k = 1; k < KW; ++k) {
@@ -697,7 +746,7 @@ void query_short_kernel(QueryParams p) {
           const int x2 = k * OB + h0 + b;
           f32x4 c;
           if (kw == k) c = f32x4{o[q][x2][0], o[q][x2][1], o[q][x2][2], o[q][x2][3]};
-          else c = fo[kw][rw][k < kw ? k : k - 1][b][lane];
+          else c = fo[kw - f0][rw][k < kw ? k : k - 1][b][lane];
           A[b] += f * c;
         }
       }
@@ -814,13 +863,13 @@ __global__ __launch_bounds__(kSMergeThreads) void query_short_merge_kernel(Query
   }
 }
 
-template <int D, int RW, int KW, bool PAGED, bool F8, bool TREE>
+template <int D, int RW, int KW, bool PAGED, bool F8, bool TREE, int RG = kSRG>
 hipError_t launch_short_r(const QueryParams& p, hipStream_t stream) {
   const size_t lds = p.P > 0 ? ((PAGED ? 1 : 2) * (size_t)p.nseg + 1) * sizeof(int64_t) : 0;
   const dim3 grid((unsigned)(p.P > 0 ? p.P : p.nseg)), block(RW * KW * kWave);
   if (p.stream_once)
-    hipLaunchKernelGGL((query_short_kernel<D, RW, KW, true, PAGED, F8, TREE>), grid, block, lds, stream, p);
-  else hipLaunchKernelGGL((query_short_kernel<D, RW, KW, false, PAGED, F8, TREE>), grid, block, lds, stream, p);
+    hipLaunchKernelGGL((query_short_kernel<D, RW, KW, true, PAGED, F8, TREE, RG>), grid, block, lds, stream, p);
+  else hipLaunchKernelGGL((query_short_kernel<D, RW, KW, false, PAGED, F8, TREE, RG>), grid, block, lds, stream, p);
   if (p.P > 1)
     hipLaunchKernelGGL((query_short_merge_kernel<D, PAGED>), dim3((unsigned)(p.nseg * p.rows)), dim3(kSMergeThreads), 0,
                        stream, p);
@@ -829,8 +878,16 @@ hipError_t launch_short_r(const QueryParams& p, hipStream_t stream) {
 
 template <int D, bool PAGED, bool F8 = false, bool TREE = false>
 hipError_t launch_short_d(const QueryParams& p, hipStream_t stream) {
-  if (p.rows <= 32) return launch_short_r<D, 1, 4, PAGED, F8, TREE>(p, stream);
-  if (p.rows <= 64) return launch_short_r<D, 2, 2, PAGED, F8, TREE>(p, stream);
+  if constexpr (F8) {
+    // two waves a SIMD throughout: with twice the keys per byte the arithmetic
+    // counts, and a wave's waits for its own
+    if (p.rows <= 16) return launch_short_r<D, 1, 8, PAGED, F8, TREE, 1>(p, stream);
+    if (p.rows <= 32) return launch_short_r<D, 1, 8, PAGED, F8, TREE>(p, stream);
+    if (p.rows <= 64) return launch_short_r<D, 2, 4, PAGED, F8, TREE>(p, stream);
+  } else {
+    if (p.rows <= 32) return launch_short_r<D, 1, 4, PAGED, F8, TREE>(p, stream);
+    if (p.rows <= 64) return launch_short_r<D, 2, 2, PAGED, F8, TREE>(p, stream);
+  }
   if (p.rows <= 128) return launch_short_r<D, 4, 2, PAGED, F8, TREE>(p, stream);
   return launch_short_r<D, 8, 1, PAGED, F8, TREE>(p, stream);
 }
