@@ -85,18 +85,6 @@ __device__ __forceinline__ F8Keys f8_keys(const uint2 (&w)[2]) {
   return k;
 }
 
-// The same from words of V's bytes alone.
-__device__ __forceinline__ F8Keys f8_keys_v(const uint32_t (&w)[2]) {
-  F8Keys k;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t b = (w[j >> 2] >> (8 * (j & 3))) & 0xFFu;
-    k.byte[j] = (float)b;
-    k.back[j] = __builtin_amdgcn_ldexpf(1.f, 127 - (int)b);
-  }
-  return k;
-}
-
 // Two weights as two fp16 pairs.
 __device__ __forceinline__ void f16_parts(float x0, float x1, uint32_t& a, uint32_t& b) {
   const auto h = __builtin_amdgcn_cvt_pkrtz(x0, x1);

@@ -169,19 +169,38 @@ __device__ __forceinline__ u32x4 tile_run_word(const PagedRun& u, int row_bytes)
                (uint32_t)((u.hi() - u.lo()) * row_bytes)};
 }
 
-// Quantised pools: where a tile's codes and exponent bytes wait for their
-// conversion, each wave's eight rows apart (nothing meets there).
-struct RawTiles {
-  uint8_t *k, *v, *exps;
-  uint8_t* v_exps[2];  // V's exponent bytes of two tiles, for the vector phases
-};
+// The runs with slots moved to the table's front, in order; returns their
+// number (256 tokens over the 35% of 131,072 positions that a selection kept,
+// in 128-row pages 333 -> 323 us, in 256-row pages 369 -> 324, in 1,024-row pages
+// 613 -> 372; 512 tokens over whole pages, without gaps, 417 -> 420).  A word moves
+// to its own index or a lower one, after the words up to it have been read.
+__device__ __forceinline__ int drop_gaps(u32x4* table, int* counts, int n) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int at = 0;
+  for (int i0 = 0, turn = 0; i0 < n; i0 += kQThreads, turn ^= 1) {
+    const int i = i0 + tid;
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (i < n) w = table[i];
+    const uint64_t some = __builtin_amdgcn_ballot_w64(w[3] != 0u);
+    if (lane == 0) counts[8 * turn + wave] = __popcll(some);
+    __syncthreads();
+    int to = at;
+    for (int k = 0; k < kQThreads / kWave; ++k) {
+      const int c = counts[8 * turn + k];
+      to += k < wave ? c : 0;
+      at += c;
+    }
+    if (w[3] != 0u) table[to + __popcll(some & ((1ull << lane) - 1))] = w;
+  }
+  __syncthreads();
+  if (tid < kTablePad) table[at + tid] = u32x4{0u, 0u, 0u, 0u};
+  return __builtin_amdgcn_readfirstlane(at);
+}
 
-template <int D, bool PAGED, bool F8 = false, bool TREE = false>
+template <int D, bool PAGED, bool TREE = false>
 __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem& item, uint16_t* k0, uint16_t* k1,
-                                           uint16_t* v0, uint16_t* v1, u32x4* table, int* counts,
-                                           const RawTiles raw = RawTiles{}) {
+                                           uint16_t* v0, uint16_t* v1, u32x4* table, int* counts) {
   using C = QCfg<D>;
-  constexpr int kPoolRow = F8 ? D : C::kRowBytes;  // bytes of a pool's row
   // bf16 parts of a probability.  Packed: two, 17 bits.  Paged: three, its 24
   // bits, at any length: two err by 2.1e-6 to 2.5e-6 of the output's norm at
   // 1,000 keys as at 131,072, three by 2.0e-7 to 5.2e-7, attention in plain fp32
@@ -191,8 +210,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // costs what it computes, as the kernel runs at the rate that the matrix units
   // reach under the power limit (two / three parts, us, 8B layer: 512 tokens at 32K
   // 349 / 423, 256 over 45K rows 277 / 330).
-  // Quantised: two of fp16 (dkv_f8.hpp).
-  constexpr int kParts = PAGED && !F8 ? 3 : 2;
+  constexpr int kParts = PAGED ? 3 : 2;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = tid >> 6;
@@ -298,7 +316,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   for (int q = 0; q < kRG; ++q) {
 #pragma unroll
     for (int b = 0; b < C::kBlocks; ++b) o[q][b][0] = o[q][b][1] = o[q][b][2] = o[q][b][3] = 0.f;
-    m[q] = F8 ? kF8None : -INFINITY;
+    m[q] = -INFINITY;
     l[q] = 0.f;
   }
 
@@ -357,36 +375,10 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
       u32x4 w = {0u, 0u, 0u, 0u};
       if (i < n) {
         const int32_t r = (int32_t)from + i * kRun;
-        w = tile_run_word(paged_run(seg, entries[r >> seg.shift], r), kPoolRow);
+        w = tile_run_word(paged_run(seg, entries[r >> seg.shift], r), C::kRowBytes);
       }
       table[i] = w;
     }
-  };
-  // The runs with slots moved to the table's front, in order; returns their
-  // number (256 tokens over the 35% of 131,072 positions that a selection kept,
-  // in 128-row pages 333 -> 323 us, in 256-row pages 369 -> 324, in 1,024-row pages
-  // 613 -> 372; 512 tokens over whole pages, without gaps, 417 -> 420).  A word moves
-  // to its own index or a lower one, after the words up to it have been read.
-  auto drop_gaps = [&](int n) __attribute__((always_inline)) {
-    int at = 0;
-    for (int i0 = 0, turn = 0; i0 < n; i0 += kQThreads, turn ^= 1) {
-      const int i = i0 + tid;
-      u32x4 w = {0u, 0u, 0u, 0u};
-      if (i < n) w = table[i];
-      const uint64_t some = __builtin_amdgcn_ballot_w64(w[3] != 0u);
-      if (lane == 0) counts[8 * turn + wave] = __popcll(some);
-      __syncthreads();
-      int to = at;
-      for (int k = 0; k < kQThreads / kWave; ++k) {
-        const int c = counts[8 * turn + k];
-        to += k < wave ? c : 0;
-        at += c;
-      }
-      if (w[3] != 0u) table[to + __popcll(some & ((1ull << lane) - 1))] = w;
-    }
-    __syncthreads();
-    if (tid < kTablePad) table[at + tid] = u32x4{0u, 0u, 0u, 0u};
-    return __builtin_amdgcn_readfirstlane(at);
   };
   auto read_runs = [&](int at) __attribute__((always_inline)) {
     coming[0] = table[at];
@@ -411,51 +403,6 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
           q_rsrc(static_cast<const char*>(pool) + ((uint64_t)(x.off_hi & 0xFFFF) << 32 | x.off), x.bytes);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(buf + 512 * mi), 16,
                                                off - x.lo() * C::kRowBytes, 0, 0, 0);
-    }
-  };
-  // Quantised: wave w brings rows 8w .. 8w + 7 of a tile (lane l: row l % 8, 16
-  // bytes l / 8 of it; with 64 dims the first 32 lanes), and with K's their
-  // exponent bytes, to LDS of its own, and reads them back (row l % 8, D / 8
-  // codes l / 8) when they have arrived: K's values, exact in bf16, and V's codes,
-  // exact in fp16, go to the tile buffers, V's bytes to where the vector phases
-  // find them.  Every row is converted once for all waves.
-  const int crow = lane & 7, ccol = lane >> 3;
-  auto raw_runs = [&](const void* pool, const TileRun (&u)[2], uint8_t* codes, bool is_k) __attribute__((always_inline)) {
-    const TileRun& x = wave_u >= 4 ? u[1] : u[0];
-    const uint64_t at = (uint64_t)(x.off_hi & 0xFFFF) << 32 | x.off;  // of the run's first slot that counts
-    const __amdgpu_buffer_rsrc_t rs = q_rsrc(static_cast<const char*>(pool) + at, x.bytes);
-    const uint32_t row = (uint32_t)(8 * (wave_u & 3));
-    if (D == 128 || lane < 32)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(codes + 8 * D * wave_u), 16,
-                                               (row + crow - x.lo()) * D + 16 * ccol, 0, 0, 0);
-    if (is_k && lane == 0)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          q_rsrc(reinterpret_cast<const char*>(p.scales) + 2 * (at / D - x.lo()), x.bytes > 0 ? 2 * kRun : 0),
-          (__attribute__((address_space(3))) void*)(raw.exps + 16 * wave_u), 16, 2 * row, 0, 0, 0);
-  };
-  const int raw_at = 8 * D * wave + (D == 128 ? 16 * lane : 16 * (crow + 8 * (ccol >> 1)) + 8 * (ccol & 1));
-  const int conv_row = 8 * wave + crow;
-  auto convert_k = [&](uint16_t* buf, uint8_t* v_exps) __attribute__((always_inline)) {
-    const uint32_t e = *reinterpret_cast<const uint16_t*>(raw.exps + 16 * wave_u + 2 * crow);
-    // a byte that belongs to no slot of the entry may be that of an infinity
-    const float power = f8_power((e & 0xFF) < 254u ? e & 0xFF : 254u);
-    if (ccol == 0) v_exps[conv_row] = (uint8_t)(e >> 8);
-#pragma unroll
-    for (int h = 0; h < D / 64; ++h) {
-      const uint2 c = *reinterpret_cast<const uint2*>(raw.k + raw_at + 8 * h);
-      const int chunk = ((conv_row / 16) * C::kRowChunks + D / 64 * ccol + h) * 16 + conv_row % 16;
-      *reinterpret_cast<u32x4*>(buf + 8 * chunk) = u32x4{f8_pair<false>(c.x, power), f8_pair<true>(c.x, power),
-                                                         f8_pair<false>(c.y, power), f8_pair<true>(c.y, power)};
-    }
-  };
-  auto convert_v = [&](uint16_t* buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int h = 0; h < D / 64; ++h) {
-      const uint2 c = *reinterpret_cast<const uint2*>(raw.v + raw_at + 8 * h);
-      const int col = D / 64 * ccol + h;
-      const int chunk = ((conv_row / 8) * (C::kRowChunks / 2) + col / 2) * 16 + (conv_row % 8) * 2 + col % 2;
-      *reinterpret_cast<u32x4*>(buf + 8 * chunk) = u32x4{f8_pair_f16<false>(c.x), f8_pair_f16<true>(c.x),
-                                                         f8_pair_f16<false>(c.y), f8_pair_f16<true>(c.y)};
     }
   };
   auto issue = [&](const char* base, uint32_t off, int64_t kt, uint16_t* buf) __attribute__((always_inline)) {
@@ -513,13 +460,7 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   // power limit).
   int32_t pos_all = PAGED ? paged_pos(blk, min(qt * kQRows + wave_rows * wave_u, rows - 1) / p.G) + 1 : 0;
   if (TREE && p.mask != nullptr) pos_all = blk.pos0;  // new tokens are seen by their bits
-  auto softmax = [&](auto masked, auto rgs, float (&sc)[kRG][2][4], int64_t kh, const TileRun& u,
-                     const uint8_t* exps) __attribute__((always_inline)) {
-    uint32_t ve[2] = {0u, 0u};  // quantised: V's exponent bytes of the lane's keys
-    if constexpr (F8) {
-      ve[0] = *reinterpret_cast<const uint32_t*>(exps + 4 * kg);
-      ve[1] = *reinterpret_cast<const uint32_t*>(exps + 16 + 4 * kg);
-    }
+  auto softmax = [&](auto masked, auto rgs, float (&sc)[kRG][2][4], int64_t kh, const TileRun& u) __attribute__((always_inline)) {
     if constexpr (TREE) {
       // slots outside the entry, or that one of the wave's rows does not see
       if (!u.whole() || (int32_t)u.pos + kRun > pos_all) {
@@ -551,54 +492,6 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
             }
         }
       }
-    }
-    if constexpr (F8) {
-      const F8Keys key = f8_keys_v(ve);
-#pragma unroll
-      for (int q = 0; q < decltype(rgs)::value; ++q) {
-        float x[2][4], mx = kF8None;
-        auto exponents = [&]() __attribute__((always_inline)) {
-          const float base = m[q] - kF8Up;
-#pragma unroll
-          for (int jj = 0; jj < 2; ++jj)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              x[jj][v] = __builtin_fmaf(sc[q][jj][v], cpos, key.byte[4 * jj + v] - base);
-              mx = fmaxf(mx, x[jj][v]);
-            }
-        };
-        exponents();
-        if (__builtin_amdgcn_ballot_w64(mx > kF8Up + kLazy)) {
-          float mt = kF8None;
-#pragma unroll
-          for (int jj = 0; jj < 2; ++jj)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) mt = fmaxf(mt, __builtin_fmaf(sc[q][jj][v], cpos, key.byte[4 * jj + v]));
-          mt = __builtin_ceilf(row4_max(mt));
-          const bool grow = mt > m[q] + kLazy;
-          const float alpha = fast_exp2(grow ? m[q] - mt : 0.f);
-          m[q] = grow ? mt : m[q];
-          l[q] *= alpha;
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float av = __shfl(alpha, 4 * kg + v, 64);
-#pragma unroll
-            for (int b = 0; b < C::kBlocks; ++b) o[q][b][v] *= av;
-          }
-          exponents();
-        }
-        float ps = l[q];
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            sc[q][jj][v] = fast_exp2(x[jj][v]);
-            ps = __builtin_fmaf(sc[q][jj][v], key.back[4 * jj + v], ps);
-          }
-        l[q] = fminf(ps, kF8SumMax);
-        asm volatile("" : "+v"(l[q]));
-      }
-      return;
     }
 #pragma unroll
     for (int q = 0; q < decltype(rgs)::value; ++q) {
@@ -657,20 +550,13 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         uint32_t x[kParts];
-        if constexpr (F8) f16_parts(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x[0], x[1]);
-        else if constexpr (PAGED) bf16_parts(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x);
+        if constexpr (PAGED) bf16_parts(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x);
         else bf16_split(sc[q][e >> 1][2 * (e & 1)], sc[q][e >> 1][2 * (e & 1) + 1], x[0], x[1]);
 #pragma unroll
         for (int part = 0; part < kParts; ++part) pp[part][q][e] = x[part];
       }
   };
 
-  auto pv_product = [](const u32x4& w, const u32x4& v, const f32x4& c) __attribute__((always_inline)) {
-    if constexpr (F8)
-      return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, w), __builtin_bit_cast(f16x8_t, v), c, 0, 0, 0);
-    else
-      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, v), c, 0, 0, 0);
-  };
   // O += P V over half h of the tile whose V is in vb; each V fragment
   // serves both row groups.  Transpose-read addresses: lane 4r + q of group
   // kg reads row R = 32h + 4kg + r (and R + 16), columns 16b + 4q .. +3, i.e.
@@ -702,7 +588,8 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
           for (int q = 0; q < decltype(rgs)::value; ++q) {
             const int b = b0 + bb;
             f32x4 c = {o[q][b][0], o[q][b][1], o[q][b][2], o[q][b][3]};
-            c = pv_product(pp[part][q], vbo[bb], c);
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pp[part][q]),
+                                                        __builtin_bit_cast(bf16x8, vbo[bb]), c, 0, 0, 0);
             o[q][b][0] = c[0];
             o[q][b][1] = c[1];
             o[q][b][2] = c[2];
@@ -746,7 +633,8 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
             for (int q = 0; q < decltype(rgs)::value; ++q) {
               const int b = 2 * n + bb;
               f32x4 c = {o[q][b][0], o[q][b][1], o[q][b][2], o[q][b][3]};
-              c = pv_product(pp[part][q], vf[n % 2][bb], c);
+              c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pp[part][q]),
+                                                          __builtin_bit_cast(bf16x8, vf[n % 2][bb]), c, 0, 0, 0);
               o[q][b][0] = c[0];
               o[q][b][1] = c[1];
               o[q][b][2] = c[2];
@@ -816,27 +704,9 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
   const bool lead = __builtin_amdgcn_readfirstlane(wave < 4 ? 1 : 0) != 0;
   float sc[kRG][2][4];
   u32x4 pp[kParts][kRG];
-  // vmcnt: the younger of two tiles may still be in flight (quantised: K's codes
-  // and exponents, V's codes)
-  constexpr int kWaitOne = 0x0F70 | (F8 ? 2 : C::kDma), kWaitK = 0x0F70 | (F8 ? 1 : C::kDma);
-  // quantised: the wave's rows of V of tile t, or K of the tile after it, have
-  // arrived; they go to the tile buffers, and those of the next tile set out
-  auto next_v = [&](uint16_t* buf, const TileRun (&u)[2]) __attribute__((always_inline)) {
-    __builtin_amdgcn_sched_barrier(0);
-    convert_v(buf);
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): read before they are overwritten, written before the meeting
-    __builtin_amdgcn_sched_barrier(0);
-    raw_runs(p.v, u, raw.v, false);
-  };
-  auto next_k = [&](uint16_t* buf, uint8_t* v_exps, const TileRun (&u)[2]) __attribute__((always_inline)) {
-    __builtin_amdgcn_sched_barrier(0);
-    convert_k(buf, v_exps);
-    __builtin_amdgcn_s_waitcnt(0xC07F);
-    __builtin_amdgcn_sched_barrier(0);
-    raw_runs(p.k, u, raw.k, true);
-  };
-  auto vphase = [&](auto masked, auto rgs, int64_t kh, const TileRun& u, const uint8_t* exps) __attribute__((always_inline)) {
-    softmax(masked, rgs, sc, kh, u, exps);
+  constexpr int kWaitOne = 0x0F70 | C::kDma;  // vmcnt(kDma): the younger of two tiles may still be in flight
+  auto vphase = [&](auto masked, auto rgs, int64_t kh, const TileRun& u) __attribute__((always_inline)) {
+    softmax(masked, rgs, sc, kh, u);
     split(rgs, sc, pp);
     if constexpr (PAGED) {
       // the parts are formed here, not sunk into the product phase
@@ -864,23 +734,16 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     fill_table(k_lo);
     __syncthreads();
     if (item.gaps && k_hi - k_lo <= kTableRuns * kRun) {
-      live = drop_gaps((int)((k_hi - k_lo + kRun - 1) / kRun));
+      live = drop_gaps(table, counts, (int)((k_hi - k_lo + kRun - 1) / kRun));
       __syncthreads();
     }
     read_runs(0);
     take_runs(run[0]);
     read_runs(2);
     take_runs(run[1]);
-    if constexpr (F8) {
-      raw_runs(p.k, run[0], raw.k, true);
-      raw_runs(p.v, run[0], raw.v, false);
-      __builtin_amdgcn_s_waitcnt(kWaitK);
-      next_k(kbuf[0], raw.v_exps[0], run[1]);
-    } else {
-      issue_runs(p.k, koff, run[0], kbuf[0]);
-      issue_runs(p.v, voff, run[0], vbuf[0]);
-      issue_runs(p.k, koff, run[1], kbuf[1]);
-    }
+    issue_runs(p.k, koff, run[0], kbuf[0]);
+    issue_runs(p.v, voff, run[0], vbuf[0]);
+    issue_runs(p.k, koff, run[1], kbuf[1]);
   } else {
     issue(kbase, koff, k_lo, kbuf[0]);
     issue(vbase, voff, k_lo, vbuf[0]);
@@ -910,39 +773,36 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     constexpr int i = decltype(par)::value;  // tile t's parity
     // 4t + 1: lead: vector phase of half 2t; follow: P V of half 2t - 1, scores of 2t
     if (PAGED && L) read_runs(at);
-    if (L) vphase(masked, rgs, kt, run[i][0], raw.v_exps[i]);
+    if (L) vphase(masked, rgs, kt, run[i][0]);
     else mphase(rgs, kbuf[i], 0, vbuf[1 - i], 1, i == 1 || kt != k_lo);
     if (PAGED && L) take_runs(ahead);
     __builtin_amdgcn_s_waitcnt(kWaitOne);  // V of tile t
-    if constexpr (F8) next_v(vbuf[i], run[1 - i]);
     meet();
     // 4t + 2: lead: P V of 2t, scores of 2t + 1; follow: vector phase of 2t
-    if constexpr (F8) ;
-    else if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
+    if constexpr (PAGED) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
     else issue(vbase, voff, kt + kQKeys, vbuf[1 - i]);
     if (PAGED && !L) read_runs(at);
     if (L) mphase(rgs, kbuf[i], 1, vbuf[i], 0, true);
-    else vphase(masked, rgs, kt, run[i][0], raw.v_exps[i]);
+    else vphase(masked, rgs, kt, run[i][0]);
     if (PAGED && !L) take_runs(ahead);
     meet();
     // 4t + 3: lead: vector phase of 2t + 1; follow: P V of 2t, scores of 2t + 1
     const TileRun second = run[i][1];
-    if (L) vphase(masked, rgs, kt + 32, second, raw.v_exps[i] + 32);
+    if (L) vphase(masked, rgs, kt + 32, second);
     else mphase(rgs, kbuf[i], 1, vbuf[i], 0, true);
-    __builtin_amdgcn_s_waitcnt(kWaitK);  // K of tile t + 1
-    if constexpr (F8) next_k(kbuf[1 - i], raw.v_exps[1 - i], ahead);
+    __builtin_amdgcn_s_waitcnt(kWaitOne);  // K of tile t + 1
     meet();
     // 4t + 4: lead: P V of 2t + 1, scores of 2t + 2; follow: vector phase of 2t + 1
     if constexpr (PAGED) {
       run[i][0] = ahead[0];
       run[i][1] = ahead[1];
-      if constexpr (!F8) issue_runs(p.k, koff, run[i], kbuf[i]);
+      issue_runs(p.k, koff, run[i], kbuf[i]);
       at += 2;
     } else {
       issue(kbase, koff, kt + 2 * kQKeys, kbuf[i]);
     }
     if (L) mphase(rgs, kbuf[1 - i], 0, vbuf[i], 1, true);
-    else vphase(masked, rgs, kt + 32, second, raw.v_exps[i] + 32);
+    else vphase(masked, rgs, kt + 32, second);
     meet();
     kt += kQKeys;
   };
@@ -984,17 +844,15 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     auto none = [&](auto par) __attribute__((always_inline)) {
       constexpr int i = decltype(par)::value;
       __builtin_amdgcn_s_waitcnt(kWaitOne);
-      if constexpr (F8) next_v(vbuf[i], run[1 - i]);
       meet();
-      if constexpr (!F8) issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
+      issue_runs(p.v, voff, run[1 - i], vbuf[1 - i]);
       read_runs(at);
       take_runs(run[i]);
       at += 2;
       meet();
-      __builtin_amdgcn_s_waitcnt(kWaitK);
-      if constexpr (F8) next_k(kbuf[1 - i], raw.v_exps[1 - i], run[i]);
+      __builtin_amdgcn_s_waitcnt(kWaitOne);
       meet();
-      if constexpr (!F8) issue_runs(p.k, koff, run[i], kbuf[i]);
+      issue_runs(p.k, koff, run[i], kbuf[i]);
       meet();
       kt += kQKeys;
     };
@@ -1044,6 +902,8 @@ __device__ __forceinline__ void query_item(const QueryParams& p, const QueryItem
     }
   }
 }
+
+#include "query_f8.hpp"
 
 // Two tile buffers per matrix (separate arrays: the compiler then tells the
 // direct loads into one apart from the reads of the other).
@@ -1246,7 +1106,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
       bool gaps;
       const int32_t rows = unit_rows(p, blk[lo], s, qt, &gaps);
       const int64_t left = (int64_t)blk[lo].n * p.G - (int64_t)qt * kQRows;
-      const int32_t cost = left <= 64 ? kThinCost : (left <= kQRows / 2 ? kHalfCost : kTileCost);
+      int32_t cost = left <= 64 ? kThinCost : (left <= kQRows / 2 ? kHalfCost : kTileCost);
+      if (p.scales != nullptr && left <= kQRows / 2) cost = kThinCost;  // two waves a key half each
       plan.unit[u] = PagedUnit{s, qt, rows, cost, blk[lo], gaps};
       mine = (unit_tiles(rows) + kUnitTiles) * cost;  // below 2^27
       most = max(most, (int32_t)mine);
@@ -1376,9 +1237,11 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(QueryParams p)
 template <int D, bool F8 = false, bool TREE = false>
 __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
   DKV_QUERY_TILES(D);
-  constexpr int kRaw = F8 ? kQKeys * D : 16, kExps = F8 ? kQKeys : 8;
-  __shared__ __align__(1024) uint8_t rk[kRaw], rv[kRaw];
-  __shared__ __align__(16) uint8_t rx[2 * kExps], vx[2][kExps];
+  // quantised: codes and exponent bytes on their way, and V's exponents of two tiles as numbers
+  constexpr int kCodes = F8 ? kQKeys * D : 16, kNumbers = F8 ? 2 * kQKeys : 4;
+  __shared__ __align__(1024) uint8_t codes_k[kCodes], codes_v[kCodes];
+  __shared__ __align__(16) uint8_t exps[F8 ? 2 * kQKeys : 16];
+  __shared__ __align__(16) float keys0[kNumbers], keys1[kNumbers];
   __shared__ __align__(16) u32x4 table[kTableRuns + kTablePad];
   __shared__ int counts[2 * kQThreads / kWave];  // runs with slots, per wave
   __shared__ PagedUnit own[kWholeRounds];  // whole units: this workgroup's
@@ -1457,9 +1320,8 @@ __global__ __launch_bounds__(kQThreads) void paged_query_kernel(QueryParams p) {
       x.single = true;
       x.rec = nullptr;
     }
-    if constexpr (F8 || TREE)
-      query_item<D, true, F8, TREE>(p, x, k0, k1, v0, v1, table, counts, RawTiles{rk, rv, rx, {vx[0], vx[1]}});
-    else query_item<D, true>(p, x, k0, k1, v0, v1, table, counts);
+    if constexpr (F8) f8_item<D>(p, x, k0, k1, v0, v1, codes_k, codes_v, exps, keys0, keys1, table, counts);
+    else query_item<D, true, TREE>(p, x, k0, k1, v0, v1, table, counts);
     __syncthreads();  // the tile buffers are free for the next unit
   }
 }

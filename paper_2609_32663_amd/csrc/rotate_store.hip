@@ -127,7 +127,7 @@ enum StoreMode { kRopeOnly, kStoreBf16, kStoreF8 };
 // LPR: lanes per row, 0 for any (dim / 8, at most 32).  FAR: an element's partner
 // is read from memory (half layout, pairs that do not line up with lanes).
 template <typename T, int MODE, int LPR, bool FAR>
-__global__ __launch_bounds__(kRotThreads) void rotate_store_kernel(RotateParams p) {
+__global__ __launch_bounds__(kRotThreads, 4) void rotate_store_kernel(RotateParams p) {
   __shared__ double2 trig[kRotWaves][kMaxPairs];
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
@@ -305,12 +305,17 @@ hipError_t launch_rotate(RotateParams p, hipStream_t stream) {
 }
 
 // ---------------------------------------------------------------- read back
-// 16 bytes of a K and of a V row per thread, rows of one token side by side.
-// Bound by moving the rows.
-template <bool F8>
+// Eight elements of a K and of a V row per thread, so that a wave writes whole
+// lines, rows of one token side by side.  Bound by moving the rows; results that
+// the 256 MB last-level cache cannot hold for whoever reads them next are written
+// past it (a context of 131,072 tokens, 8 heads, 816 MB moved: 146 us, 160 through it,
+// 5.6 and 5.1 TB/s; 16 codes a thread, whose stores then leave lines in halves, 160
+// and 239).
+constexpr int64_t kLoadCachedBytes = 256 << 20;
+
+template <bool F8, bool NT>
 __global__ __launch_bounds__(kRotThreads) void paged_load_kernel(LoadParams p) {
-  constexpr int kElems = F8 ? 16 : 8;
-  const int per_row = p.dim / kElems;  // a power of two
+  const int per_row = p.dim / 8;  // a power of two
   const int shift = 31 - __builtin_clz(per_row);
   const int64_t i = (int64_t)blockIdx.x * kRotThreads + threadIdx.x;
   const int64_t r = i >> shift;  // token * Hkv + head
@@ -319,25 +324,29 @@ __global__ __launch_bounds__(kRotThreads) void paged_load_kernel(LoadParams p) {
   if (slot < 0 || slot >= p.pool_rows) return;
   const int c = (int)(i & (per_row - 1));
   const uint32_t t = (uint32_t)r / (uint32_t)p.Hkv;
-  const int64_t to = t * p.stride + ((r - (int64_t)t * p.Hkv) * p.dim + c * kElems) * 2;
-  const int64_t from = slot * p.dim * (F8 ? 1 : 2) + c * 16;
-  const u32x4 k = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.k_pages) + from);
-  const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.v_pages) + from);
-  u32x4* ko = reinterpret_cast<u32x4*>(static_cast<char*>(p.k_out) + to);
-  u32x4* vo = reinterpret_cast<u32x4*>(static_cast<char*>(p.v_out) + to);
+  const int64_t to = t * p.stride + ((r - (int64_t)t * p.Hkv) * p.dim + c * 8) * 2;
+  const int64_t from = (slot * p.dim + c * 8) * (F8 ? 1 : 2);
+  const char* const kp = static_cast<const char*>(p.k_pages) + from;
+  const char* const vp = static_cast<const char*>(p.v_pages) + from;
+  u32x4 k, v;
   if constexpr (F8) {
+    const uint2 kc = *reinterpret_cast<const uint2*>(kp), vc = *reinterpret_cast<const uint2*>(vp);
     const uint32_t ex = *reinterpret_cast<const uint16_t*>(p.scales + 2 * slot);
-    const float kp = f8_power(ex & 0xFF), vp = f8_power(ex >> 8);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      ko[j] = u32x4{f8_pair<false>(k[2 * j], kp), f8_pair<true>(k[2 * j], kp), f8_pair<false>(k[2 * j + 1], kp),
-                    f8_pair<true>(k[2 * j + 1], kp)};
-      vo[j] = u32x4{f8_pair<false>(v[2 * j], vp), f8_pair<true>(v[2 * j], vp), f8_pair<false>(v[2 * j + 1], vp),
-                    f8_pair<true>(v[2 * j + 1], vp)};
-    }
+    const float ke = f8_power(ex & 0xFF), ve = f8_power(ex >> 8);
+    k = u32x4{f8_pair<false>(kc.x, ke), f8_pair<true>(kc.x, ke), f8_pair<false>(kc.y, ke), f8_pair<true>(kc.y, ke)};
+    v = u32x4{f8_pair<false>(vc.x, ve), f8_pair<true>(vc.x, ve), f8_pair<false>(vc.y, ve), f8_pair<true>(vc.y, ve)};
   } else {
-    ko[0] = k;
-    vo[0] = v;
+    k = *reinterpret_cast<const u32x4*>(kp);
+    v = *reinterpret_cast<const u32x4*>(vp);
+  }
+  u32x4* const ko = reinterpret_cast<u32x4*>(static_cast<char*>(p.k_out) + to);
+  u32x4* const vo = reinterpret_cast<u32x4*>(static_cast<char*>(p.v_out) + to);
+  if constexpr (NT) {
+    __builtin_nontemporal_store(k, ko);
+    __builtin_nontemporal_store(v, vo);
+  } else {
+    *ko = k;
+    *vo = v;
   }
 }
 
@@ -352,10 +361,13 @@ hipError_t launch_paged_store(const RotateParams& p, bool f8, hipStream_t stream
 }
 
 hipError_t launch_paged_load(const LoadParams& p, bool f8, hipStream_t stream) {
-  const int64_t n = (int64_t)p.tokens * p.Hkv * (p.dim / (f8 ? 16 : 8));
+  const int64_t n = (int64_t)p.tokens * p.Hkv * (p.dim / 8);
   const dim3 grid((unsigned)((n + kRotThreads - 1) / kRotThreads)), block(kRotThreads);
-  if (f8) hipLaunchKernelGGL(paged_load_kernel<true>, grid, block, 0, stream, p);
-  else hipLaunchKernelGGL(paged_load_kernel<false>, grid, block, 0, stream, p);
+  const bool once = n * 32 > kLoadCachedBytes;
+  if (f8 && once) hipLaunchKernelGGL((paged_load_kernel<true, true>), grid, block, 0, stream, p);
+  else if (f8) hipLaunchKernelGGL((paged_load_kernel<true, false>), grid, block, 0, stream, p);
+  else if (once) hipLaunchKernelGGL((paged_load_kernel<false, true>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((paged_load_kernel<false, false>), grid, block, 0, stream, p);
   return hipGetLastError();
 }
 

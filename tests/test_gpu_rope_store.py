@@ -336,3 +336,33 @@ def test_other_streams_and_empty_calls(d):
     d.dkv_paged_store(none, none, torch.zeros(0, 2, dtype=torch.int64, device=DEV), pool, pool.clone())
     d.dkv_paged_load(torch.zeros(0, 2, dtype=torch.int64, device=DEV), pool, pool, none, none)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["f8", "bf16"])
+def test_load_of_a_long_context(d, fmt):
+    """More than 256 MB of results, which are written past the caches; the last tokens' rows have no slots."""
+    rng = np.random.default_rng(8)
+    Hkv, dim, R, tokens = 8, 128, 256, 70001
+    pages = tokens * Hkv // R + 2
+    P = Pools(fmt, pages, R, dim)
+    bits = torch.randint(0, 120, (pages, R, dim), dtype=torch.uint8, device=DEV)
+    if fmt == "f8":
+        P.k, P.v = bits.view(torch.float8_e4m3fn), bits.flip(0).contiguous().view(torch.float8_e4m3fn)
+        P.ex = torch.randint(110, 140, (pages, R, 2), dtype=torch.uint8, device=DEV)
+    else:
+        P.k, P.v = bits.bfloat16(), bits.flip(0).bfloat16()
+    slots = torch.randperm(pages * R, device=DEV)[:tokens * Hkv].view(tokens, Hkv)
+    slots[-5:] = -1
+    out = torch.full((tokens, 2 * Hkv, dim), KEEP, dtype=torch.bfloat16, device=DEV)
+    d.dkv_paged_load(slots, P.k, P.v, out[:, :Hkv], out[:, Hkv:], scales=P.ex)
+    assert (out[-5:] == KEEP).all()
+    at = slots[:-5]
+    for i, pool in enumerate((P.k, P.v)):
+        want = pool.view(torch.uint8 if fmt == "f8" else torch.int16).view(pages * R, dim)[at]
+        if fmt == "f8":
+            values = torch.from_numpy(tc.codes_to_values(np.arange(256))).to(DEV, torch.float32)[want.int()]
+            want = (values.double() * torch.ldexp(torch.ones((), dtype=torch.float64, device=DEV),
+                                                  P.ex[..., i].reshape(-1)[at].int() - 127)[..., None]).bfloat16()
+        else:
+            want = want.view(torch.bfloat16)
+        assert torch.equal(out[:-5, i * Hkv:(i + 1) * Hkv], want)
