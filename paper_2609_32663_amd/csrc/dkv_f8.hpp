@@ -85,11 +85,14 @@ __device__ __forceinline__ F8Keys f8_keys(const uint2 (&w)[2]) {
   return k;
 }
 
-// Two weights as two fp16 pairs.
+// Two weights as two fp16 pairs: rounded towards zero, and what that left out
+// (exact, in one mixed-precision instruction each; conversions and differences,
+// as the compiler forms them, take two).
 __device__ __forceinline__ void f16_parts(float x0, float x1, uint32_t& a, uint32_t& b) {
-  const auto h = __builtin_amdgcn_cvt_pkrtz(x0, x1);
-  const float r0 = __builtin_fmaf((float)h[0], -1.f, x0), r1 = __builtin_fmaf((float)h[1], -1.f, x1);
-  a = __builtin_bit_cast(uint32_t, h);
+  a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x0, x1));
+  float r0, r1;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r0) : "v"(a), "v"(x0));
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r1) : "v"(a), "v"(x1));
   b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(r0, r1));
 }
 

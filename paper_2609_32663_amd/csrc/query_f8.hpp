@@ -116,30 +116,21 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
                      (uint32_t)__builtin_amdgcn_readfirstlane(coming[i][2]),
                      (uint32_t)__builtin_amdgcn_readfirstlane(coming[i][3])};
   };
-  // What follows from the lane is formed anew each time: kept for the whole walk
-  // it does not fit the registers, and a reload from scratch memory waits for
-  // every load on its way.
-  auto lane_anew = [&]() __attribute__((always_inline)) {
-    int x = lane;
-    asm volatile("" : "+v"(x));
-    return x;
-  };
   // lane l: row l % 8 of the wave's eight, 16 bytes l / 8 of it (64 dims: the first 32 lanes)
   auto raw_rows = [&](const TileRun (&u)[2]) __attribute__((always_inline)) {
-    const int now = lane_anew();
     const TileRun& x = wave_u >= 4 ? u[1] : u[0];
     const uint64_t at = (uint64_t)(x.off_hi & 0xFFFF) << 32 | x.off;  // of the run's first slot that counts
     const uint32_t row = (uint32_t)(8 * (wave_u & 3));
-    const uint32_t off = (row + (now & 7) - x.lo()) * D + 16 * (now >> 3);
+    const uint32_t off = (row + (lane & 7) - x.lo()) * D + 16 * (lane >> 3);
     const __amdgpu_buffer_rsrc_t ks = q_rsrc(static_cast<const char*>(p.k) + at, x.bytes);
     const __amdgpu_buffer_rsrc_t vs = q_rsrc(static_cast<const char*>(p.v) + at, x.bytes);
-    if (D == 128 || now < 32) {
+    if (D == 128 || lane < 32) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           ks, (__attribute__((address_space(3))) void*)(raw_k + 8 * D * wave_u), 16, off, 0, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           vs, (__attribute__((address_space(3))) void*)(raw_v + 8 * D * wave_u), 16, off, 0, 0, 0);
     }
-    if (now == 0)
+    if (lane == 0)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           q_rsrc(reinterpret_cast<const char*>(p.scales) + 2 * (at / D - x.lo()), x.bytes > 0 ? 2 * kRun : 0),
           (__attribute__((address_space(3))) void*)(exps + 16 * wave_u), 16, 2 * row, 0, 0, 0);
@@ -150,8 +141,8 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
   uint2 rk[D / 64], rv[D / 64];
   uint32_t rx;
   auto read_raw = [&]() __attribute__((always_inline)) {
-    const int now = lane_anew(), row = now & 7, col = now >> 3;
-    const int at = 8 * D * wave_u + (D == 128 ? 16 * now : 16 * (row + 8 * (col >> 1)) + 8 * (col & 1));
+    const int row = lane & 7, col = lane >> 3;
+    const int at = 8 * D * wave_u + (D == 128 ? 16 * lane : 16 * (row + 8 * (col >> 1)) + 8 * (col & 1));
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
       rk[i] = *reinterpret_cast<const uint2*>(raw_k + at + 8 * i);
@@ -160,7 +151,7 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
     rx = *reinterpret_cast<const uint16_t*>(exps + 16 * wave_u + 2 * row);
   };
   auto convert = [&](uint16_t* kb, uint16_t* vb, float* keys) __attribute__((always_inline)) {
-    const int now = lane_anew(), col = now >> 3, R = 8 * wave_u + (now & 7);
+    const int col = lane >> 3, R = 8 * wave_u + (lane & 7);
     // a byte that belongs to no slot of the entry may be that of an infinity
     const float power = f8_power((rx & 0xFF) < 254u ? rx & 0xFF : 254u);
     if (col == 0) {
@@ -181,18 +172,42 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
 
   // ---- 32 keys -----------------------------------------------------------------
   const int32_t pos_all = p.mask != nullptr ? blk.pos0 : paged_pos(blk, min(wave_row0, rows - 1) / p.G) + 1;
-  auto scores = [&](const uint16_t* kb, int half) __attribute__((always_inline)) {
+  // LDS reads go out well before their products: K's of 32 keys at once, V's two
+  // groups of products ahead.  The fences keep the compiler from gathering them in
+  // front of their uses again.
+  u32x4 kf[NU];
+  auto load_k = [&](const uint16_t* kb, int half) __attribute__((always_inline)) {
     const uint16_t* kr = kb + 8 * (half * C::kRowChunks * 32 + lane);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) kf[u] = *reinterpret_cast<const u32x4*>(kr + 8 * 64 * u);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto scores = [&]() __attribute__((always_inline)) {
     f32x16 a = {};
 #pragma unroll
     for (int u = 0; u < NU; ++u)
-      a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(kr + 8 * 64 * u)), __builtin_bit_cast(bf16x8, qb[u]), a,
-          0, 0, 0);
+      a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[u]), __builtin_bit_cast(bf16x8, qb[u]), a, 0,
+                                                  0, 0);
+    __builtin_amdgcn_sched_barrier(0);
     return a;
   };
+  constexpr int NG = NB;  // groups of V: two blocks of one of the two products
+  u32x4 vf[2][2];
+  auto load_v = [&](const uint16_t* vb, int half, int n) __attribute__((always_inline)) {
+    const int j = lane & 15, ch = (lane >> 4) & 1;
+    const uint16_t* vr = vb + (4 * half * (C::kRowChunks / 2) + ch) * 128 + (4 * h + (j >> 2)) * 16 + (j & 3) * 4;
+    const int t = n / (NB / 2), b0 = n % (NB / 2) * 2;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const uint16_t* at = vr + (2 * t * (C::kRowChunks / 2) + 2 * (b0 + b)) * 128;
+      const uint2 w0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at));
+      const uint2 w1 = __builtin_bit_cast(
+          uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + (C::kRowChunks / 2) * 128)));
+      vf[n % 2][b] = u32x4{w0.x, w0.y, w1.x, w1.y};
+    }
+  };
   u32x4 pp[2][2];  // [part][product]
-  auto softmax = [&](f32x16 sc, const TileRun& u, const float* keys) __attribute__((always_inline)) {
+  auto softmax = [&](f32x16 sc, const TileRun& u, const float* keys, const uint16_t* vb, int half) __attribute__((always_inline)) {
     // slots outside the entry, or that one of the wave's rows does not see
     if (!u.whole() || (int32_t)u.pos + kRun > pos_all) {
       asm volatile("");  // keeps this a branch
@@ -238,6 +253,9 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
       }
       exponents();
     }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) load_v(vb, half, n);
+    __builtin_amdgcn_sched_barrier(0);
     float ps = l;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -259,28 +277,19 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
     asm volatile("" : "+v"(l));
   };
   auto outputs = [&](const uint16_t* vb, int half) __attribute__((always_inline)) {
-    const int j = lane & 15, ch = (lane >> 4) & 1;
-    const uint16_t* vr = vb + (4 * half * (C::kRowChunks / 2) + ch) * 128 + (4 * h + (j >> 2)) * 16 + (j & 3) * 4;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int n = 0; n < NG; ++n) {
+      const int t = n / (NB / 2), b0 = n % (NB / 2) * 2;
 #pragma unroll
-      for (int b0 = 0; b0 < NB; b0 += 2) {
-        u32x4 vf[2];
+      for (int part = 0; part < 2; ++part)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint16_t* at = vr + (2 * t * (C::kRowChunks / 2) + 2 * (b0 + b)) * 128;
-          const uint2 w0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at));
-          const uint2 w1 = __builtin_bit_cast(
-              uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + (C::kRowChunks / 2) * 128)));
-          vf[b] = u32x4{w0.x, w0.y, w1.x, w1.y};
-        }
-#pragma unroll
-        for (int part = 0; part < 2; ++part)
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-            o[b0 + b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, pp[part][t]),
-                                                               __builtin_bit_cast(f16x8_t, vf[b]), o[b0 + b], 0, 0, 0);
-      }
+        for (int b = 0; b < 2; ++b)
+          o[b0 + b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, pp[part][t]),
+                                                             __builtin_bit_cast(f16x8_t, vf[n % 2][b]), o[b0 + b], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (n + 2 < NG) load_v(vb, half, n + 2);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
   // ---- the walk ------------------------------------------------------------------
@@ -327,17 +336,21 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
     read_raw();
     const int first = decltype(two)::value ? 0 : my_half;
     f32x16 sc;
-    if constexpr (decltype(any)::value) sc = scores(kbuf[i], first);
+    if constexpr (decltype(any)::value) {
+      load_k(kbuf[i], first);
+      sc = scores();
+    }
     take_runs(ahead);
     convert(kbuf[1 - i], vbuf[1 - i], kkeys[1 - i]);
     __builtin_amdgcn_sched_barrier(0);
     raw_rows(ahead);
     if constexpr (decltype(any)::value) {
-      softmax(sc, first ? run[i][1] : run[i][0], kkeys[i] + 32 * first);
+      softmax(sc, first ? run[i][1] : run[i][0], kkeys[i] + 32 * first, vbuf[i], first);
+      if constexpr (decltype(two)::value) load_k(kbuf[i], 1);
       outputs(vbuf[i], first);
       if constexpr (decltype(two)::value) {
-        sc = scores(kbuf[i], 1);
-        softmax(sc, run[i][1], kkeys[i] + 32);
+        sc = scores();
+        softmax(sc, run[i][1], kkeys[i] + 32, vbuf[i], 1);
         outputs(vbuf[i], 1);
       }
     }
