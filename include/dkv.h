@@ -27,6 +27,13 @@
  *   dkv_paged_append  new tokens -> their slots in the pages
  *   dkv_paged_query_attn  a chunk of new tokens of every sequence over a paged
  *                     cache, causally
+ *   dkv_rope          rotary positions (dkv_rope_freqs: their frequencies)
+ *   dkv_paged_store   new tokens into a paged cache of bf16 or 8-bit rows, with
+ *                     their rotation (dkv_paged_load: rows back in bf16)
+ *   dkv_tree_plan     positions and ancestors of drafted trees
+ *   dkv_paged_tree_attn  trees, chunks and single tokens over a paged cache of
+ *                     bf16 or 8-bit rows
+ *   dkv_paged_accept  the accepted path of a tree kept in the cache
  *   dkv_topk_pattern  the exact-budget export of a pattern from retention
  *                     probabilities (K_rho largest entries)
  *
@@ -903,7 +910,8 @@ size_t dkv_paged_tree_workspace_bytes(dkv_cache_format format, int32_t batch, in
  * dkv_paged_tree_workspace_bytes and the same rules for the launches.
  * mask_words at most 2^20.
  * Quantised values enter the products exactly; scores, maxima and sums are
- * fp32; a probability enters its product with V as three bf16 parts (24 bits).
+ * fp32; a probability enters its product with V as three bf16 parts (24 bits)
+ * or, with a quantised cache, as two fp16 parts (22 bits).
  */
 dkv_status dkv_paged_tree_attn(dkv_cache_format format, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
                                int32_t head_dim, int32_t num_tokens, int32_t max_q, const void *q, int64_t q_stride,
@@ -931,7 +939,8 @@ dkv_status dkv_paged_tree_attn(dkv_cache_format format, int32_t batch, int32_t n
  *           its own).
  * keep      optional out, uint8 [num_units * Hkv][pages_per_seg]: 1 for the pages
  *           of the first new_len positions, 0 for those behind them: the argument
- *           of dkv_page_release that takes the others back.
+ *           of dkv_page_release that takes the others back (set to 1
+ *           before, so that units that are left out keep theirs).
  * Entries need no change: what lies past a chunk's last position is not read,
  * and the next dkv_page_extend (with new_len as unit_len, after the pages
  * behind it have been released) writes those that change.

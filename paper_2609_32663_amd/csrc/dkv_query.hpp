@@ -153,6 +153,28 @@ inline bool paged_takes_short(int64_t nseg, int64_t rows, int64_t rows_hint) {
            (nseg <= 256 && rows_hint <= 1 << 16);
   return rows <= kShortRows && nseg <= 16 && rows_hint > 0 && rows_hint <= 1 << 17;
 }
+// The same for a quantised cache (us, short blocks / query tiles, 32 query heads
+// on 8 of 128 dims, 128-row pages).
+//   * Up to 64 rows: always.  The short kernels read the codes at 6 TB/s, the tiles
+//     hold one tile's codes on their way (8 rows: 256 segments of 8,000 keys 90 /
+//     182).  They lose a few microseconds at most: 64 rows, 128 segments of 2,000
+//     keys 54 / 51.
+//   * Up to 128 rows: few keys, or few segments, whose keys the short kernels cut
+//     evenly: the tiles convert a key once for all rows, the short kernels once in
+//     each row group (96 rows: 8 segments of 2,000 keys 23 / 32, of 32,000 48 / 55,
+//     of 100,000 104 / 100; 32 of 2,000 36 / 42, of 8,000 55 / 49, of 32,000 134 /
+//     113; 128 of 300 31 / 45, of 2,000 78 / 54, of 32,000 488 / 420; 256 of 300
+//     36 / 33).
+//   * More rows: fewer still (192 rows: 8 segments of 300 keys 37 / 25, of 2,000
+//     32 / 37, of 8,000 41 / 48, of 32,000 79 / 70; 32 of 2,000 54 / 48, of 8,000
+//     94 / 65).
+//   * Without a hint, up to 128 rows: up to 16 segments, as above.
+inline bool paged_f8_takes_short(int64_t nseg, int64_t rows, int64_t rows_hint) {
+  if (rows <= kShortRows / 4) return true;
+  if (rows <= kShortRows / 2)
+    return (rows_hint > 0 && rows_hint <= 1 << 16) || (nseg <= 16 && rows_hint < 1 << 19);
+  return rows <= kShortRows && nseg <= 16 && rows_hint > 1 << 13 && rows_hint <= 1 << 17;
+}
 
 // How a paged call is split: the most units ((segment, query tile) pairs) it
 // can have, and the slices its keys are cut into (0: no split).
@@ -165,7 +187,7 @@ struct PagedPlanShape {
   int32_t rec_rows;
 };
 PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t head_dim, int32_t num_tokens,
-                                int32_t max_q, int64_t rows_hint);
+                                int32_t max_q, int64_t rows_hint, bool f8 = false);
 hipError_t launch_paged_query_attn(const QueryParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_paged_query_short(const QueryParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_paged_tree_attn(const QueryParams& p, int head_dim, hipStream_t stream);

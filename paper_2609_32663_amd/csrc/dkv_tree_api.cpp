@@ -238,7 +238,7 @@ size_t dkv_paged_tree_workspace_bytes(dkv_cache_format format, int32_t batch, in
   if (batch == 0 || num_tokens == 0 || max_q == 0) return 0;
   const dkv::PagedPlanShape sh =
       dkv::paged_plan_shape(batch, num_kv_heads, num_q_heads / num_kv_heads, head_dim, num_tokens,
-                            max_q < num_tokens ? max_q : num_tokens, rows_hint);
+                            max_q < num_tokens ? max_q : num_tokens, rows_hint, format == DKV_CACHE_F8);
   return sh.plan_bytes + sh.rec_bytes;
 }
 
@@ -268,7 +268,7 @@ dkv_status dkv_paged_tree_attn(dkv_cache_format format, int32_t batch, int32_t n
     return DKV_ERR_MISALIGNED;
   const dkv::PagedPlanShape sh =
       dkv::paged_plan_shape(batch, num_kv_heads, num_q_heads / num_kv_heads, head_dim, num_tokens,
-                            max_q < num_tokens ? max_q : num_tokens, rows_hint);
+                            max_q < num_tokens ? max_q : num_tokens, rows_hint, format == DKV_CACHE_F8);
   const size_t need = sh.plan_bytes + sh.rec_bytes;
   if (need > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need)) return DKV_ERR_WORKSPACE;
 

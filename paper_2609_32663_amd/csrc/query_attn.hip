@@ -1517,7 +1517,7 @@ hipError_t launch_query_attn(const QueryParams& p, int head_dim, int64_t grid, h
 constexpr int64_t kWholeTileRows = 2048, kWholeShortRows = 4096;
 
 PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t head_dim, int32_t num_tokens,
-                                int32_t max_q, int64_t rows_hint) {
+                                int32_t max_q, int64_t rows_hint, bool f8) {
   PagedPlanShape sh;
   const int64_t nseg = (int64_t)batch * hkv;
   const int64_t qtiles = ((int64_t)max_q * G + kQRows - 1) / kQRows;
@@ -1530,7 +1530,7 @@ PagedPlanShape paged_plan_shape(int32_t batch, int32_t hkv, int32_t G, int32_t h
   sh.plan_bytes = sh.rec_bytes = 0;
   const int64_t rows = (int64_t)max_q * G;
   sh.rec_rows = (int32_t)((rows + 3) / 4 * 4);
-  sh.shorts = paged_takes_short(nseg, rows, rows_hint);
+  sh.shorts = f8 ? paged_f8_takes_short(nseg, rows, rows_hint) : paged_takes_short(nseg, rows, rows_hint);
   // No split for segments of fewer than two ranges' worth of keys on average,
   // where it saves two launches or one, unless all sequences together have so
   // many rows that one long one among them would be a workgroup's alone (us,

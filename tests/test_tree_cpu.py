@@ -4,6 +4,9 @@ points' refusals (no call passes validation, so nothing reaches a GPU)."""
 
 import ctypes
 import math
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -17,6 +20,7 @@ A = ctypes.c_void_p(0x10000)    # fake 16-byte-aligned device address
 MIS = ctypes.c_void_p(0x10008)  # 8-byte-aligned only
 ODD = ctypes.c_void_p(0x10002)
 NUL = None
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 # ---------------------------------------------------------------------------
@@ -261,6 +265,69 @@ def test_accept_validation():
     for bad in (dict(k=MIS), dict(v=MIS), dict(ex=ODD)):
         assert call(**bad) == d.DKV_ERR_MISALIGNED, bad
     assert call(N=0, first=NUL, path=NUL, n_path=NUL, table=NUL, new_len=NUL) == d.DKV_OK
+
+
+def test_tree_attention_validation():
+    lib = d.library()
+
+    def call(fmt=d.DKV_CACHE_F8, B=2, Hq=8, Hkv=2, dim=128, n=9, most=5, q=A, qs=1024, off=A, first=A, mask=A, words=1, k=A,
+             v=A, ex=A, pages=9, R=128, ent=A, n_ent=A, max_ent=4, scale=0.1, hint=1000, out=A, ws=A, ws_bytes=1 << 30):
+        return lib.dkv_paged_tree_attn(fmt, B, Hq, Hkv, dim, n, most, q, qs, off, first, mask, words, k, v, ex, pages, R, ent,
+                                       n_ent, max_ent, scale, hint, out, ws, ws_bytes, NUL)
+
+    for bad in (dict(fmt=2), dict(fmt=-1), dict(B=-1), dict(Hkv=0), dict(Hq=9), dict(n=-1), dict(most=-1), dict(words=-1),
+                dict(pages=-1), dict(max_ent=-1), dict(scale=float("nan")), dict(scale=float("inf")), dict(qs=1023),
+                dict(qs=1 << 31), dict(q=NUL), dict(off=NUL), dict(first=NUL), dict(k=NUL), dict(v=NUL), dict(ex=NUL),
+                dict(ent=NUL), dict(n_ent=NUL), dict(out=NUL)):
+        assert call(**bad) == d.DKV_ERR_INVALID_ARG, bad
+    for bad in (dict(dim=96), dict(Hq=34, qs=34 * 128), dict(R=48), dict(R=16), dict(pages=1 << 31), dict(B=1025),
+                dict(max_ent=1 << 24), dict(words=(1 << 20) + 1)):
+        assert call(**bad) == d.DKV_ERR_UNSUPPORTED, bad
+    for bad in (dict(q=MIS), dict(k=MIS), dict(v=MIS), dict(ex=MIS), dict(ent=MIS), dict(out=MIS), dict(qs=1028),
+                dict(mask=ODD)):
+        assert call(**bad) == d.DKV_ERR_MISALIGNED, bad
+    big = dict(n=900, most=512, hint=1 << 20)
+    need = lib.dkv_paged_tree_workspace_bytes(d.DKV_CACHE_F8, 2, 8, 2, 128, 900, 512, 1 << 20)
+    assert need > 0
+    for bad in (dict(ws=NUL), dict(ws=MIS), dict(ws_bytes=need - 1)):
+        assert call(**big, **bad) == d.DKV_ERR_WORKSPACE, bad
+    for empty in (dict(B=0), dict(n=0), dict(most=0)):
+        assert call(**empty, q=NUL, out=NUL, off=NUL) == d.DKV_OK
+    for bad in ((2, 2, 8, 2, 128, 9, 5, 0), (1, -1, 8, 2, 128, 9, 5, 0), (1, 2, 8, 3, 128, 9, 5, 0), (1, 2, 8, 2, 80, 9, 5, 0)):
+        assert lib.dkv_paged_tree_workspace_bytes(*bad) == 0
+    assert call(fmt=d.DKV_CACHE_BF16, ex=NUL, q=NUL) == d.DKV_ERR_INVALID_ARG  # no exponents there: q is what is missing
+
+
+TREE_ROUTE = r"""
+#include "dkv_query.hpp"
+#include <cstdio>
+int main() {
+  long long nseg, rows, hint;
+  while (std::scanf("%lld %lld %lld", &nseg, &rows, &hint) == 3)
+    std::printf("%d\n", dkv::paged_f8_takes_short(nseg, rows, hint) ? 1 : 0);
+}
+"""
+
+
+def test_quantised_blocks_take_the_faster_kernel(tmp_path):
+    """The route over a quantised cache at sizes where the two kernels' times are 10% and more apart on an MI355X,
+    at the rule's edges, and without a hint."""
+    cxx, rocm = shutil.which("g++"), "/opt/rocm/include"
+    if cxx is None or not os.path.isdir(rocm):
+        pytest.skip("no host compiler or HIP headers")
+    src, exe = tmp_path / "route.cpp", tmp_path / "route"
+    src.write_text(TREE_ROUTE)
+    subprocess.run([cxx, "-std=c++17", "-D__HIP_PLATFORM_AMD__", f"-I{rocm}",
+                    f"-I{os.path.join(ROOT, 'paper_2609_32663_amd', 'csrc')}", str(src), "-o", str(exe)], check=True)
+    # (segments, query rows, keys per segment, short kernel)
+    sizes = [(256, 8, 8000, 1), (8, 64, 32000, 1), (2048, 64, 0, 1), (8, 96, 2000, 1), (8, 96, 32000, 1), (32, 96, 2000, 1),
+             (32, 96, 8000, 0), (128, 96, 300, 1), (128, 128, 2000, 0), (128, 96, 32000, 0), (16, 65, 1 << 15, 0),
+             (16, 65, (1 << 15) - 1, 1), (17, 128, 3855, 1), (17, 128, 3856, 0), (16, 128, 0, 1), (17, 128, 0, 0),
+             (8, 192, 300, 0), (8, 192, 2000, 1), (8, 192, 32000, 0), (32, 192, 2000, 0), (16, 256, 8192, 1),
+             (16, 256, 8193, 0), (8, 257, 2000, 0), (16, 129, 0, 0)]
+    out = subprocess.run([str(exe)], input="\n".join(f"{n} {r} {n * k}" for n, r, k, _ in sizes), check=True,
+                         capture_output=True, text=True).stdout.split()
+    assert [int(x) for x in out] == [w for *_, w in sizes]
 
 
 def test_binding_refuses_what_the_kernels_would_misread():
