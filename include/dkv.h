@@ -770,7 +770,7 @@ dkv_status dkv_paged_query_attn(dkv_dtype dtype, int32_t batch, int32_t num_q_he
  * infinities) in a pool [num_pages][page_rows][d] of bytes, and an exponent
  * byte 127 + e; code c stands for c * 2^e.  scales is uint8
  * [num_pages][page_rows][2], 16-byte aligned, the bytes of the K and the V row.  e is the smallest
- * with the row's largest magnitude at most 448 * 2^e, within [-117, 120]; codes
+ * with the row's largest magnitude at most 448 * 2^e, within [-60, 120]; codes
  * are rounded to nearest, ties to even.  NaN and infinities become NaN, and do
  * not count for e.  A value is off by at most 2^-4 of itself, or 2^-10 * 2^e.
  * Pages, tables, slots and entries are the same for both formats.
@@ -903,6 +903,10 @@ size_t dkv_paged_tree_workspace_bytes(dkv_cache_format format, int32_t batch, in
  *           DKV_CACHE_F8, 16-byte aligned.
  * out       [num_tokens][Hq][d] fp32; zeros for a token that sees nothing.  Rows
  *           of no sequence are left as they were.
+ * DKV_CACHE_F8: |sm_scale q k| below 2^23 and |V| below 2^25; the sum of the
+ * probabilities is off beyond (a key's share of it counts down to 2^-56 of the
+ * largest within).  The exponent bytes are those that dkv_paged_store writes, 67
+ * to 247.
  * q, sm_scale, and the K and V of all positions below first_pos[b] + (new tokens)
  * that entries name must be finite, also those of new tokens that a mask
  * hides; other slots may hold anything.

@@ -43,7 +43,7 @@ def quantise(x):
     x = np.asarray(x, dtype=np.float64)
     finite = np.isfinite(x)
     most = np.where(finite, np.abs(x), 0.0).max(axis=-1)
-    e = np.full(most.shape, -117, dtype=np.int64)
+    e = np.full(most.shape, -60, dtype=np.int64)
     while True:  # the smallest exponent that is large enough
         small = (most > 448.0 * 2.0 ** e) & (e < 120)
         if not small.any():

@@ -16,9 +16,11 @@ namespace dkv {
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
-// e stays within [-117, 120]: the smallest code, 2^-9, is then a normal bf16
-// and 2^(127 - e) a normal fp32.
-constexpr int kF8MinExp = -117, kF8MaxExp = 120;
+// e stays within [-60, 120].  The lower end is for attention, whose weights carry
+// 2^e of V's rows (below): a row of zeros would otherwise have e = -117, and
+// beside rows of 2^7 the weight of a key that counts 2^-17 of another would
+// leave fp32's range, and that share of the sum with it.
+constexpr int kF8MinExp = -60, kF8MaxExp = 120;
 
 // Exponent of a row whose largest finite magnitude has these fp32 bits.
 __device__ __forceinline__ int f8_exponent(uint32_t amax) {
@@ -60,11 +62,15 @@ __device__ __forceinline__ uint32_t f8_pair_f16(uint32_t codes) {
 // them by 2^7: the smaller ones then stay clear of fp16's subnormals, and 2^(7 + 8)
 // of a lazy maximum below its largest), for which codes, exact in fp16, need one
 // product less than bf16 parts do.  The sum of the probabilities takes 2^-e_j back, in
-// fp32.  It could only overflow where thousands of keys with |V| below 2^-100
-// outweigh all others: kept below 2^126 it is then still no infinity, and the
-// output zero.  A row that has seen no key has M = kF8None.
+// fp32 (at most 2^(15 + 60) a key).  A key's share of it is lost where its weight
+// leaves fp32: 2^(s_j + e_j) below 2^-133 of the largest, with |V| below 2^25 throughout
+// (e_j from -60 to 17) a probability below 2^-56 of the largest.
+// A row that has seen no key has M = kF8None.
+//
+// s_j + e_j - M is exact in its whole part below 2^24.  Scores beyond that are off
+// by units anyway; kF8Top then keeps the exponents finite.
 constexpr float kF8Up = 7.f;
-constexpr float kF8SumMax = 0x1p126f;
+constexpr float kF8Top = 16.f;  // above kF8Up and a lazy maximum's 8
 constexpr float kF8None = -0x1p127f;
 
 struct F8Keys {

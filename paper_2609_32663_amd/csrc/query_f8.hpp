@@ -2,13 +2,17 @@
 // over key tiles [t_lo, t_hi), as query_item does it for bf16 pools (included by
 // query_attn.hip, whose items, tables and records these are).
 //
-// A SIMD issues vector instructions of one wave at half its rate, so the two
-// waves of a SIMD must not take turns between products and vector work, as the
-// bf16 tiles' waves do: a vector phase of 200 instructions is then as long as
-// both phases' work together (six quarters of the time went into meetings and
-// half-idle issue, 7,000 cycles a tile; without its products a tile took as long).
-// Here every wave runs through its keys by itself and meets the others once per
-// 64-key tile; while one waits for the matrix unit the other has the vector unit.
+// A SIMD issues vector instructions of one wave at half its rate (2.3 ns each, 1.0
+// with two waves at it), so the two waves of a SIMD must not take turns between
+// products and vector work, as the bf16 tiles' waves do: a vector phase is then as
+// long as both waves' vector work together.  Here every wave runs through its keys
+// by itself and meets the others once per 64-key tile; while one waits for the
+// matrix unit the other has the vector unit (24 tokens of 16 requests over 16K in turns
+// 152 us, so 133).  What bounds it, for 512 tokens over 32K (8 heads of 128, 390 us with plan
+// and merge): three products a pair of key and query, 155 us of matrix instructions at the
+// rate that a loop of nothing else reaches, and the vector work of the softmax
+// beside them, which adds to that nearly in full (without the products of V 128 us
+// less, without the softmax 114, without the conversion 25).
 //
 //   * Waves are 32 query rows each: eight of them, or, with at most 128 rows, four
 //     times two that share the rows and take a tile's halves (a key half each),
@@ -252,6 +256,8 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
         for (int b = 0; b < NB; ++b) o[b][i] *= a;
       }
       exponents();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = fminf(x[i], kF8Top);
     }
 #pragma unroll
     for (int n = 0; n < 2; ++n) load_v(vb, half, n);
@@ -273,7 +279,7 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
         pp[1][i >> 1][2 * (i & 1) + v / 2] = w[1];
       }
     }
-    l = fminf(ps, kF8SumMax);
+    l = ps;
     asm volatile("" : "+v"(l));
   };
   auto outputs = [&](const uint16_t* vb, int half) __attribute__((always_inline)) {
@@ -400,7 +406,7 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
       const float m1 = ml[lane], l1 = ml[64 + lane];
       const float M = fmaxf(m, m1);
       const float f0 = fast_exp2(m - M), f1 = fast_exp2(m1 - M);
-      l = fminf(l * f0 + l1 * f1, kF8SumMax);
+      l = l * f0 + l1 * f1;
       m = M;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {

@@ -510,6 +510,10 @@ void query_short_kernel(QueryParams p) {
               for (int b = 0; b < C::kBlocks; ++b) o[q][b][v] *= av;
             }
             exponents();
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) x[j][v] = fminf(x[j][v], kF8Top);
           }
           float ps = l[q];
 #pragma unroll
@@ -519,7 +523,7 @@ void query_short_kernel(QueryParams p) {
               sc[q][j][v] = fast_exp2(x[j][v]);
               ps = __builtin_fmaf(sc[q][j][v], key.back[4 * j + v], ps);
             }
-          l[q] = fminf(ps, kF8SumMax);
+          l[q] = ps;
           asm volatile("" : "+v"(l[q]));
 #pragma unroll
           for (int e = 0; e < 4; ++e) {

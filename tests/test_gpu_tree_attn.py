@@ -52,7 +52,8 @@ def random_mask(rng, new, tokens, words, kind):
 class Batch:
     """Sequences that hold held[b] positions and bring new[b] tokens; keep < 1: a selection's runs of the held ones."""
 
-    def __init__(self, rng, fmt, held, new, Hkv, G, dim, R, keep=1.0, mask="tree", spare=3, pad=0, extra_words=0, kscale=1.0):
+    def __init__(self, rng, fmt, held, new, Hkv, G, dim, R, keep=1.0, mask="tree", spare=3, pad=0, extra_words=0, kscale=1.0,
+                 vsizes=(1e-3, 1.0, 30.0)):
         B, self.Hkv, self.G, self.dim, self.R, self.fmt = len(held), Hkv, G, dim, R, fmt
         held, new = np.asarray(held), np.asarray(new)
         start = np.full(B, int(held.max())) if keep < 1.0 else held
@@ -83,7 +84,7 @@ class Batch:
             lists.append(runs)
             for page, _, lo, hi in runs:
                 for i, pool in enumerate((self.k, self.v)):
-                    x = rng.standard_normal((hi - lo, dim)) * (kscale if i == 0 else rng.choice([1e-3, 1.0, 30.0], size=(hi - lo, 1)))
+                    x = rng.standard_normal((hi - lo, dim)) * (kscale if i == 0 else rng.choice(vsizes, size=(hi - lo, 1)))
                     if f8:
                         c, e = tc.quantise(x)
                         codes[i][page, lo:hi], exps[page, lo:hi, i] = c, e
@@ -255,6 +256,28 @@ def test_scales_and_large_logits(d, fmt):
         for n in (2, 20, 90):
             rng = np.random.default_rng(n)
             Batch(rng, fmt, [300], [n], 1, 4, 128, 64, kscale=kscale).check(d, scale=scale)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n", [1, 10, 40, 200])
+def test_rows_of_v_far_apart(d, fmt, dim, n):
+    """Rows of zeros and of 2^-40 beside rows of 1 and of 2^20, at probabilities that differ as much: a key's share of the
+    sum must not depend on the size of its V (the share of one of 2^-60 beside one of 2^24 counts down to 2^-49, beyond
+    the tolerance); one or two large rows among zeros."""
+    for vsizes in ((0.0, 2.0 ** -40, 1.0, 2.0 ** 20), (0.0,) * 60 + (100.0,), (0.0,)):
+        rng = np.random.default_rng([dim, n])
+        b = Batch(rng, fmt, [900, 3], [n, 1], 2, 4, dim, 64, kscale=1.5, vsizes=vsizes)
+        got = b.check(d, scale=0.7)
+        assert vsizes != (0.0,) or (got == 0).all()
+
+
+@pytest.mark.parametrize("n", [1, 10, 40, 200])
+def test_scores_beyond_the_range_stay_finite(d, n):
+    """Quantised, scores of 2^25 to 2^100: which keys win is lost to rounding, but nothing overflows."""
+    for scale in (1e6, -1e12, 1e30):
+        b = Batch(np.random.default_rng(n), "f8", [700], [n], 1, 4, 128, 64)
+        assert torch.isfinite(b.run(d, scale=scale)).all()
 
 
 @pytest.mark.parametrize("fmt", FMTS)

@@ -54,12 +54,13 @@ def test_codes_are_torchs_e4m3():
 
 
 @pytest.mark.parametrize("most, e", [(448.0, 0), (448.0000001, 1), (1.75, -8), (1.7500001, -7), (1.0, -8), (2.0, -7),
-                                     (0.0, -117), (1e-38, -117), (3.0e38, 120), (2.0 ** -109, -117)])
+                                     (0.0, -60), (1e-38, -60), (3.0e38, 120), (1.75 * 2.0 ** -51, -59),
+                                     (1.75 * 2.0 ** -52, -60), (2.0 ** -52, -60)])
 def test_exponent_of_a_row(most, e):
     codes, ex = tc.quantise(np.array([[most, -most / 3, 0.0]]))
     assert int(ex[0]) - 127 == e
     v = tc.row_values(codes, ex)[0]
-    if most >= 2.0 ** -109:
+    if most >= 2.0 ** -52:
         assert abs(v[0] - most) <= most * 2.0 ** -4
 
 
