@@ -9,10 +9,13 @@
 // by itself and meets the others once per 64-key tile; while one waits for the
 // matrix unit the other has the vector unit (24 tokens of 16 requests over 16K in turns
 // 152 us, so 133).  What bounds it, for 512 tokens over 32K (8 heads of 128, 390 us with plan
-// and merge): three products a pair of key and query, 155 us of matrix instructions at the
-// rate that a loop of nothing else reaches, and the vector work of the softmax
-// beside them, which adds to that nearly in full (without the products of V 128 us
-// less, without the softmax 114, without the conversion 25).
+// and merge): three products a pair of key and query, 200 us of matrix instructions at the
+// rate that a loop of nothing else reaches (2.08 PFLOP/s), and the vector work of the
+// softmax beside them, which adds to that nearly in full (without the products of V
+// 128 us less, without the softmax 114, without the conversion 25).  With up to 128 rows a
+// SIMD has one wave or two at work, and a tile is as long as their chain of
+// phases (1.3 us with 32 rows, 1.6 with 96).  Two tiles' rows on their way, in registers,
+// gain 6% with 64 dims or up to 64 rows and lose 4% at 96 rows of 128 dims to spills.
 //
 //   * Waves are 32 query rows each: eight of them, or, with at most 128 rows, four
 //     times two that share the rows and take a tile's halves (a key half each),
@@ -57,9 +60,12 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
   const int g = s - bseq * p.Hkv;
   const int64_t tok_row0 = blk.tok0;
 
-  // this wave's rows and key half (-1: both)
+  // This wave's rows and key half (-1: both).  Waves w and w + 4 share a SIMD: the
+  // halves of the same rows go to different ones, so that up to 64 rows use all
+  // four (16 requests of 4 to 256 rows over up to 16K keys 206 us, so 199; of 64 rows over
+  // 16K, in these tiles, 197 and 179).
   const bool halves = rows - qt * kQRows <= kQRows / 2;
-  const int row_wave = halves ? wave_u & 3 : wave_u;
+  const int row_wave = halves ? (wave_u + 2 * (wave_u >> 2)) & 3 : wave_u;
   const int my_half = halves ? wave_u >> 2 : -1;
   const int wave_row0 = qt * kQRows + 32 * row_wave;
   const bool some = wave_row0 < rows;
@@ -388,7 +394,7 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
   // ---- the two key halves' waves; row totals; the output or this range's record ----
   if (halves) {
     __syncthreads();  // nobody reads tiles any more
-    // Wave w + 4 hands its rows to wave w: 16 KB (8 with 64 dims) of accumulators through a tile
+    // The second half's waves hand theirs over: 16 KB (8 with 64 dims) of accumulators through a tile
     // buffer, maximum and sum through the codes' room.
     f32x4* const hand = reinterpret_cast<f32x4*>((row_wave & 2) ? ((row_wave & 1) ? v1 : v0) : ((row_wave & 1) ? k1 : k0));
     float* const ml = reinterpret_cast<float*>(raw_k) + 128 * row_wave;
