@@ -146,8 +146,12 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
           (__attribute__((address_space(3))) void*)(exps + 16 * wave_u), 16, 2 * row, 0, 0, 0);
   };
   // Row l % 8, D / 8 codes l / 8.  K's layout, in 16-byte chunks: ((R / 32) *
-  // kRowChunks + c) * 32 + R % 32, so that a product's lanes read 64 in a row; V's as
-  // in query_item.
+  // kRowChunks + c) * 32 + (R + 8 (c % 2)) % 32, so that a product's lanes read 32 in a
+  // row; V's: ((R / 8) * kRowChunks / 2 + c / 2) * 16 + 2 (R % 8 ^ 4 (c / 2 % 2)) + c % 2.  The
+  // turn by 8 rows and the exchange of 4, and odd columns' eights in the other order,
+  // keep the lanes that write or read together in different banks (a tenth of the
+  // kernel's cycles were conflicts, a third of that is left; trees of 48 over 32K 432 -> 427 us).
+  const int swap = D == 128 ? (lane >> 3) & 1 : 0;
   uint2 rk[D / 64], rv[D / 64];
   uint32_t rx;
   auto read_raw = [&]() __attribute__((always_inline)) {
@@ -155,8 +159,8 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
     const int at = 8 * D * wave_u + (D == 128 ? 16 * lane : 16 * (row + 8 * (col >> 1)) + 8 * (col & 1));
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
-      rk[i] = *reinterpret_cast<const uint2*>(raw_k + at + 8 * i);
-      rv[i] = *reinterpret_cast<const uint2*>(raw_v + at + 8 * i);
+      rk[i] = *reinterpret_cast<const uint2*>(raw_k + at + 8 * (i ^ swap));
+      rv[i] = *reinterpret_cast<const uint2*>(raw_v + at + 8 * (i ^ swap));
     }
     rx = *reinterpret_cast<const uint16_t*>(exps + 16 * wave_u + 2 * row);
   };
@@ -170,11 +174,11 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
     }
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
-      const int c = D / 64 * col + i;  // eight columns
-      *reinterpret_cast<u32x4*>(kb + 8 * (((R / 32) * C::kRowChunks + c) * 32 + R % 32)) =
+      const int c = D / 64 * col + (i ^ swap);  // eight columns
+      *reinterpret_cast<u32x4*>(kb + 8 * (((R / 32) * C::kRowChunks + c) * 32 + (R + 8 * (c & 1)) % 32)) =
           u32x4{f8_pair<false>(rk[i].x, power), f8_pair<true>(rk[i].x, power), f8_pair<false>(rk[i].y, power),
                 f8_pair<true>(rk[i].y, power)};
-      *reinterpret_cast<u32x4*>(vb + 8 * (((R / 8) * (C::kRowChunks / 2) + c / 2) * 16 + (R % 8) * 2 + c % 2)) =
+      *reinterpret_cast<u32x4*>(vb + 8 * (((R / 8) * (C::kRowChunks / 2) + c / 2) * 16 + (R % 8 ^ 4 * (c / 2 & 1)) * 2 + c % 2)) =
           u32x4{f8_pair_f16<false>(rv[i].x), f8_pair_f16<true>(rv[i].x), f8_pair_f16<false>(rv[i].y),
                 f8_pair_f16<true>(rv[i].y)};
     }
@@ -187,7 +191,7 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
   // front of their uses again.
   u32x4 kf[NU];
   auto load_k = [&](const uint16_t* kb, int half) __attribute__((always_inline)) {
-    const uint16_t* kr = kb + 8 * (half * C::kRowChunks * 32 + lane);
+    const uint16_t* kr = kb + 8 * ((half * C::kRowChunks + h) * 32 + ((n32 + 8 * h) & 31));
 #pragma unroll
     for (int u = 0; u < NU; ++u) kf[u] = *reinterpret_cast<const u32x4*>(kr + 8 * 64 * u);
     __builtin_amdgcn_sched_barrier(0);
@@ -205,7 +209,7 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
   u32x4 vf[2][2];
   auto load_v = [&](const uint16_t* vb, int half, int n) __attribute__((always_inline)) {
     const int j = lane & 15, ch = (lane >> 4) & 1;
-    const uint16_t* vr = vb + (4 * half * (C::kRowChunks / 2) + ch) * 128 + (4 * h + (j >> 2)) * 16 + (j & 3) * 4;
+    const uint16_t* vr = vb + (4 * half * (C::kRowChunks / 2) + ch) * 128 + (4 * (h ^ ch) + (j >> 2)) * 16 + (j & 3) * 4;
     const int t = n / (NB / 2), b0 = n % (NB / 2) * 2;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {

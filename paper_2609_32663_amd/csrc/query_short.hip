@@ -40,6 +40,14 @@
 // has three bf16 parts.  A decode step of 32 sequences of up to 16,384 positions
 // (1.14 GB of an 8B layer's K and V) takes 181 us, 6.3 TB/s.
 //
+// Quantised pools (F8, dkv_f8.hpp): tiles come as codes, K's codes are converted
+// with their power of two on the way to their product, V's transposed as bytes and
+// converted to fp16.  A key takes half the bytes and the same arithmetic, so two
+// waves a SIMD share it: eight key waves with up to 32 rows (the decode step above,
+// 574 MB with queries and outputs, 94 us, 6.1 TB/s; four key waves and bf16 parts
+// 130).  TREE: a token's own chunk is seen through its mask bits (tree_sees), the
+// rest of the keys without a look at them.
+//
 // Compiled like query_attn.hip (no IEEE mode, no NaN semantics).
 
 #include <hip/hip_runtime.h>
