@@ -280,16 +280,19 @@ __global__ __launch_bounds__(kRotThreads, 4) void rotate_store_kernel(RotatePara
   }
 }
 
-// Waves per token: a whole token to a wave where tokens fill the card (16
-// waves a compute unit), else its row groups over several.
-constexpr int64_t kRotFill = 4096;
+// Waves per token: a whole token to a wave where tokens fill the card, else its
+// row groups over several, up to 8 waves a compute unit where that gives a token
+// three, else 16: more take a second round or the sines' work again (us, up to 8 /
+// 16 / 32 waves, 32 + 8 + 8 heads quantised: 400 tokens 5.1 / 5.9 / 6.6, 1,001 tokens
+// 8.5 / 8.3 / 11.5).
+constexpr int64_t kRotFew = 2048, kRotFill = 4096;
 
 template <typename T, int MODE>
 hipError_t launch_rotate(RotateParams p, hipStream_t stream) {
   const int rows = p.heads + (MODE == kRopeOnly ? 0 : 2 * p.Hkv);
   const int per = kWave / (p.dim / 8);
   const int groups = (rows + per - 1) / per;
-  const int64_t want = (kRotFill + p.tokens - 1) / p.tokens;
+  const int64_t few = kRotFew / p.tokens, want = few >= 3 ? few : kRotFill / p.tokens;
   p.parts = (int32_t)(want < groups ? (want > 1 ? want : 1) : groups);
   const unsigned blocks = (unsigned)(((int64_t)p.tokens * p.parts + kRotWaves - 1) / kRotWaves);
   const bool far = p.pos != nullptr && !p.interleaved && p.pairs % 8 != 0;
