@@ -332,6 +332,7 @@ dkv_status dkv_paged_accept(dkv_cache_format format, int32_t num_units, int32_t 
   if (first_pos == nullptr || n_path == nullptr || new_len == nullptr || (max_path > 0 && path == nullptr) ||
       (pages_per_seg > 0 && page_table == nullptr))
     return DKV_ERR_INVALID_ARG;
+  if (new_len == first_pos) return DKV_ERR_INVALID_ARG;  // a unit's segments read the one, the first writes the other
   if (num_pages > 0 && (k_pages == nullptr || v_pages == nullptr || (format == DKV_CACHE_F8 && scales == nullptr)))
     return DKV_ERR_INVALID_ARG;
   if (!aligned16(k_pages) || !aligned16(v_pages) || (format == DKV_CACHE_F8 && !aligned16(scales)))

@@ -253,12 +253,12 @@ def test_accept_validation():
     lib = d.library()
 
     def call(fmt=d.DKV_CACHE_F8, N=4, B=2, Hkv=2, dim=128, first=A, path=A, n_path=A, most=8, table=A, pps=5, R=128, k=A, v=A,
-             ex=A, pages=9, new_len=A, keep=A):
+             ex=A, pages=9, new_len=ctypes.c_void_p(0x20000), keep=A):
         return lib.dkv_paged_accept(fmt, N, B, Hkv, dim, first, path, n_path, most, table, pps, R, k, v, ex, pages, new_len,
                                     keep, NUL)
 
     for bad in (dict(fmt=3), dict(N=-1), dict(B=-1), dict(B=0), dict(B=3), dict(Hkv=0), dict(most=-1), dict(pps=-1),
-                dict(pages=-1), dict(first=NUL), dict(path=NUL), dict(n_path=NUL), dict(table=NUL), dict(new_len=NUL),
+                dict(pages=-1), dict(first=NUL), dict(path=NUL), dict(n_path=NUL), dict(table=NUL), dict(new_len=NUL), dict(new_len=A),
                 dict(k=NUL), dict(v=NUL), dict(ex=NUL)):
         assert call(**bad) == d.DKV_ERR_INVALID_ARG, bad
     for bad in (dict(dim=32), dict(R=33), dict(most=65), dict(N=32768, B=2), dict(pages=1 << 31)):
