@@ -143,3 +143,60 @@ def test_prompts_whose_tiles_stay_whole(d, fmt, dim, masked):
             err = (out[b * n:(b + 1) * n, g * G + h].double() - p @ v).abs().amax(1)
             tol = (4 * dim ** 0.5 * big[:, h] + 16 + 4 * n ** 0.5) * 2.0 ** -24 * (p @ v.abs()).amax(1)
             assert (err <= tol).all(), (s, h, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("fmt", ["f8", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("gaps", [False, True])
+def test_ranges_of_more_runs_than_a_table_holds(d, fmt, dim, gaps):
+    """32 sequences of 70,000 positions, 96 rows for each of 8 heads: a workgroup walks a whole segment, 2,188 runs of 32
+    rows, whose table is filled twice; whole pages, and pages of which a part is kept.  Pages are shared."""
+    Hkv, G, R, B, n, held, pool = 8, 4, 128, 32, 24, 70000, 300
+    gen = torch.Generator(device=DEV).manual_seed(dim)
+    rand = lambda *s: torch.randn(*s, generator=gen, device=DEV)  # noqa: E731
+    i32 = lambda x: torch.as_tensor(np.asarray(x), device=DEV).to(torch.int32)  # noqa: E731
+    T = held + n
+    per, tokens = -(-T // R), B * n
+    entries = torch.zeros((B * Hkv, per, 4), dtype=torch.int32, device=DEV)
+    entries[..., 0] = torch.randint(pool, entries.shape[:2], generator=gen, device=DEV)
+    entries[..., 1] = torch.arange(per, device=DEV)
+    entries[..., 3] = (T - entries[..., 1] * R).clamp(0, R)
+    if gaps:
+        entries[:, :-2, 2] = torch.randint(0, R, (B * Hkv, per - 2), generator=gen, device=DEV).to(torch.int32)
+    scales = None
+    if fmt == "f8":
+        pools = [(100 * rand(pool, R, dim)).clamp(-448, 448).to(torch.float8_e4m3fn) for _ in range(2)]
+        scales = torch.randint(117, 123, (pool, R, 2), generator=gen, device=DEV).to(torch.uint8)
+        values = [p.double() * torch.exp2(scales[..., i:i + 1].double() - 127) for i, p in enumerate(pools)]
+    else:
+        pools = [rand(pool, R, dim).bfloat16() for _ in range(2)]
+        values = [p.double() for p in pools]
+    q = rand(tokens, Hkv * G, dim).bfloat16()
+    off, first = i32(np.arange(B + 1) * n), i32([held] * B)
+    code, hint = d.DKV_CACHE_F8 if fmt == "f8" else d.DKV_CACHE_BF16, B * Hkv * per * R
+    ws = torch.full((d.dkv_paged_tree_workspace_bytes(code, B, Hkv * G, Hkv, dim, tokens, n, hint),), 0xFF, dtype=torch.uint8,
+                    device=DEV)
+    # a tree: token t continues t - 3
+    pos, mask = torch.empty(tokens, dtype=torch.int32, device=DEV), torch.zeros(tokens, 1, dtype=torch.int64, device=DEV)
+    d.dkv_tree_plan(off, first, n, pos, parent=i32(np.tile(np.arange(n) - 3, B)), mask=mask)
+    out = torch.empty((tokens, Hkv * G, dim), device=DEV)
+    d.dkv_paged_tree_attn(q, off, first, *pools, entries, i32([per] * (B * Hkv)), dim ** -0.5, out, ws, Hkv, n, mask=mask,
+                          scales=scales, rows_hint=hint)
+    slot, at = torch.arange(R, device=DEV), torch.arange(n, device=DEV)
+    sees = (at[:, None] - at[None] >= 0) & ((at[:, None] - at[None]) % 3 == 0)
+    for s in range(0, B * Hkv, 51):
+        b, g = divmod(s, Hkv)
+        e = entries[s].long()
+        kept = ((slot >= e[:, 2:3]) & (slot < e[:, 3:4])).view(-1)
+        where = torch.arange(per * R, device=DEV)[kept]
+        k, v = (x[e[:, 0]].view(per * R, dim)[kept] for x in values)
+        ok = torch.ones(n, len(where), dtype=torch.bool, device=DEV)
+        new = where >= held
+        ok[:, new] = sees[:, where[new] - held]
+        qs = q[b * n:(b + 1) * n, g * G:(g + 1) * G].double()
+        big = dim ** -0.5 * qs.abs().amax(2) * k.abs().sum(1).max()
+        for h in range(G):
+            p = (qs[:, h] @ k.T * dim ** -0.5).masked_fill(~ok, -float("inf")).softmax(1)
+            err = (out[b * n:(b + 1) * n, g * G + h].double() - p @ v).abs().amax(1)
+            tol = (4 * dim ** 0.5 * big[:, h] + 16 + 4 * T ** 0.5) * 2.0 ** -24 * (p @ v.abs()).amax(1)
+            assert (err <= tol).all(), (s, h, float((err / tol).max()))
