@@ -1395,18 +1395,26 @@ __global__ __launch_bounds__(kMergeThreads) void query_merge_kernel(QueryParams 
   *reinterpret_cast<f32x4*>(orow + 4 * c4) = A * inv;
 }
 
-// Combine kernel of paged calls: kParts workgroups per unit that several slices
-// share, as the plan lists them.
+// Combine kernel of paged calls: merge_parts workgroups per unit that several
+// slices share, as the plan lists them; as many as the rows that a unit of this
+// call can have need (for a full tile throughout, trees of up to 24 tokens of 32
+// sequences over 8,000 quantised keys 150 us, so 143).
+template <int D>
+__host__ __device__ inline int merge_parts(const QueryParams& p) {
+  const int rows = p.rows < kQRows ? p.rows : kQRows;
+  return (rows * (D / 4) + kMergeThreads - 1) / kMergeThreads;
+}
+
 template <int D>
 __global__ __launch_bounds__(kMergeThreads, 5) void paged_merge_kernel(QueryParams p) {
   using C = QCfg<D>;
-  constexpr int kParts = kQRows * (D / 4) / kMergeThreads;
-  const int i = blockIdx.x / kParts;
+  const int parts = merge_parts<D>(p);
+  const int i = blockIdx.x / parts;
   const PagedPlan plan = paged_plan_of(p.plan, p.max_items);
   if (i >= plan.head[3]) return;
   const PagedShared x = plan.shared[i];
   const int nr = x.parts;
-  const int it = (blockIdx.x - i * kParts) * kMergeThreads + threadIdx.x;
+  const int it = (blockIdx.x - i * parts) * kMergeThreads + threadIdx.x;
   const int rr = it / (D / 4);
   const int c4 = it - rr * (D / 4);
   const int rq = x.qt * kQRows + rr;
@@ -1464,7 +1472,7 @@ hipError_t launch_paged_d(const QueryParams& p, hipStream_t stream) {
   hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p);
   hipLaunchKernelGGL((paged_query_kernel<D, F8, TREE>), dim3((unsigned)p.P), dim3(kQThreads), 0, stream, p);
   if (p.P > 1)
-    hipLaunchKernelGGL((paged_merge_kernel<D>), dim3((unsigned)((p.P - 1) * (kQRows * (D / 4) / kMergeThreads))),
+    hipLaunchKernelGGL((paged_merge_kernel<D>), dim3((unsigned)((p.P - 1) * merge_parts<D>(p))),
                        dim3(kMergeThreads), 0, stream, p);
   return hipGetLastError();
 }
