@@ -155,22 +155,27 @@ inline bool paged_takes_short(int64_t nseg, int64_t rows, int64_t rows_hint) {
 }
 // The same for a quantised cache (us, short blocks / query tiles, 32 query heads
 // on 8 of 128 dims, 128-row pages).
-//   * Up to 64 rows: always.  The short kernels read the codes at 6 TB/s, the tiles
+//   * Up to 32 rows: always.  The short kernels read the codes at 6 TB/s, the tiles
 //     hold one tile's codes on their way (8 rows: 256 segments of 8,000 keys 90 /
-//     182).  They lose a few microseconds at most: 64 rows, 128 segments of 2,000
-//     keys 54 / 51.
+//     182).
+//   * Up to 64 rows: as well (64 rows: 8 segments of 4,000 keys 24 / 32; 32 of 2,000
+//     29 / 37; 128 of 300 28 / 36, of up to 16,000 105 / 121; 256 of 8,000 157 /
+//     183), but where most segments are cut once or twice, each piece with its fold
+//     and records, and are too short for that (128 of 1,000 47 / 35, of 2,000 54 /
+//     43, of up to 2,000 47 / 43, of up to 4,000 59 / 56, of up to 8,000 75 / 79; 192
+//     of up to 1,000 50 / 48, of up to 4,000 77 / 78).
 //   * Up to 128 rows: few keys, or few segments, whose keys the short kernels cut
 //     evenly: the tiles convert a key once for all rows, the short kernels once in
 //     each row group (96 rows: 8 segments of 2,000 keys 23 / 32, of 32,000 48 / 55,
-//     of 100,000 104 / 100; 32 of 2,000 36 / 42, of 8,000 55 / 49, of 32,000 134 /
-//     113; 128 of 300 31 / 45, of 2,000 78 / 54, of 32,000 488 / 420; 256 of 300
-//     36 / 33).
+//     of 100,000 107 / 100; 32 of 2,000 36 / 42, of 4,000 43 / 39, of 8,000 55 / 48; 128 of
+//     300 31 / 42, of 2,000 78 / 50, of 8,000 159 / 123; 256 of 300 36 / 33).
 //   * More rows: fewer still (192 rows: 8 segments of 300 keys 37 / 25, of 2,000
 //     32 / 37, of 8,000 41 / 48, of 32,000 79 / 70; 32 of 2,000 54 / 48, of 8,000
 //     94 / 65).
-//   * Without a hint, up to 128 rows: up to 16 segments, as above.
+//   * Without a hint: up to 64 rows, and up to 128 over up to 16 segments.
 inline bool paged_f8_takes_short(int64_t nseg, int64_t rows, int64_t rows_hint) {
-  if (rows <= kShortRows / 4) return true;
+  if (rows <= kShortRows / 8) return true;
+  if (rows <= kShortRows / 4) return nseg <= 64 || nseg >= 256 || rows_hint <= 1 << 16 || rows_hint > 1 << 19;
   if (rows <= kShortRows / 2)
     return (rows_hint > 0 && rows_hint <= 1 << 16) || (nseg <= 16 && rows_hint < 1 << 19);
   return rows <= kShortRows && nseg <= 16 && rows_hint > 1 << 13 && rows_hint <= 1 << 17;

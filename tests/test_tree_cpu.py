@@ -321,7 +321,9 @@ def test_quantised_blocks_take_the_faster_kernel(tmp_path):
     subprocess.run([cxx, "-std=c++17", "-D__HIP_PLATFORM_AMD__", f"-I{rocm}",
                     f"-I{os.path.join(ROOT, 'paper_2609_32663_amd', 'csrc')}", str(src), "-o", str(exe)], check=True)
     # (segments, query rows, keys per segment, short kernel)
-    sizes = [(256, 8, 8000, 1), (8, 64, 32000, 1), (2048, 64, 0, 1), (8, 96, 2000, 1), (8, 96, 32000, 1), (32, 96, 2000, 1),
+    sizes = [(256, 8, 8000, 1), (8, 64, 32000, 1), (2048, 64, 0, 1), (128, 64, 2000, 0),
+             (128, 32, 2000, 1), (128, 64, 300, 1), (128, 64, 16000, 1), (64, 64, 4000, 1), (256, 33, 1000, 1), (65, 33, 8065, 0),
+             (65, 33, 8066, 1), (128, 40, 0, 1), (8, 96, 2000, 1), (8, 96, 32000, 1), (32, 96, 2000, 1),
              (32, 96, 8000, 0), (128, 96, 300, 1), (128, 128, 2000, 0), (128, 96, 32000, 0), (16, 65, 1 << 15, 0),
              (16, 65, (1 << 15) - 1, 1), (17, 128, 3855, 1), (17, 128, 3856, 0), (16, 128, 0, 1), (17, 128, 0, 0),
              (8, 192, 300, 0), (8, 192, 2000, 1), (8, 192, 32000, 0), (32, 192, 2000, 0), (16, 256, 8192, 1),
