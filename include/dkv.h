@@ -939,12 +939,13 @@ dkv_status dkv_paged_tree_attn(dkv_cache_format format, int32_t batch, int32_t n
  * The rows of token path[b][i] (position first_pos + path[b][i]) move to position
  * first_pos + i, in every segment's K and V; a row whose page (from or to) is
  * outside the pool does not move.
- * new_len   out, int32 [num_units]: first_pos + accepted tokens (a buffer of
- *           its own).
+ * new_len   out, int32 [num_units]: first_pos + accepted tokens.
  * keep      optional out, uint8 [num_units * Hkv][pages_per_seg]: 1 for the pages
  *           of the first new_len positions, 0 for those behind them: the argument
  *           of dkv_page_release that takes the others back (set to 1
  *           before, so that units that are left out keep theirs).
+ * new_len and keep share no byte with each other or with first_pos, path, n_path
+ * and page_table (DKV_ERR_INVALID_ARG otherwise).
  * Entries need no change: what lies past a chunk's last position is not read,
  * and the next dkv_page_extend (with new_len as unit_len, after the pages
  * behind it have been released) writes those that change.

@@ -17,6 +17,12 @@ namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// Whether [a, a + na) and [b, b + nb) share a byte.
+bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
+  const uint64_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a != nullptr && b != nullptr && (x <= y ? y - x < na : x - y < nb) && na > 0 && nb > 0;
+}
+
 dkv_status hip_status(hipError_t e) { return e == hipSuccess ? DKV_OK : DKV_ERR_HIP; }
 
 bool page_rows_ok(int32_t pr) {
@@ -332,11 +338,18 @@ dkv_status dkv_paged_accept(dkv_cache_format format, int32_t num_units, int32_t 
   if (first_pos == nullptr || n_path == nullptr || new_len == nullptr || (max_path > 0 && path == nullptr) ||
       (pages_per_seg > 0 && page_table == nullptr))
     return DKV_ERR_INVALID_ARG;
-  if (new_len == first_pos) return DKV_ERR_INVALID_ARG;  // a unit's segments read the one, the first writes the other
   if (num_pages > 0 && (k_pages == nullptr || v_pages == nullptr || (format == DKV_CACHE_F8 && scales == nullptr)))
     return DKV_ERR_INVALID_ARG;
   if (!aligned16(k_pages) || !aligned16(v_pages) || (format == DKV_CACHE_F8 && !aligned16(scales)))
     return DKV_ERR_MISALIGNED;
+  // A unit's first segment writes new_len, and every segment its own row of keep, while others still read the
+  // lengths, paths and tables.
+  const uint64_t units = 4 * (uint64_t)num_units, cells = (uint64_t)num_units * num_kv_heads * pages_per_seg;
+  const struct { const void* p; uint64_t n; } read[] = {
+      {first_pos, units}, {path, 4 * (uint64_t)batch * max_path}, {n_path, 4 * (uint64_t)batch}, {page_table, 4 * cells}};
+  for (const auto& in : read)
+    if (overlap(new_len, units, in.p, in.n) || overlap(keep, cells, in.p, in.n)) return DKV_ERR_INVALID_ARG;
+  if (overlap(new_len, units, keep, cells)) return DKV_ERR_INVALID_ARG;
   dkv::AcceptParams p;
   std::memset(&p, 0, sizeof(p));
   p.first_pos = first_pos;
