@@ -838,6 +838,8 @@ dkv_status dkv_rope(dkv_dtype dtype, int32_t num_tokens, int32_t num_heads, int3
  *           set when new token j of the sequence is the token itself or an
  *           ancestor; zeros where pos is -1.  mask_words * 64 must be at least
  *           max_q (or num_tokens, if that is less).
+ * pos may be parent itself; otherwise pos and mask share no byte with each other
+ * or with tok_off, first_pos and parent (DKV_ERR_INVALID_ARG).
  * With parents max_q is at most DKV_MAX_TREE, batch at most DKV_MAX_SEGMENTS
  * (DKV_ERR_UNSUPPORTED otherwise).
  */

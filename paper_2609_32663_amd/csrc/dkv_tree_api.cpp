@@ -224,6 +224,13 @@ dkv_status dkv_tree_plan(int32_t batch, int32_t num_tokens, int32_t max_q, const
   if (num_tokens == 0) return DKV_OK;
   if (tok_off == nullptr || pos == nullptr || (batch > 0 && first_pos == nullptr)) return DKV_ERR_INVALID_ARG;
   if (!aligned(mask, 8)) return DKV_ERR_MISALIGNED;
+  // A sequence's workgroup writes its rows while others still read offsets and parents; its own parents it has read.
+  const uint64_t tokens = 4 * (uint64_t)num_tokens, bits = 8 * (uint64_t)num_tokens * mask_words;
+  const struct { const void* p; uint64_t n; } read[] = {
+      {tok_off, 4 * ((uint64_t)batch + 1)}, {first_pos, 4 * (uint64_t)batch}, {parent, tokens}};
+  for (const auto& in : read)
+    if ((pos != in.p && overlap(pos, tokens, in.p, in.n)) || overlap(mask, bits, in.p, in.n)) return DKV_ERR_INVALID_ARG;
+  if (pos == tok_off || pos == first_pos || overlap(pos, tokens, mask, bits)) return DKV_ERR_INVALID_ARG;
   dkv::TreePlanParams p;
   std::memset(&p, 0, sizeof(p));
   p.tok_off = tok_off;

@@ -47,3 +47,19 @@ def test_accept_takes_neighbouring_parts(d):
     assert f.tolist() == first.tolist() and p.tolist() == path.tolist() and t.tolist() == table.tolist()
     with pytest.raises(d.DkvError):
         d.dkv_paged_accept(f, p, n, t, Hkv, k, v, f, keep=keep)
+
+
+def test_plan_takes_the_parents_place_and_neighbouring_parts(d):
+    rng = np.random.default_rng(4)
+    new = np.array([5, 0, 70, 1, 33])
+    tokens, words = int(new.sum()) + 3, 2
+    off = np.concatenate([[0], np.cumsum(new)])
+    first = np.array([7, 3, 0, 500, -1])
+    parent = rng.integers(-2, 40, size=tokens)
+    want, bits = tc.tree_plan(off, first, 70, tokens, parent, words)
+    o, f, p, pos = _parts(off, first, parent, np.zeros(tokens))
+    for at in (pos, p):
+        mask = torch.zeros((tokens, words), dtype=torch.int64, device="cuda")
+        d.dkv_tree_plan(o, f, 70, at, parent=p, mask=mask)
+        assert at.tolist() == want.tolist() and np.array_equal(mask.cpu().numpy(), bits.view(np.int64))
+        assert o.tolist() == off.tolist() and f.tolist() == first.tolist()

@@ -33,3 +33,26 @@ def test_accept_refuses_outputs_over_its_inputs(out, other):
     unit = 1 if out == "keep" else 4
     for at in (AT[other], AT[other] + BYTES[other] - unit, AT[other] - BYTES[out] + unit):
         assert accept(**{out: at}) == d.DKV_ERR_INVALID_ARG, hex(at - AT[other])
+
+
+PLAN_BYTES = {"off": 4 * 3, "first": 4 * 2, "parent": 4 * 80, "pos": 4 * 80, "mask": 8 * 80 * 2}
+PLAN_AT = {name: 0x10000 * i for i, name in enumerate(PLAN_BYTES, 1)}
+
+
+def plan(**kw):
+    p = {k: ctypes.c_void_p(v) for k, v in {**PLAN_AT, **kw}.items()}
+    return d.library().dkv_tree_plan(2, 80, 70, p["off"], p["first"], p["parent"], p["pos"], p["mask"], 2, None)
+
+
+@pytest.mark.parametrize("out", ["pos", "mask"])
+@pytest.mark.parametrize("other", list(PLAN_BYTES))
+def test_plan_refuses_outputs_over_its_inputs(out, other):
+    """One sequence's workgroup writes its rows while another's reads offsets and parents.  Positions in the very place of
+    the parents are the exception: a workgroup holds its own parents by then."""
+    if out == other:
+        return
+    unit = 8  # of the mask, whose alignment is checked first
+    for at in (PLAN_AT[other], PLAN_AT[other] + (PLAN_BYTES[other] - 1) // unit * unit, PLAN_AT[other] - PLAN_BYTES[out] + unit):
+        if (out, other) == ("pos", "parent") and at == PLAN_AT[other]:
+            continue
+        assert plan(**{out: at}) == d.DKV_ERR_INVALID_ARG, hex(at - PLAN_AT[other])
