@@ -788,7 +788,7 @@ typedef enum dkv_rope_scaling {
   DKV_ROPE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)): the slowest pair divided by factor */
   DKV_ROPE_WAVE = 3,   /* pairs with up to `low` turns over trained_len divided, from `high` on kept, linear between */
   DKV_ROPE_RAMP = 4    /* the same, linear in the pair's index between the pairs with `high` and `low` turns
-                          (rounded outwards); *mscale = 0.1 ln(factor) + 1 */
+                          (rounded outwards, cut to 0 .. rot_dim - 1); *mscale = 0.1 ln(factor) + 1 */
 } dkv_rope_scaling;
 
 /*

@@ -71,8 +71,10 @@ dkv_status dkv_rope_freqs(dkv_rope_scaling kind, int32_t rot_dim, double base, d
   if (kind == DKV_ROPE_RAMP) {
     // the pair that turns t times over the trained length
     const auto pair = [&](double t) { return rot_dim * std::log(trained_len / (2 * pi * t)) / (2 * std::log(base)); };
-    first = std::floor(pair(high));
-    last = std::ceil(pair(low));  // past `first`, as low < high
+    // Cut to a head's indexes before the slope is taken (a fastest pair that turns fewer than `high` times over a short
+    // length stays as it was).
+    first = std::fmax(std::floor(pair(high)), 0.0);
+    last = std::fmin(std::ceil(pair(low)), rot_dim - 1.0);
   }
   for (int32_t i = 0; i < n; ++i) {
     const double f = std::pow(b, -(double)i / n);
@@ -81,7 +83,8 @@ dkv_status dkv_rope_freqs(dkv_rope_scaling kind, int32_t rot_dim, double base, d
     if (bands) {
       double keep;  // how much of the pair stays as trained
       if (kind == DKV_ROPE_WAVE) keep = (trained_len * f / (2 * pi) - low) / (high - low);  // by its turns
-      else keep = 1.0 - (i - first) / (last - first);
+      else if (last > first) keep = 1.0 - (i - first) / (last - first);
+      else keep = i <= last ? 1.0 : 0.0;  // the band lies beyond the indexes
       keep = std::fmin(std::fmax(keep, 0.0), 1.0);
       g = keep * f + (1.0 - keep) * f / factor;
     }
