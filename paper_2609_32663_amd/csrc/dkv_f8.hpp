@@ -21,6 +21,7 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 // beside rows of 2^7 the weight of a key that counts 2^-17 of another would
 // leave fp32's range, and that share of the sum with it.
 constexpr int kF8MinExp = -60, kF8MaxExp = 120;
+constexpr uint32_t kF8MinByte = 127 + kF8MinExp;
 
 // Exponent of a row whose largest finite magnitude has these fp32 bits.
 __device__ __forceinline__ int f8_exponent(uint32_t amax) {
@@ -73,18 +74,23 @@ constexpr float kF8Up = 7.f;
 constexpr float kF8Top = 16.f;  // above kF8Up and a lazy maximum's 8
 constexpr float kF8None = -0x1p127f;
 
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+
 struct F8Keys {
   float byte[8], back[8];  // exponent byte of the lane's key, and 2^(127 - byte)
 };
 
 // From the words of the lane's keys 4kg .. 4kg + 3 of two 16-key blocks
-// (exponent bytes K V K V).
+// (exponent bytes K V K V).  A byte of V below those of the store counts as its
+// least: rows of zeros may come with any (one instruction for two keys, V's
+// bytes being the upper ones).
 __device__ __forceinline__ F8Keys f8_keys(const uint2 (&w)[2]) {
   F8Keys k;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const uint32_t x = (j & 2) ? w[j >> 2].y : w[j >> 2].x;
-    const uint32_t b = (x >> ((j & 1) ? 24 : 8)) & 0xFFu;
+    const u16x2_t x = __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, (j & 2) ? w[j >> 2].y : w[j >> 2].x),
+                                                u16x2_t(kF8MinByte << 8));
+    const uint32_t b = (__builtin_bit_cast(uint32_t, x) >> ((j & 1) ? 24 : 8)) & 0xFFu;
     k.byte[j] = (float)b;
     k.back[j] = __builtin_amdgcn_ldexpf(1.f, 127 - (int)b);
   }

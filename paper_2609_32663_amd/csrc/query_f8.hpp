@@ -169,8 +169,9 @@ __device__ __forceinline__ void f8_item(const QueryParams& p, const QueryItem& i
     // a byte that belongs to no slot of the entry may be that of an infinity
     const float power = f8_power((rx & 0xFF) < 254u ? rx & 0xFF : 254u);
     if (col == 0) {
-      keys[R] = (float)(rx >> 8);
-      keys[kQKeys + R] = __builtin_amdgcn_ldexpf(1.f, 127 - (int)(rx >> 8));
+      const uint32_t byte = rx >> 8 > kF8MinByte ? rx >> 8 : kF8MinByte;  // rows of zeros may come with any
+      keys[R] = (float)byte;
+      keys[kQKeys + R] = __builtin_amdgcn_ldexpf(1.f, 127 - (int)byte);
     }
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
