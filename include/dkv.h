@@ -906,7 +906,7 @@ size_t dkv_paged_tree_workspace_bytes(dkv_cache_format format, int32_t batch, in
  * out       [num_tokens][Hq][d] fp32; zeros for a token that sees nothing.  Rows
  *           of no sequence are left as they were.
  * DKV_CACHE_F8: |sm_scale q k| below 2^23 and |V| below 2^25; the sum of the
- * probabilities is off beyond (a key's share of it counts down to 2^-56 of the
+ * probabilities is off beyond (a key's share of it counts down to 2^-41 of the
  * largest within).  The exponent bytes are those that dkv_paged_store writes, 67
  * to 247; one of a row of V below 67 counts as 67 (a row of zeros may have any).
  * q, sm_scale, and the K and V of all positions below first_pos[b] + (new tokens)

@@ -1,9 +1,10 @@
 // Quantised cache rows: a row of d values is d codes of e4m3 (sign, four
 // exponent and three mantissa bits, no infinities, largest value 448) and one
 // exponent byte 127 + e; code c stands for c * 2^e.  e is the smallest with
-// the row's largest magnitude at most 448 * 2^e, so a value down to 2^-15 of
-// the largest keeps four significant bits.  A power of two rounds nothing by
-// itself, the type being relative already (another factor would round once
+// the row's largest magnitude at most 448 * 2^e, so that lies in (224, 448] codes
+// and a value keeps four significant bits down to the least normal code, 2^-6:
+// 2^-13.8 of the largest (2^-14.8 at best; rows below 448 * 2^-60, whose e would
+// have to be smaller, less).  A power of two rounds nothing by itself, the type being relative already (another factor would round once
 // more, and no value nearer), and every value is exact in bf16.
 #pragma once
 
@@ -63,9 +64,13 @@ __device__ __forceinline__ uint32_t f8_pair_f16(uint32_t codes) {
 // them by 2^7: the smaller ones then stay clear of fp16's subnormals, and 2^(7 + 8)
 // of a lazy maximum below its largest), for which codes, exact in fp16, need one
 // product less than bf16 parts do.  The sum of the probabilities takes 2^-e_j back, in
-// fp32 (at most 2^(15 + 60) a key).  A key's share of it is lost where its weight
-// leaves fp32: 2^(s_j + e_j) below 2^-133 of the largest, with |V| below 2^25 throughout
-// (e_j from -60 to 17) a probability below 2^-56 of the largest.
+// fp32 (at most 2^(16 + 60) a key).  A key's share of it is lost where one factor of it
+// leaves fp32's exponential, at 2^-127: its weight in its tile, below 2^-133 of the
+// largest, or, sooner, a step of M, when a tile's maximum or a fold's other side
+// (key waves and halves, records) raises it by 127 or more.  A key lies at most kLazy = 8
+// above the M that it was summed with, and M less than one above the largest, so
+// no key within 2^-118 of the largest weight is lost; with |V| below 2^25
+// throughout (e_j from -60 to 17) that is a probability of 2^-41 of the largest.
 // A row that has seen no key has M = kF8None.
 //
 // s_j + e_j - M is exact in its whole part below 2^24.  Scores beyond that are off
