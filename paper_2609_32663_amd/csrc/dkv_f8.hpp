@@ -4,8 +4,9 @@
 // the row's largest magnitude at most 448 * 2^e, so that lies in (224, 448] codes
 // and a value keeps four significant bits down to the least normal code, 2^-6:
 // 2^-13.8 of the largest (2^-14.8 at best; rows below 448 * 2^-60, whose e would
-// have to be smaller, less).  A power of two rounds nothing by itself, the type being relative already (another factor would round once
-// more, and no value nearer), and every value is exact in bf16.
+// have to be smaller, keep fewer).  A power of two rounds nothing by itself, the
+// type being relative already (another factor would round once more, and no value
+// nearer), and every value is exact in bf16.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -65,7 +66,7 @@ __device__ __forceinline__ uint32_t f8_pair_f16(uint32_t codes) {
 // of a lazy maximum below its largest), for which codes, exact in fp16, need one
 // product less than bf16 parts do.  The sum of the probabilities takes 2^-e_j back, in
 // fp32 (at most 2^(16 + 60) a key).  A key's share of it is lost where one factor of it
-// leaves fp32's exponential, at 2^-127: its weight in its tile, below 2^-133 of the
+// leaves fp32's exponential, at 2^-127: its weight in its tile, below 2^-132 of the
 // largest, or, sooner, a step of M, when a tile's maximum or a fold's other side
 // (key waves and halves, records) raises it by 127 or more.  A key lies at most kLazy = 8
 // above the M that it was summed with, and M less than one above the largest, so

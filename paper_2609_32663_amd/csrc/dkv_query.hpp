@@ -163,7 +163,12 @@ inline bool paged_takes_short(int64_t nseg, int64_t rows, int64_t rows_hint) {
 //     183), but where most segments are cut once or twice, each piece with its fold
 //     and records, and are too short for that (128 of 1,000 47 / 35, of 2,000 54 /
 //     43, of up to 2,000 47 / 43, of up to 4,000 59 / 56, of up to 8,000 75 / 79; 192
-//     of up to 1,000 50 / 48, of up to 4,000 77 / 78).
+//     of up to 1,000 50 / 48, of up to 4,000 77 / 78; of one length 72 of 1,000 37 / 39, of
+//     2,000 42 / 41, of 6,000 59 / 60; 96 of 1,000 42 / 39, of 4,000 59 / 56, of 7,900 82 /
+//     82; 160 of 500 44 / 40, of 3,000 75 / 66; 248 of 500 54 / 43, of 2,000 83 / 69).
+//     The bound is one of all rows: with more segments it ends at fewer keys of each
+//     than the tiles are ahead at (128 of 6,000 85 / 77; 192 of 3,000 86 / 73, of
+//     6,000 120 / 117; 248 of 4,000 117 / 106, of 6,000 148 / 146).
 //   * Up to 128 rows: few keys, or few segments, whose keys the short kernels cut
 //     evenly: the tiles convert a key once for all rows, the short kernels once in
 //     each row group (96 rows: 8 segments of 2,000 keys 23 / 32, of 32,000 48 / 55,

@@ -6,16 +6,20 @@
 // with two waves at it), so the two waves of a SIMD must not take turns between
 // products and vector work, as the bf16 tiles' waves do: a vector phase is then as
 // long as both waves' vector work together.  Here every wave runs through its keys
-// by itself and meets the others once per 64-key tile; while one waits for the
-// matrix unit the other has the vector unit (24 tokens of 16 requests over 16K in turns
-// 152 us, so 133).  What bounds it, for 512 tokens over 32K (8 heads of 128, 390 us with plan
-// and merge): three products a pair of key and query, 200 us of matrix instructions at the
-// rate that a loop of nothing else reaches (2.08 PFLOP/s), and the vector work of the
-// softmax beside them, which adds to that nearly in full (without the products of V
-// 128 us less, without the softmax 114, without the conversion 25).  With up to 128 rows a
-// SIMD has one wave or two at work, and a tile is as long as their chain of
-// phases (1.3 us with 32 rows, 1.6 with 96).  Two tiles' rows on their way, in registers,
-// gain 6% with 64 dims or up to 64 rows and lose 4% at 96 rows of 128 dims to spills.
+// by itself and meets the others once per 64-key tile, so that the two waves' vector
+// phases can share the unit (24 tokens of 16 requests over 16K in turns 152 us, so
+// 133).  What bounds it is this schedule.  Scores, conversion, softmax and outputs
+// of a wave are one chain, in that order (the fences below keep it), and the two
+// waves of a SIMD start every tile together at the meeting, so little of the
+// matrix work lies beside vector work: for 512 tokens over 32K (8 heads of 128, 371 to
+// 398 us with plan and merge, by card) the matrix units are busy 57% of the time,
+// 51% for trees, and the parts' times nearly add up (without the products of V 128 us
+// less, all of their matrix time, without the softmax 114, without the conversion
+// 25).  Three products a pair of key and query take 200 us at the rate that a loop
+// of matrix instructions alone reaches (2.08 PFLOP/s).  With up to 128 rows a SIMD
+// has one wave or two at work, and a tile is as long as their chain of phases (1.3
+// us with 32 rows, 1.6 with 96).  Two tiles' rows on their way, in registers, gain
+// 6% with 64 dims or up to 64 rows and lose 4% at 96 rows of 128 dims to spills.
 //
 //   * Waves are 32 query rows each: eight of them, or, with at most 128 rows, four
 //     times two that share the rows and take a tile's halves (a key half each),

@@ -282,9 +282,13 @@ __global__ __launch_bounds__(kRotThreads, 4) void rotate_store_kernel(RotatePara
 
 // Waves per token: a whole token to a wave where tokens fill the card, else its
 // row groups over several, up to 8 waves a compute unit where that gives a token
-// three, else 16: more take a second round or the sines' work again (us, up to 8 /
-// 16 / 32 waves, 32 + 8 + 8 heads quantised: 400 tokens 5.1 / 5.9 / 6.6, 1,001 tokens
-// 8.5 / 8.3 / 11.5).
+// three, else 16: with fewer, a token's rows wait for its few waves, more take a
+// second round or the sines' work again (us, up to 8 / 16 waves, 32 + 8 + 8 heads
+// quantised: 400 tokens 5.1 / 5.9, 500 5.6 / 6.6, 600 6.3 / 6.7, 682 6.5 / 6.9; 683
+// 7.6 / 7.2, 760 7.8 / 7.4, 850 8.2 / 7.9, 1,001 8.5 / 8.3, 1,100 12.4 / 9.6, 1,365
+// 12.8 / 10.2, 1,700 13.1 / 12.1, 2,047 13.4 / 12.4; in up to 32 waves 400 tokens 6.6,
+// 1,001 11.5.  bf16 rows alike; 40 heads only rotated as well, but for 850 tokens, 6.2 /
+// 6.4).
 constexpr int64_t kRotFew = 2048, kRotFill = 4096;
 
 template <typename T, int MODE>
