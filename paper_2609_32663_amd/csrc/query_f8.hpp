@@ -12,8 +12,8 @@
 // of a wave are one chain, in that order (the fences below keep it), and the two
 // waves of a SIMD start every tile together at the meeting, so little of the
 // matrix work lies beside vector work: for 512 tokens over 32K (8 heads of 128, 371 to
-// 398 us with plan and merge, by card) the matrix units are busy 57% of the time,
-// 51% for trees, and the parts' times nearly add up (without the products of V 128 us
+// 398 us with plan and merge, by card) the matrix units are busy 56% of the time,
+// 52% for trees of 48, and the parts' times nearly add up (without the products of V 128 us
 // less, all of their matrix time, without the softmax 114, without the conversion
 // 25).  Three products a pair of key and query take 200 us at the rate that a loop
 // of matrix instructions alone reaches (2.08 PFLOP/s).  With up to 128 rows a SIMD
